@@ -55,8 +55,12 @@ enum {
   GBA_DERR_FUTURE_TOKEN = 2,  /* a token newer than the step being applied         */
   GBA_DERR_OFFSETS = 4,       /* contribution offsets not 0 .. N and non-decreasing */
   GBA_DERR_ROW_RANGE = 8,     /* a row index passed to a sparse apply outside [0, R) */
-  GBA_DERR_TABLE_FULL = 16    /* the ID index or the row pool has no room left      */
+  GBA_DERR_TABLE_FULL = 16,   /* the ID index or the row pool has no room left      */
+  GBA_DERR_NONFINITE = 32     /* a gradient norm that is infinite or not a number   */
 };
+
+/* Element types of the worker's operators (32-bit float, bfloat16, half). */
+typedef enum gba_dtype { GBA_F32 = 0, GBA_BF16 = 1, GBA_F16 = 2 } gba_dtype;
 
 /* How embedding gradients are decayed (Alg. 2). */
 typedef enum gba_decay {
@@ -449,6 +453,148 @@ gba_status gba_hash_find_or_insert(int64_t* slot_ids, int32_t* slot_rows, int64_
 gba_status gba_hash_rehash(const int64_t* old_slot_ids, const int32_t* old_slot_rows, int64_t old_capacity,
                            int64_t* new_slot_ids, int32_t* new_slot_rows, int64_t new_capacity, int32_t* err,
                            hipStream_t stream);
+
+/*
+ * ---- The worker's side of a step: the embedding lookup and its gradient,
+ * layer norm, the gradients' norm and clipping.  A worker (Alg. 1) looks up
+ * the rows of its batch, computes a gradient and pushes it; these calls take
+ * it from token IDs to activations and from the activations' gradients to the
+ * contribution that gba_aggregate_* consume.
+ *
+ * Matrices are row-major with their own row strides, counted in elements, of
+ * at least their width; elements of a row are adjacent.  Their pointers need
+ * the alignment of one element only.  Values are read in the type given,
+ * computed in 32 bits or more and rounded to the output's type once.
+ */
+
+/*
+ * Embedding lookup with scaling: out[i][c] = scale * table[ids[i]][c].
+ *   ids     [n] int64.
+ *   table   [R][D] of table_type, out [n][D] of out_type.
+ *   err     GBA_DERR_ID_RANGE for an ID outside [0, R) (its output row is 0).
+ * Limits: 0 <= n < 2^31, 1 <= R <= 2^32, 1 <= D <= 2^20.
+ */
+gba_status gba_embedding_lookup(const int64_t* ids, int64_t n, const void* table, gba_dtype table_type,
+                                int64_t table_stride, int64_t R, int32_t D, float scale, void* out,
+                                gba_dtype out_type, int64_t out_stride, int32_t* err, hipStream_t stream);
+
+/*
+ * The lookup's gradient, by sorted tokens: for each row r of the table
+ *   G[r][c] = scale * (sum over i with ids[i] == r != padding_id of grad[i][c])
+ * summed in 32 bits in a fixed order (the same inputs give the same bits).
+ * A token equal to padding_id takes no part, and its gradient may hold
+ * anything; padding_id < 0: none.
+ *   ids     [n] int64 in [0, R), 16-byte aligned.
+ *   grad    [n][D] of grad_type.
+ *
+ * gba_embedding_grad_rows: one row per distinct ID, as a push takes them.
+ *   unique_ids  [U] int64 out, the distinct IDs ascending (size it for n).
+ *   rows        [U][D] float out (row_stride; size it for n).
+ *   num_unique  one int64 out, U.  What lies past U is left as it was.
+ * gba_embedding_grad_dense: the whole table's gradient.
+ *   table_grad  [R][D] of out_type.  accumulate == 0: written whole, zero
+ *               where no token asked for the row; else G is added to the rows
+ *               that have one and the others are left as they are.
+ * workspace  gba_embedding_grad_workspace_size bytes, 16-byte aligned.
+ * err        GBA_DERR_ID_RANGE for an ID outside [0, R) (outputs then undefined).
+ * Limits: 0 <= n < 2^28, 1 <= R <= 2^32, 1 <= D <= 2^20.
+ */
+gba_status gba_embedding_grad_workspace_size(int64_t n, int32_t D, int64_t R, size_t* bytes /* host out */);
+
+gba_status gba_embedding_grad_rows(const int64_t* ids, int64_t n, const void* grad, gba_dtype grad_type,
+                                   int64_t grad_stride, int32_t D, int64_t R, float scale, int64_t padding_id,
+                                   int64_t* unique_ids, float* rows, int64_t row_stride, int64_t* num_unique,
+                                   void* workspace, size_t workspace_bytes, int32_t* err, hipStream_t stream);
+
+gba_status gba_embedding_grad_dense(const int64_t* ids, int64_t n, const void* grad, gba_dtype grad_type,
+                                    int64_t grad_stride, int32_t D, int64_t R, float scale, int64_t padding_id,
+                                    void* table_grad, gba_dtype out_type, int64_t out_stride, int32_t accumulate,
+                                    void* workspace, size_t workspace_bytes, int32_t* err, hipStream_t stream);
+
+/*
+ * Layer norm over the D columns of each of n rows:
+ *   mean = sum x / D,  rstd = 1 / sqrt(sum (x - mean)^2 / D + eps),
+ *   y = (x - mean) * rstd * weight + bias.
+ *   x, y          [n][D] of `type`; y may be x itself (the same stride).
+ *   weight, bias  [D] of weight_type; either may be NULL (1 and 0).
+ *   mean, rstd    [n] float out; either may be NULL.
+ *
+ * gba_layer_norm_grad: with xh = (x - mean) * rstd and h = dy * weight,
+ *   dx = rstd * (h - (sum h) / D - xh * (sum h * xh) / D),
+ *   dweight = sum over rows of dy * xh,  dbias = sum over rows of dy,
+ * the sums over rows in 32 bits in a fixed order.
+ *   dy, x, dx       [n][D] of `type`; dx may be NULL, and may be dy itself.
+ *   mean, rstd      [n] float, as the forward call left them.
+ *   weight          [D] of weight_type, or NULL (1).
+ *   dweight, dbias  [D] of grad_type; either may be NULL.  With n == 0 they are 0.
+ *   workspace       gba_layer_norm_grad_workspace_size bytes, 16-byte aligned.
+ * Limits: 0 <= n < 2^31, 1 <= D <= 2^20, eps >= 0.
+ */
+gba_status gba_layer_norm(const void* x, int64_t x_stride, gba_dtype type, int64_t n, int32_t D, const void* weight,
+                          const void* bias, gba_dtype weight_type, double eps, void* y, int64_t y_stride,
+                          float* mean, float* rstd, hipStream_t stream);
+
+gba_status gba_layer_norm_grad_workspace_size(int64_t n, int32_t D, size_t* bytes /* host out */);
+
+gba_status gba_layer_norm_grad(const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, gba_dtype type,
+                               int64_t n, int32_t D, const float* mean, const float* rstd, const void* weight,
+                               gba_dtype weight_type, void* dx, int64_t dx_stride, void* dweight, void* dbias,
+                               gba_dtype grad_type, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * The global norm of many gradient tensors, and clipping by it:
+ *   norm = sqrt(sum over all tensors of g^2), in float64, rounded once;
+ *   coef = max_norm / norm where norm > max_norm, else 1;
+ *   out  = g * coef, each tensor to its own place (which may be the tensor
+ *          itself, or its part of the flat dense contribution of a push).
+ *
+ * The tensors are described once, in a list that the caller copies to the
+ * device and keeps for as long as the buffers stay where they are.
+ * gba_tensor (host):
+ *   grad, grad_type  n adjacent elements.
+ *   out, out_type    where they go; NULL: only their norm is wanted (clipping
+ *                    then skips the tensor).  Equal to grad with the same type
+ *                    (in place), else it overlaps no tensor of the list.
+ *   rows, width      device int64, may be NULL: only the first
+ *                    min(n, max(0, *rows) * width) elements count, read when
+ *                    the kernels run (num_unique of gba_embedding_grad_rows,
+ *                    with width = D); the others are neither read nor written.
+ * gba_tensor_list_size: bytes of the list, and its number of chunks, which
+ * the calls below take.
+ * gba_tensor_list_fill: writes the list to host memory.
+ *
+ * gba_grad_norm: norm alone (one float, device).
+ * gba_clip_grads: norm and coef (one float each, device; coef may be NULL),
+ *   and the clipped tensors.  max_norm > 0 (infinity: never clip).  Where the
+ *   norm is not finite, GBA_DERR_NONFINITE is set, coef is 0 and nothing is
+ *   written to any tensor: the caller skips the step.
+ * list       the device copy, 16-byte aligned.
+ * workspace  gba_grad_norm_workspace_size bytes, 16-byte aligned.
+ * Limits: 0 <= T <= 2^20 tensors, 0 <= n <= 2^40 elements each.
+ */
+typedef struct gba_tensor {
+  const void* grad;
+  void* out;
+  const int64_t* rows;
+  int64_t n;
+  int64_t width;
+  int32_t grad_type;   /* gba_dtype */
+  int32_t out_type;
+} gba_tensor;
+
+gba_status gba_tensor_list_size(const gba_tensor* tensors /* host */, int32_t T, size_t* bytes /* host out */,
+                                int64_t* chunks /* host out */);
+
+gba_status gba_tensor_list_fill(const gba_tensor* tensors /* host */, int32_t T, void* list /* host out */,
+                                size_t list_bytes);
+
+gba_status gba_grad_norm_workspace_size(int64_t chunks, size_t* bytes /* host out */);
+
+gba_status gba_grad_norm(const void* list, int64_t chunks, float* norm, void* workspace, size_t workspace_bytes,
+                         int32_t* err, hipStream_t stream);
+
+gba_status gba_clip_grads(const void* list, int64_t chunks, double max_norm, float* norm, float* coef,
+                          void* workspace, size_t workspace_bytes, int32_t* err, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -24,6 +24,10 @@ __all__ = [
     "gba_aggregate_sparse_plan_workspace_size", "gba_aggregate_sparse_plan", "gba_aggregate_sparse_noalloc",
     "NOALLOC_SCRATCH_BYTES", "ERR_SCRATCH_LIMIT", "gba_ceiling_read", "gba_ceiling_copy",
     "gba_ceiling_gather_rows", "gba_ceiling_sink_words",
+    "gba_embedding_lookup", "gba_embedding_grad_workspace_size", "gba_embedding_grad_rows",
+    "gba_embedding_grad_dense", "gba_layer_norm", "gba_layer_norm_grad_workspace_size", "gba_layer_norm_grad",
+    "TensorList", "gba_tensor_list", "gba_grad_norm_workspace_size", "gba_grad_norm", "gba_clip_grads",
+    "DERR_NONFINITE",
     "pointer_table", "DECAY_TOKEN", "DECAY_ID_TAG", "NORM_PER_ID_COUNT", "NORM_BY_K",
     "DERR_ID_RANGE", "DERR_FUTURE_TOKEN", "DERR_OFFSETS", "DERR_ROW_RANGE", "MAX_K", "MAX_D",
     "LIB_PATH",
@@ -37,6 +41,7 @@ LIB_PATH = os.environ.get("GBA_LIBRARY") or os.path.join(os.path.dirname(os.path
 DECAY_TOKEN, DECAY_ID_TAG = 0, 1
 NORM_PER_ID_COUNT, NORM_BY_K = 0, 1
 DERR_ID_RANGE, DERR_FUTURE_TOKEN, DERR_OFFSETS, DERR_ROW_RANGE, DERR_TABLE_FULL = 1, 2, 4, 8, 16
+DERR_NONFINITE = 32
 EMPTY_ID = -1
 SORT_AUTO, SORT_PLAIN, SORT_HOT = -1, 0, 1
 MAX_K, MAX_D = 4096, 256
@@ -47,6 +52,8 @@ _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
 _I64 = ctypes.c_int64
 _F64 = ctypes.c_double
+_F32 = ctypes.c_float
+_SIZE = ctypes.c_size_t
 
 _SIGNATURES = {
     "gba_status_string": ([_I32], ctypes.c_char_p),
@@ -94,6 +101,21 @@ _SIGNATURES = {
     "gba_apply_adagrad": ([_P, _P, _P, _P, _P, _P, _I64, _I32, _I64, _F64, _F64, _P, _P], _I32),
     "gba_apply_adam": ([_P, _P, _P, _P, _P, _P, _P, _I64, _I32, _I64, _F64, _F64, _F64, _F64, _I64,
                         _P, _P], _I32),
+    "gba_embedding_lookup": ([_P, _I64, _P, _I32, _I64, _I64, _I32, _F32, _P, _I32, _I64, _P, _P], _I32),
+    "gba_embedding_grad_workspace_size": ([_I64, _I32, _I64, ctypes.POINTER(_SIZE)], _I32),
+    "gba_embedding_grad_rows": ([_P, _I64, _P, _I32, _I64, _I32, _I64, _F32, _I64, _P, _P, _I64, _P, _P, _SIZE, _P, _P],
+                                _I32),
+    "gba_embedding_grad_dense": ([_P, _I64, _P, _I32, _I64, _I32, _I64, _F32, _I64, _P, _I32, _I64, _I32, _P, _SIZE,
+                                  _P, _P], _I32),
+    "gba_layer_norm": ([_P, _I64, _I32, _I64, _I32, _P, _P, _I32, _F64, _P, _I64, _P, _P, _P], _I32),
+    "gba_layer_norm_grad_workspace_size": ([_I64, _I32, ctypes.POINTER(_SIZE)], _I32),
+    "gba_layer_norm_grad": ([_P, _I64, _P, _I64, _I32, _I64, _I32, _P, _P, _P, _I32, _P, _I64, _P, _P, _I32, _P, _SIZE,
+                             _P], _I32),
+    "gba_tensor_list_size": ([_P, _I32, ctypes.POINTER(_SIZE), ctypes.POINTER(_I64)], _I32),
+    "gba_tensor_list_fill": ([_P, _I32, _P, _SIZE], _I32),
+    "gba_grad_norm_workspace_size": ([_I64, ctypes.POINTER(_SIZE)], _I32),
+    "gba_grad_norm": ([_P, _I64, _P, _P, _SIZE, _P, _P], _I32),
+    "gba_clip_grads": ([_P, _I64, _F64, _P, _P, _P, _SIZE, _P, _P], _I32),
 }
 
 _LIB = None
@@ -510,6 +532,217 @@ def gba_apply_adam(param, m, v, grad, lr, beta1, beta2, eps, t, rows=None, activ
     _check(lib().gba_apply_adam(_ptr(param), _ptr(m), _ptr(v), _ptr(grad), _ptr(rows), _ptr(active),
                                 _ptr(num_rows), n, D, int(R), float(lr), float(beta1), float(beta2),
                                 float(eps), int(t), _ptr(err), _stream(stream)))
+
+
+# ------------------------------------------------- the worker's operators
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # gba_dtype
+
+
+def _matrix(t, name, n=None, D=None):
+    """Checks a matrix on the GPU whose rows' elements are adjacent; returns its
+    type and row stride.  With ``n`` and ``D``: at least n rows of D columns."""
+    kind = _DTYPES.get(t.dtype)
+    if kind is None or not t.is_cuda or t.dim() != 2:
+        raise GBAError(f"{name}: expected a float32, bfloat16 or float16 matrix on the GPU")
+    rows, columns = t.shape
+    step, inner = t.stride()
+    if n is not None and (rows < n or columns != D):
+        raise GBAError(f"{name}: expected [{n}, {D}], got {list(t.shape)}")
+    if columns > 1 and inner != 1:
+        raise GBAError(f"{name}: the elements of a row must be adjacent")
+    if rows <= 1:
+        step = max(step, columns)
+    if step < columns:
+        raise GBAError(f"{name}: rows overlap")
+    return kind, step
+
+
+def _vector(t, name, D):
+    kind = _DTYPES.get(t.dtype)
+    if kind is None or not t.is_cuda or t.numel() != D or not t.is_contiguous():
+        raise GBAError(f"{name}: expected {D} adjacent float32, bfloat16 or float16 values on the GPU")
+    return kind
+
+
+def gba_embedding_lookup(ids, table, out, scale=1.0, err=None, stream=None):
+    """out[i] = scale * table[ids[i]], for float32, bfloat16 or float16 matrices
+    with any row stride; ``table`` and ``out`` may differ in type."""
+    n = ids.numel()
+    _need(ids, torch.int64, "ids")
+    _need(err, torch.int32, "err", 1)
+    kind, step = _matrix(table, "table")
+    R, D = table.shape
+    out_kind, out_step = _matrix(out, "out", n, D)
+    _check(lib().gba_embedding_lookup(_ptr(ids), n, _ptr(table), kind, step, R, D, scale, _ptr(out), out_kind, out_step,
+                                      _ptr(err), _stream(stream)))
+
+
+def gba_embedding_grad_workspace_size(n, D, R) -> int:
+    b = _SIZE(0)
+    _check(lib().gba_embedding_grad_workspace_size(int(n), int(D), int(R), ctypes.byref(b)))
+    return int(b.value)
+
+
+def gba_embedding_grad_rows(ids, grad, R, unique_ids, rows, num_unique, workspace, scale=1.0, padding_id=-1, err=None,
+                            stream=None):
+    """The lookup's gradient as one float32 row per distinct ID: for s < U =
+    num_unique, rows[s] = scale * sum of grad[i] over ids[i] == unique_ids[s].
+    Tokens equal to ``padding_id`` (-1: none) take no part."""
+    n = ids.numel()
+    _need(ids, torch.int64, "ids")
+    _need(unique_ids, torch.int64, "unique_ids", n)
+    _need(num_unique, torch.int64, "num_unique", 1)
+    _need(workspace, torch.uint8, "workspace")
+    _need(err, torch.int32, "err", 1)
+    kind, step = _matrix(grad, "grad")
+    D = grad.shape[1]
+    if grad.shape[0] < n:
+        raise GBAError(f"grad: expected {n} rows, got {grad.shape[0]}")
+    row_kind, row_step = _matrix(rows, "rows", n, D)
+    if row_kind != 0:
+        raise GBAError("rows: expected float32")
+    _check(lib().gba_embedding_grad_rows(_ptr(ids), n, _ptr(grad), kind, step, D, int(R), scale, int(padding_id),
+                                         _ptr(unique_ids), _ptr(rows), row_step, _ptr(num_unique), _ptr(workspace),
+                                         workspace.numel(), _ptr(err), _stream(stream)))
+
+
+def gba_embedding_grad_dense(ids, grad, table_grad, workspace, scale=1.0, padding_id=-1, accumulate=False, err=None,
+                             stream=None):
+    """The lookup's gradient as a whole table (zero rows where no token asked),
+    or, with ``accumulate``, added to ``table_grad``."""
+    n = ids.numel()
+    _need(ids, torch.int64, "ids")
+    _need(workspace, torch.uint8, "workspace")
+    _need(err, torch.int32, "err", 1)
+    out_kind, out_step = _matrix(table_grad, "table_grad")
+    R, D = table_grad.shape
+    kind, step = _matrix(grad, "grad", n, D)
+    _check(lib().gba_embedding_grad_dense(_ptr(ids), n, _ptr(grad), kind, step, D, R, scale, int(padding_id),
+                                          _ptr(table_grad), out_kind, out_step, int(bool(accumulate)), _ptr(workspace),
+                                          workspace.numel(), _ptr(err), _stream(stream)))
+
+
+def gba_layer_norm(x, weight, bias, y, eps=1e-5, mean=None, rstd=None, stream=None):
+    """y = (x - mean) * rstd * weight + bias over the columns of ``x``; ``weight``
+    and ``bias`` (one type) may be None, and so may the statistics (float32)."""
+    kind, step = _matrix(x, "x")
+    n, D = x.shape
+    y_kind, y_step = _matrix(y, "y", n, D)
+    if y_kind != kind:
+        raise GBAError("y: expected the type of x")
+    w_kind = _vector(weight, "weight", D) if weight is not None else None
+    if bias is not None:
+        b_kind = _vector(bias, "bias", D)
+        if w_kind is not None and b_kind != w_kind:
+            raise GBAError("bias: expected the type of weight")
+        w_kind = b_kind
+    _need(mean, torch.float32, "mean", n)
+    _need(rstd, torch.float32, "rstd", n)
+    _check(lib().gba_layer_norm(_ptr(x), step, kind, n, D, _ptr(weight), _ptr(bias), w_kind or 0, eps, _ptr(y), y_step,
+                                _ptr(mean), _ptr(rstd), _stream(stream)))
+
+
+def gba_layer_norm_grad_workspace_size(n, D) -> int:
+    b = _SIZE(0)
+    _check(lib().gba_layer_norm_grad_workspace_size(int(n), int(D), ctypes.byref(b)))
+    return int(b.value)
+
+
+def gba_layer_norm_grad(dy, x, mean, rstd, weight, dx, dweight, dbias, workspace, stream=None):
+    """Gradients of gba_layer_norm from ``dy``; ``weight``, ``dx``, ``dweight``
+    and ``dbias`` (one type) may be None."""
+    kind, step = _matrix(x, "x")
+    n, D = x.shape
+    dy_kind, dy_step = _matrix(dy, "dy", n, D)
+    dx_kind, dx_step = _matrix(dx, "dx", n, D) if dx is not None else (kind, D)
+    if dy_kind != kind or dx_kind != kind:
+        raise GBAError("dy, dx: expected the type of x")
+    _need(mean, torch.float32, "mean", n)
+    _need(rstd, torch.float32, "rstd", n)
+    _need(workspace, torch.uint8, "workspace")
+    w_kind = _vector(weight, "weight", D) if weight is not None else 0
+    g_kind = _vector(dweight, "dweight", D) if dweight is not None else None
+    if dbias is not None:
+        b_kind = _vector(dbias, "dbias", D)
+        if g_kind is not None and b_kind != g_kind:
+            raise GBAError("dbias: expected the type of dweight")
+        g_kind = b_kind
+    _check(lib().gba_layer_norm_grad(_ptr(dy), dy_step, _ptr(x), step, kind, n, D, _ptr(mean), _ptr(rstd), _ptr(weight),
+                                     w_kind, _ptr(dx), dx_step, _ptr(dweight), _ptr(dbias), g_kind or 0,
+                                     _ptr(workspace), workspace.numel(), _stream(stream)))
+
+
+class _Tensor(ctypes.Structure):   # gba_tensor
+    _fields_ = [("grad", _P), ("out", _P), ("rows", _P), ("n", _I64), ("width", _I64), ("grad_type", _I32),
+                ("out_type", _I32)]
+
+
+class TensorList:
+    """Gradient tensors described for gba_grad_norm and gba_clip_grads: the
+    device list, its number of chunks, and the tensors, which it keeps alive."""
+
+    def __init__(self, entries, chunks, tensors):
+        self.entries, self.chunks, self.tensors = entries, chunks, tensors
+
+
+def gba_tensor_list(grads, outs=None, rows=None) -> TensorList:
+    """Describes ``grads`` (contiguous float32, bfloat16 or float16 tensors, kept
+    where they are from step to step).  ``outs``: where each goes when clipped (its
+    own type; default: in place; None entries: nowhere).  ``rows``: for a matrix
+    whose first rows alone count, their number as one int64 on the GPU (None
+    entries: all count)."""
+    grads = list(grads)
+    outs = grads if outs is None else list(outs)
+    rows = [None] * len(grads) if rows is None else list(rows)
+    if not len(grads) == len(outs) == len(rows):
+        raise GBAError("grads, outs and rows differ in length")
+    host = (_Tensor * len(grads))()
+    for i, (g, o, r) in enumerate(zip(grads, outs, rows)):
+        for t, name in ((g, "grads"), (o, "outs")):
+            if t is not None and (t.dtype not in _DTYPES or not t.is_cuda or not t.is_contiguous()):
+                raise GBAError(f"{name}[{i}]: expected a contiguous float32, bfloat16 or float16 tensor on the GPU")
+        if o is not None and o.numel() < g.numel():
+            raise GBAError(f"outs[{i}]: expected at least {g.numel()} elements, got {o.numel()}")
+        _need(r, torch.int64, f"rows[{i}]", 1)
+        if r is not None and g.dim() < 2:
+            raise GBAError(f"rows[{i}]: expected a matrix to count rows of")
+        r = r if g.numel() else None
+        host[i] = _Tensor(g.data_ptr() if g.numel() else None, o.data_ptr() if o is not None and g.numel() else None,
+                          r.data_ptr() if r is not None else None, g.numel(),
+                          g.numel() // g.shape[0] if r is not None else 1, _DTYPES[g.dtype],
+                          _DTYPES[g.dtype if o is None or not g.numel() else o.dtype])
+    size, chunks = _SIZE(0), _I64(0)
+    _check(lib().gba_tensor_list_size(host, len(grads), ctypes.byref(size), ctypes.byref(chunks)))
+    image = torch.empty(size.value, dtype=torch.uint8)
+    _check(lib().gba_tensor_list_fill(host, len(grads), _ptr(image), size.value))
+    device = grads[0].device if grads else torch.device("cuda")
+    return TensorList(image.to(device), int(chunks.value), (grads, outs, rows))
+
+
+def gba_grad_norm_workspace_size(tensors: TensorList) -> int:
+    b = _SIZE(0)
+    _check(lib().gba_grad_norm_workspace_size(tensors.chunks, ctypes.byref(b)))
+    return int(b.value)
+
+
+def gba_grad_norm(tensors: TensorList, norm, workspace, err=None, stream=None):
+    """norm = sqrt of the sum of squares over all tensors of the list."""
+    _need(norm, torch.float32, "norm", 1)
+    _need(workspace, torch.uint8, "workspace")
+    _need(err, torch.int32, "err", 1)
+    _check(lib().gba_grad_norm(_ptr(tensors.entries), tensors.chunks, _ptr(norm), _ptr(workspace), workspace.numel(),
+                               _ptr(err), _stream(stream)))
+
+
+def gba_clip_grads(tensors: TensorList, max_norm, norm, workspace, coef=None, err=None, stream=None):
+    """The norm, and every tensor scaled by min(1, max_norm / norm) to its place.
+    A norm that is not finite sets DERR_NONFINITE and writes no tensor."""
+    _need(norm, torch.float32, "norm", 1)
+    _need(coef, torch.float32, "coef", 1)
+    _need(workspace, torch.uint8, "workspace")
+    _need(err, torch.int32, "err", 1)
+    _check(lib().gba_clip_grads(_ptr(tensors.entries), tensors.chunks, float(max_norm), _ptr(norm), _ptr(coef),
+                                _ptr(workspace), workspace.numel(), _ptr(err), _stream(stream)))
 
 
 # ------------------------------------------------- measurement kernels

@@ -497,4 +497,252 @@ gba_status gba_apply_adam(float* param, float* m, float* v, const float* grad, c
   return from_hip(launch_rows_adam(param, m, v, grad, rows, active, num_rows, n, D, R, hp, err, stream));
 }
 
+// ------------------------------------------------ the worker's operators
+static bool dtype_ok(int32_t t) { return t == GBA_F32 || t == GBA_BF16 || t == GBA_F16; }
+static bool columns_ok(int32_t D) { return D >= 1 && D <= (1 << 20); }
+static bool stride_ok(int64_t stride, int32_t D) { return stride >= D && stride <= (int64_t(1) << 40); }
+static bool element_aligned(const void* p, int32_t type) {
+  return (reinterpret_cast<uintptr_t>(p) & (type == GBA_F32 ? 3u : 1u)) == 0;
+}
+
+gba_status gba_embedding_lookup(const int64_t* ids, int64_t n, const void* table, gba_dtype table_type,
+                                int64_t table_stride, int64_t R, int32_t D, float scale, void* out,
+                                gba_dtype out_type, int64_t out_stride, int32_t* err, hipStream_t stream) {
+  if (n < 0 || n > INT32_MAX || R < 1 || R > (int64_t(1) << 32) || !columns_ok(D)) return GBA_ERR_INVALID_ARG;
+  if (!dtype_ok(table_type) || !dtype_ok(out_type) || !stride_ok(table_stride, D) || !stride_ok(out_stride, D))
+    return GBA_ERR_INVALID_ARG;
+  if (n == 0) return GBA_OK;
+  if (!ids || !table || !out) return GBA_ERR_NULL;
+  if (!element_aligned(table, table_type) || !element_aligned(out, out_type) ||
+      (reinterpret_cast<uintptr_t>(ids) & 7u) != 0)
+    return GBA_ERR_INVALID_ARG;
+  LookupArgs a;
+  a.ids = ids;
+  a.table = table;
+  a.out = out;
+  a.n = n;
+  a.R = R;
+  a.table_stride = table_stride;
+  a.out_stride = out_stride;
+  a.D = D;
+  a.table_type = (int32_t)table_type;
+  a.out_type = (int32_t)out_type;
+  a.scale = scale;
+  a.err = err;
+  return from_hip(launch_embedding_lookup(a, stream));
+}
+
+gba_status gba_embedding_grad_workspace_size(int64_t n, int32_t D, int64_t R, size_t* bytes) {
+  if (!bytes) return GBA_ERR_NULL;
+  if (n < 0 || n > kMaxN || R < 1 || R > (int64_t(1) << 32) || !columns_ok(D)) return GBA_ERR_INVALID_ARG;
+  *bytes = align_up(plan_sort(n, R).bytes) + align_up(embedding_grad_workspace_bytes(n, D));
+  return GBA_OK;
+}
+
+// The two forms of the gradient: a holds the outputs.
+static gba_status embedding_grad_call(const int64_t* ids, const void* grad, size_t workspace_bytes, void* workspace,
+                                      int32_t* err, EmbeddingGradArgs& a, hipStream_t stream) {
+  const SortPlan plan = plan_sort(a.n, a.R);
+  const size_t sort_bytes = align_up(plan.bytes);
+  if (workspace_bytes < sort_bytes + align_up(embedding_grad_workspace_bytes(a.n, a.D))) return GBA_ERR_WORKSPACE;
+  char* ws = static_cast<char*>(workspace);
+  a.keys = a.vals = nullptr;
+  a.grad = grad;
+  if (a.n > 0 && launch_sort_ids(ids, a.n, a.R, plan, ws, &a.keys, &a.vals, err, stream) != hipSuccess)
+    return GBA_ERR_HIP;
+  return from_hip(launch_embedding_grad(a, ws + sort_bytes, stream));
+}
+
+// Checks of the arguments that the two forms share.
+static gba_status embedding_grad_check(const int64_t* ids, int64_t n, const void* grad, gba_dtype grad_type,
+                                       int64_t grad_stride, int32_t D, int64_t R, const void* out, int32_t out_type,
+                                       int64_t out_stride, const void* workspace) {
+  if (n < 0 || n > kMaxN || R < 1 || R > (int64_t(1) << 32) || !columns_ok(D)) return GBA_ERR_INVALID_ARG;
+  if (!dtype_ok(grad_type) || !dtype_ok(out_type) || !stride_ok(grad_stride, D) || !stride_ok(out_stride, D))
+    return GBA_ERR_INVALID_ARG;
+  if (!workspace || (n > 0 && (!ids || !grad))) return GBA_ERR_NULL;
+  if ((ids && !aligned16(ids)) || !aligned16(workspace) || (grad && !element_aligned(grad, grad_type)) ||
+      (out && !element_aligned(out, out_type)))
+    return GBA_ERR_INVALID_ARG;
+  return GBA_OK;
+}
+
+gba_status gba_embedding_grad_rows(const int64_t* ids, int64_t n, const void* grad, gba_dtype grad_type,
+                                   int64_t grad_stride, int32_t D, int64_t R, float scale, int64_t padding_id,
+                                   int64_t* unique_ids, float* rows, int64_t row_stride, int64_t* num_unique,
+                                   void* workspace, size_t workspace_bytes, int32_t* err, hipStream_t stream) {
+  const gba_status st = embedding_grad_check(ids, n, grad, grad_type, grad_stride, D, R, rows, GBA_F32, row_stride,
+                                             workspace);
+  if (st != GBA_OK) return st;
+  if (!num_unique || (n > 0 && (!unique_ids || !rows))) return GBA_ERR_NULL;
+  EmbeddingGradArgs a{};
+  a.n = n;
+  a.R = R;
+  a.grad_stride = grad_stride;
+  a.padding = padding_id;
+  a.D = D;
+  a.grad_type = (int32_t)grad_type;
+  a.scale = scale;
+  a.unique_ids = unique_ids;
+  a.num_unique = num_unique;
+  a.out = rows;
+  a.out_stride = row_stride;
+  a.out_type = GBA_F32;
+  return embedding_grad_call(ids, grad, workspace_bytes, workspace, err, a, stream);
+}
+
+gba_status gba_embedding_grad_dense(const int64_t* ids, int64_t n, const void* grad, gba_dtype grad_type,
+                                    int64_t grad_stride, int32_t D, int64_t R, float scale, int64_t padding_id,
+                                    void* table_grad, gba_dtype out_type, int64_t out_stride, int32_t accumulate,
+                                    void* workspace, size_t workspace_bytes, int32_t* err, hipStream_t stream) {
+  const gba_status st = embedding_grad_check(ids, n, grad, grad_type, grad_stride, D, R, table_grad,
+                                             (int32_t)out_type, out_stride, workspace);
+  if (st != GBA_OK) return st;
+  if (!table_grad) return GBA_ERR_NULL;
+  EmbeddingGradArgs a{};
+  a.n = n;
+  a.R = R;
+  a.grad_stride = grad_stride;
+  a.padding = padding_id;
+  a.D = D;
+  a.grad_type = (int32_t)grad_type;
+  a.scale = scale;
+  a.accumulate = accumulate != 0;
+  a.out = table_grad;
+  a.out_stride = out_stride;
+  a.out_type = (int32_t)out_type;
+  return embedding_grad_call(ids, grad, workspace_bytes, workspace, err, a, stream);
+}
+
+gba_status gba_layer_norm(const void* x, int64_t x_stride, gba_dtype type, int64_t n, int32_t D, const void* weight,
+                          const void* bias, gba_dtype weight_type, double eps, void* y, int64_t y_stride,
+                          float* mean, float* rstd, hipStream_t stream) {
+  if (n < 0 || n > INT32_MAX || !columns_ok(D) || !(eps >= 0.0)) return GBA_ERR_INVALID_ARG;
+  if (!dtype_ok(type) || !dtype_ok(weight_type) || !stride_ok(x_stride, D) || !stride_ok(y_stride, D))
+    return GBA_ERR_INVALID_ARG;
+  if (n == 0) return GBA_OK;
+  if (!x || !y) return GBA_ERR_NULL;
+  if (!element_aligned(x, type) || !element_aligned(y, type) || !element_aligned(weight, weight_type) ||
+      !element_aligned(bias, weight_type) || (x == y && x_stride != y_stride))
+    return GBA_ERR_INVALID_ARG;
+  LayerNormArgs a;
+  a.x = x;
+  a.weight = weight;
+  a.bias = bias;
+  a.y = y;
+  a.mean = mean;
+  a.rstd = rstd;
+  a.n = n;
+  a.x_stride = x_stride;
+  a.y_stride = y_stride;
+  a.D = D;
+  a.type = (int32_t)type;
+  a.weight_type = (int32_t)weight_type;
+  a.eps = (float)eps;
+  return from_hip(launch_layer_norm(a, stream));
+}
+
+gba_status gba_layer_norm_grad_workspace_size(int64_t n, int32_t D, size_t* bytes) {
+  if (!bytes) return GBA_ERR_NULL;
+  if (n < 0 || n > INT32_MAX || !columns_ok(D)) return GBA_ERR_INVALID_ARG;
+  *bytes = align_up(layer_norm_grad_workspace_bytes(n, D));
+  return GBA_OK;
+}
+
+gba_status gba_layer_norm_grad(const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, gba_dtype type,
+                               int64_t n, int32_t D, const float* mean, const float* rstd, const void* weight,
+                               gba_dtype weight_type, void* dx, int64_t dx_stride, void* dweight, void* dbias,
+                               gba_dtype grad_type, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (n < 0 || n > INT32_MAX || !columns_ok(D)) return GBA_ERR_INVALID_ARG;
+  if (!dtype_ok(type) || !dtype_ok(weight_type) || !dtype_ok(grad_type) || !stride_ok(dy_stride, D) ||
+      !stride_ok(x_stride, D) || (dx && !stride_ok(dx_stride, D)))
+    return GBA_ERR_INVALID_ARG;
+  if (!workspace || (n > 0 && (!dy || !x || !mean || !rstd))) return GBA_ERR_NULL;
+  if (!aligned16(workspace) || !element_aligned(dy, type) || !element_aligned(x, type) ||
+      !element_aligned(dx, type) || !element_aligned(weight, weight_type) || !element_aligned(dweight, grad_type) ||
+      !element_aligned(dbias, grad_type) || (dx && dx == dy && dx_stride != dy_stride))
+    return GBA_ERR_INVALID_ARG;
+  if (workspace_bytes < align_up(layer_norm_grad_workspace_bytes(n, D))) return GBA_ERR_WORKSPACE;
+  LayerNormGradArgs a;
+  a.dy = dy;
+  a.x = x;
+  a.mean = mean;
+  a.rstd = rstd;
+  a.weight = weight;
+  a.dx = dx;
+  a.dweight = dweight;
+  a.dbias = dbias;
+  a.n = n;
+  a.dy_stride = dy_stride;
+  a.x_stride = x_stride;
+  a.dx_stride = dx_stride;
+  a.D = D;
+  a.type = (int32_t)type;
+  a.weight_type = (int32_t)weight_type;
+  a.grad_type = (int32_t)grad_type;
+  return from_hip(launch_layer_norm_grad(a, workspace, stream));
+}
+
+static gba_status tensors_check(const gba_tensor* t, int32_t T) {
+  if (T < 0 || T > (1 << 20)) return GBA_ERR_INVALID_ARG;
+  if (T > 0 && !t) return GBA_ERR_NULL;
+  for (int32_t i = 0; i < T; ++i) {
+    if (t[i].n < 0 || t[i].n > (int64_t(1) << 40) || !dtype_ok(t[i].grad_type) || !dtype_ok(t[i].out_type))
+      return GBA_ERR_INVALID_ARG;
+    if (t[i].n > 0 && !t[i].grad) return GBA_ERR_NULL;
+    if (!element_aligned(t[i].grad, t[i].grad_type) || !element_aligned(t[i].out, t[i].out_type) ||
+        (t[i].out == t[i].grad && t[i].out_type != t[i].grad_type))
+      return GBA_ERR_INVALID_ARG;
+    if (t[i].rows && (t[i].width < 1 || t[i].width > (int64_t(1) << 40))) return GBA_ERR_INVALID_ARG;
+  }
+  return GBA_OK;
+}
+
+gba_status gba_tensor_list_size(const gba_tensor* tensors, int32_t T, size_t* bytes, int64_t* chunks) {
+  if (!bytes || !chunks) return GBA_ERR_NULL;
+  const gba_status st = tensors_check(tensors, T);
+  if (st != GBA_OK) return st;
+  *chunks = tensor_chunks(tensors, T);
+  *bytes = tensor_list_bytes(*chunks);
+  return GBA_OK;
+}
+
+gba_status gba_tensor_list_fill(const gba_tensor* tensors, int32_t T, void* list, size_t list_bytes) {
+  const gba_status st = tensors_check(tensors, T);
+  if (st != GBA_OK) return st;
+  const size_t need = tensor_list_bytes(tensor_chunks(tensors, T));
+  if (list_bytes < need) return GBA_ERR_WORKSPACE;
+  if (need == 0) return GBA_OK;
+  if (!list) return GBA_ERR_NULL;
+  fill_tensor_list(tensors, T, list);
+  return GBA_OK;
+}
+
+static bool chunks_ok(int64_t chunks) { return chunks >= 0 && chunks <= (int64_t(1) << 48); }
+
+gba_status gba_grad_norm_workspace_size(int64_t chunks, size_t* bytes) {
+  if (!bytes) return GBA_ERR_NULL;
+  if (!chunks_ok(chunks)) return GBA_ERR_INVALID_ARG;
+  *bytes = align_up(grad_norm_workspace_bytes(chunks));
+  return GBA_OK;
+}
+
+gba_status gba_grad_norm(const void* list, int64_t chunks, float* norm, void* workspace, size_t workspace_bytes,
+                         int32_t* err, hipStream_t stream) {
+  if (!chunks_ok(chunks)) return GBA_ERR_INVALID_ARG;
+  if (!norm || !workspace || (chunks > 0 && !list)) return GBA_ERR_NULL;
+  if (!aligned16(workspace) || !aligned16(list)) return GBA_ERR_INVALID_ARG;
+  if (workspace_bytes < align_up(grad_norm_workspace_bytes(chunks))) return GBA_ERR_WORKSPACE;
+  return from_hip(launch_grad_norm(list, chunks, norm, workspace, err, stream));
+}
+
+gba_status gba_clip_grads(const void* list, int64_t chunks, double max_norm, float* norm, float* coef,
+                          void* workspace, size_t workspace_bytes, int32_t* err, hipStream_t stream) {
+  if (!chunks_ok(chunks) || !(max_norm > 0.0)) return GBA_ERR_INVALID_ARG;
+  if (!norm || !workspace || (chunks > 0 && !list)) return GBA_ERR_NULL;
+  if (!aligned16(workspace) || !aligned16(list)) return GBA_ERR_INVALID_ARG;
+  if (workspace_bytes < align_up(grad_norm_workspace_bytes(chunks))) return GBA_ERR_WORKSPACE;
+  return from_hip(launch_clip_grads(list, chunks, max_norm, norm, coef, workspace, err, stream));
+}
+
 }  // extern "C"

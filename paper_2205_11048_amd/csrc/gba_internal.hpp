@@ -190,4 +190,74 @@ hipError_t launch_hash_find_or_insert(int64_t* slot_ids, int32_t* slot_rows, int
 hipError_t launch_hash_rehash(const int64_t* old_ids, const int32_t* old_rows, int64_t old_capacity, int64_t* new_ids,
                               int32_t* new_rows, int64_t new_capacity, int32_t* err, hipStream_t stream);
 
+// ---- embedding lookup and its gradient
+struct LookupArgs {
+  const int64_t* ids;    // [n]
+  const void* table;     // [R][D]
+  void* out;             // [n][D]
+  int64_t n, R, table_stride, out_stride;
+  int32_t D, table_type, out_type;
+  float scale;
+  int32_t* err;
+};
+hipError_t launch_embedding_lookup(const LookupArgs& a, hipStream_t stream);
+
+struct EmbeddingGradArgs {
+  const uint32_t* keys;  // sorted IDs [n]
+  const uint32_t* vals;  // token of each sorted entry [n]
+  const void* grad;      // [n][D]
+  int64_t n, R, grad_stride, padding;   // padding < 0: none
+  int32_t D, grad_type;
+  float scale;
+  // one row per distinct ID (unique_ids non-null) ...
+  int64_t* unique_ids;
+  int64_t* num_unique;
+  // ... or the whole table
+  int32_t accumulate;
+  void* out;             // rows [U][D] (float) or the table [R][D]
+  int64_t out_stride;
+  int32_t out_type;
+};
+size_t embedding_grad_workspace_bytes(int64_t n, int32_t D);
+hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, void* ws, hipStream_t stream);
+
+// ---- layer norm and its gradient
+struct LayerNormArgs {
+  const void* x;
+  const void* weight;    // null: 1
+  const void* bias;      // null: 0
+  void* y;
+  float* mean;           // may be null
+  float* rstd;           // may be null
+  int64_t n, x_stride, y_stride;
+  int32_t D, type, weight_type;
+  float eps;
+};
+hipError_t launch_layer_norm(const LayerNormArgs& a, hipStream_t stream);
+
+struct LayerNormGradArgs {
+  const void* dy;
+  const void* x;
+  const float* mean;
+  const float* rstd;
+  const void* weight;    // null: 1
+  void* dx;              // may be null
+  void* dweight;         // may be null
+  void* dbias;           // may be null
+  int64_t n, dy_stride, x_stride, dx_stride;
+  int32_t D, type, weight_type, grad_type;
+};
+// (the most of any n up to this one)
+size_t layer_norm_grad_workspace_bytes(int64_t n, int32_t D);
+hipError_t launch_layer_norm_grad(const LayerNormGradArgs& a, void* ws, hipStream_t stream);
+
+// ---- norm of many tensors, clipping
+int64_t tensor_chunks(const gba_tensor* t, int32_t T);
+size_t tensor_list_bytes(int64_t chunks);
+void fill_tensor_list(const gba_tensor* t, int32_t T, void* list);
+size_t grad_norm_workspace_bytes(int64_t chunks);
+hipError_t launch_grad_norm(const void* list, int64_t chunks, float* norm, void* ws, int32_t* err, hipStream_t stream);
+hipError_t launch_clip_grads(const void* list, int64_t chunks, double max_norm, float* norm, float* coef, void* ws,
+                             int32_t* err, hipStream_t stream);
+
 }  // namespace gba

@@ -1,0 +1,241 @@
+"""Layer norm and its gradient against float64.
+
+Tolerances.  u = 2^-24 is float32's unit roundoff, u_t that of the output's
+type.  No element of a row passes through more than h = D / 64 + 40 additions
+(the row is spread over the lanes and joined pairwise), so a row sum is off by
+at most h u times the sum of magnitudes; the other errors are single roundings
+(products, differences, the reciprocal square root within 4 u), propagated to
+first order and widened by a percent.  A sum over n rows is bounded for any
+order, (n + 4) u times the sum of magnitudes."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2205_11048_amd as gba
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+U32 = 2.0 ** -24
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+ROUND = {F32: 2.0 ** -24, BF16: 2.0 ** -8, F16: 2.0 ** -11}
+TINY = {F32: 2.0 ** -148, BF16: 2.0 ** -134, F16: 2.0 ** -25}
+EPS = 1e-5
+
+
+def _matrix(x64, dtype, pad):
+    n, D = x64.shape
+    x = torch.from_numpy(x64).to(dtype)
+    wide = torch.full((n, D + pad), float("nan"), dtype=dtype)
+    wide[:, :D] = x
+    return wide.to(DEV)[:, :D], x.double().numpy()
+
+
+def _close(got, ref, bound, name):
+    got = got.double().cpu().numpy()
+    bad = ~(np.abs(got - ref) <= bound)
+    assert not bad.any(), (name, int(bad.sum()), got[bad][:3], ref[bad][:3], np.broadcast_to(bound, ref.shape)[bad][:3])
+
+
+def _params(rng, D, wtype, which):
+    w = torch.from_numpy(1.0 + 0.3 * rng.normal(size=D)).to(wtype) if "w" in which else None
+    b = torch.from_numpy(0.3 * rng.normal(size=D)).to(wtype) if "b" in which else None
+    w64 = w.double().numpy() if w is not None else np.ones(D)
+    b64 = b.double().numpy() if b is not None else np.zeros(D)
+    return (w.to(DEV) if w is not None else None), (b.to(DEV) if b is not None else None), w64, b64
+
+
+def _ws(n, D):
+    return torch.full((gba.gba_layer_norm_grad_workspace_size(n, D),), 255, dtype=torch.uint8, device=DEV)
+
+
+SHAPES = [
+    # n, D, type, weight type, parameters, pad, shift of the values
+    (1, 1, F32, F32, "wb", 0, 0.0),
+    (3, 2, BF16, F32, "wb", 0, 0.0),
+    (1, 8, BF16, BF16, "w", 0, 1.0),
+    (7, 16, F32, F32, "wb", 0, 0.0),
+    (129, 31, F16, F16, "wb", 1, 0.5),
+    (1000, 32, BF16, F32, "b", 0, 0.0),
+    (2049, 64, F32, F32, "wb", 0, 3.0),
+    (513, 100, F32, BF16, "wb", 5, 0.0),
+    (300, 128, BF16, BF16, "wb", 0, 0.0),
+    (65, 255, F16, F32, "", 0, 0.0),
+    (64, 257, BF16, F32, "wb", 3, 0.0),
+    (33, 520, F32, F32, "wb", 0, 100.0),
+    (8, 1024, BF16, BF16, "wb", 0, 0.0),
+    (200, 1001, F32, F32, "wb", 5, 0.0),
+    (1, 2048, F16, F16, "wb", 0, 0.0),
+    (301, 2048, BF16, F32, "w", 0, 0.0),
+    (130, 4096, BF16, BF16, "wb", 0, 0.25),
+    (77, 4100, F32, F32, "wb", 0, 0.0),
+    (40, 8192, BF16, F32, "wb", 8, 0.0),
+    (9, 10_007, F16, F32, "wb", 0, 0.0),
+    (5, 16_384, F32, F32, "wb", 0, 0.0),
+    (6, 40_000, BF16, BF16, "wb", 0, 0.0),
+    (2, 70_001, F32, F32, "wb", 1, 0.0),
+]
+
+
+def _statistics(x64):
+    mean = x64.mean(1)
+    var = ((x64 - mean[:, None]) ** 2).mean(1)
+    return mean, var, 1.0 / np.sqrt(var + EPS)
+
+
+@pytest.mark.parametrize("n,D,dtype,wtype,which,pad,shift", SHAPES)
+def test_forward(n, D, dtype, wtype, which, pad, shift):
+    rng = np.random.default_rng(n * 13 + D)
+    x, x64 = _matrix(shift + rng.normal(size=(n, D)) * np.exp(rng.normal(size=(n, 1))), dtype, pad)
+    w, b, w64, b64 = _params(rng, D, wtype, which)
+    wide = torch.full((n, D + pad), float("nan"), dtype=dtype, device=DEV)
+    y = wide[:, :D]
+    mean = torch.full((n,), float("nan"), device=DEV)
+    rstd = torch.full((n,), float("nan"), device=DEV)
+    gba.gba_layer_norm(x, w, b, y, eps=EPS, mean=mean, rstd=rstd)
+
+    m, v, r = _statistics(x64)
+    h = D / 64 + 40
+    dm = 1.01 * (h + 2) * U32 * np.abs(x64).mean(1)
+    _close(mean, m, dm + 1e-38, "mean")
+    dr = 1.01 * (0.5 * ((h + 6) * U32 + dm ** 2 / (v + EPS)) + 5 * U32)   # relative
+    _close(rstd, r, dr * r, "rstd")
+    d = np.abs(x64 - m[:, None])
+    aw = np.abs(w64)[None, :]
+    ref = (x64 - m[:, None]) * r[:, None] * w64 + b64
+    bound = aw * r[:, None] * (dm[:, None] + d * (dr[:, None] + 4 * U32)) + 2 * U32 * np.abs(ref)
+    _close(y, ref, 1.01 * bound + 1.01 * ROUND[dtype] * (np.abs(ref) + bound) + TINY[dtype], "y")
+    if pad:
+        assert torch.isnan(wide[:, D:]).all()
+    # without the statistics, and in place: the same bits
+    z = x.clone(memory_format=torch.preserve_format) if not pad else wide.clone().fill_(0)[:, :D].copy_(x)
+    gba.gba_layer_norm(z, w, b, z, eps=EPS)
+    assert torch.equal(z, y)
+
+
+@pytest.mark.parametrize("n,D,dtype,wtype,which,pad,shift", SHAPES)
+def test_backward(n, D, dtype, wtype, which, pad, shift):
+    rng = np.random.default_rng(n * 17 + D)
+    x, x64 = _matrix(shift + rng.normal(size=(n, D)), dtype, pad)
+    dy, g64 = _matrix(rng.normal(size=(n, D)) * 0.1, dtype, 2 * pad)
+    w, _, w64, _ = _params(rng, D, wtype, which)
+    m, _, r = _statistics(x64)
+    mean, rstd = torch.from_numpy(m.astype(np.float32)).to(DEV), torch.from_numpy(r.astype(np.float32)).to(DEV)
+    m, r = mean.double().cpu().numpy()[:, None], rstd.double().cpu().numpy()[:, None]
+    wide = torch.full((n, D + pad), float("nan"), dtype=dtype, device=DEV)
+    dx = wide[:, :D]
+    dw, db = torch.full((D,), float("nan"), device=DEV), torch.full((D,), float("nan"), device=DEV)
+    ws = _ws(n, D)
+    gba.gba_layer_norm_grad(dy, x, mean, rstd, w, dx, dw, db, ws)
+
+    h = D / 64 + 40
+    xh = (x64 - m) * r
+    hh = g64 * w64
+    s1, s2 = hh.mean(1, keepdims=True), (hh * xh).mean(1, keepdims=True)
+    d1 = (h + 4) * U32 * np.abs(hh).mean(1, keepdims=True)
+    d2 = (h + 8) * U32 * np.abs(hh * xh).mean(1, keepdims=True)
+    ref = r * (hh - s1 - xh * s2)
+    bound = r * (6 * U32 * (np.abs(hh) + np.abs(s1) + 2 * np.abs(xh * s2)) + d1 + np.abs(xh) * d2)
+    _close(dx, ref, 1.01 * bound + 1.01 * ROUND[dtype] * (np.abs(ref) + bound) + TINY[dtype], "dx")
+    _close(dw, (g64 * xh).sum(0), 1.01 * (n + 4) * U32 * np.abs(g64 * xh).sum(0) + 1e-38, "dweight")
+    _close(db, g64.sum(0), 1.01 * (n + 4) * U32 * np.abs(g64).sum(0) + 1e-38, "dbias")
+    if pad:
+        assert torch.isnan(wide[:, D:]).all()
+
+    # again, and each output alone: the same bits; the parameters' gradients in their own type
+    again, dw2, db2 = torch.empty_like(dx), torch.empty_like(dw), torch.empty_like(db)
+    gba.gba_layer_norm_grad(dy, x, mean, rstd, w, again, dw2, None, ws)
+    assert torch.equal(again, dx) and torch.equal(dw2, dw)
+    gba.gba_layer_norm_grad(dy, x, mean, rstd, w, None, None, db2, ws)
+    assert torch.equal(db2, db)
+    low, low_b = torch.empty(D, dtype=BF16, device=DEV), torch.empty(D, dtype=BF16, device=DEV)
+    gba.gba_layer_norm_grad(dy, x, mean, rstd, w, None, low, low_b, ws)
+    assert torch.equal(low, dw.to(BF16)) and torch.equal(low_b, db.to(BF16))
+    # in the place of dy
+    gba.gba_layer_norm_grad(dy, x, mean, rstd, w, dy, dw2, db2, ws)
+    assert torch.equal(dy, dx) and torch.equal(dw2, dw) and torch.equal(db2, db)
+
+
+def test_backward_over_many_rows():
+    """Rows beyond one pass of the resident blocks."""
+    n, D = 30_011, 40
+    rng = np.random.default_rng(2)
+    x, x64 = _matrix(rng.normal(size=(n, D)), F32, 0)
+    dy, g64 = _matrix(rng.normal(size=(n, D)), F32, 0)
+    m, _, r = _statistics(x64)
+    mean, rstd = torch.from_numpy(m.astype(np.float32)).to(DEV), torch.from_numpy(r.astype(np.float32)).to(DEV)
+    dx, dw, db = torch.empty_like(x), torch.empty(D, device=DEV), torch.empty(D, device=DEV)
+    gba.gba_layer_norm_grad(dy, x, mean, rstd, None, dx, dw, db, _ws(n, D))
+    xh = (x64 - mean.double().cpu().numpy()[:, None]) * rstd.double().cpu().numpy()[:, None]
+    _close(dw, (g64 * xh).sum(0), 1.01 * (n + 4) * U32 * np.abs(g64 * xh).sum(0), "dweight")
+    _close(db, g64.sum(0), 1.01 * (n + 4) * U32 * np.abs(g64).sum(0), "dbias")
+
+
+def test_the_gradient_is_the_forwards():
+    """Central differences, in float64, of L = sum(c * layer_norm(x)): off by the third derivative times the step's
+    square, below 1e-6 of the row's scale at a step of 1e-4."""
+    rng = np.random.default_rng(9)
+    n, D = 4, 48
+    x64 = rng.normal(size=(n, D)).astype(np.float32).astype(np.float64)
+    c = rng.normal(size=(n, D)).astype(np.float32).astype(np.float64)
+    w64 = (1 + 0.3 * rng.normal(size=D)).astype(np.float32).astype(np.float64)
+
+    def loss(x, w, b):
+        m, _, r = _statistics(x)
+        return (c * ((x - m[:, None]) * r[:, None] * w + b)).sum()
+
+    x, dy, w = (torch.from_numpy(t.astype(np.float32)).to(DEV) for t in (x64, c, w64))
+    y, mean, rstd = torch.empty_like(x), torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    gba.gba_layer_norm(x, w, None, y, eps=EPS, mean=mean, rstd=rstd)
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty_like(w)
+    gba.gba_layer_norm_grad(dy, x, mean, rstd, w, dx, dw, db, _ws(n, D))
+    e, zero = 1e-4, np.zeros(D)
+    for i, k in [(0, 0), (1, 47), (2, 20), (3, 31)]:
+        step = np.zeros((n, D))
+        step[i, k] = e
+        assert abs((loss(x64 + step, w64, zero) - loss(x64 - step, w64, zero)) / (2 * e) - float(dx[i, k])) < 2e-5
+        step = np.zeros(D)
+        step[k] = e
+        assert abs((loss(x64, w64 + step, zero) - loss(x64, w64 - step, zero)) / (2 * e) - float(dw[k])) < 2e-5
+        assert abs((loss(x64, w64, step) - loss(x64, w64, -step)) / (2 * e) - float(db[k])) < 2e-5
+
+
+def test_no_rows():
+    D = 24
+    x = torch.empty((0, D), device=DEV)
+    none = torch.empty(0, device=DEV)
+    gba.gba_layer_norm(x, None, None, x, mean=none, rstd=none)
+    dw, db = torch.full((D,), 5.0, device=DEV), torch.full((D,), 5.0, device=DEV)
+    gba.gba_layer_norm_grad(x, x, none, none, None, x, dw, db, _ws(0, D))
+    assert (dw == 0).all() and (db == 0).all()
+
+
+def test_rows_that_are_constant_infinite_or_not_numbers():
+    x = torch.ones((4, 96), device=DEV)
+    x[1], x[2, 5], x[3, 6] = 7.0, float("inf"), float("nan")
+    y, mean, rstd = torch.empty_like(x), torch.empty(4, device=DEV), torch.empty(4, device=DEV)
+    b = torch.full((96,), 2.0, device=DEV)
+    gba.gba_layer_norm(x, None, b, y, eps=EPS, mean=mean, rstd=rstd)
+    assert (y[:2] == 2.0).all() and mean[:2].tolist() == [1.0, 7.0]
+    assert abs(float(rstd[0]) * EPS ** 0.5 - 1) < 1e-6
+    assert torch.isnan(y[2]).any() and torch.isnan(y[3]).all()
+
+
+def test_refusals():
+    x, w = torch.zeros((5, 16), device=DEV), torch.ones(16, device=DEV)
+    s = torch.zeros(5, device=DEV)
+    ws = _ws(5, 16)
+    wide = torch.zeros((5, 20), device=DEV)
+    for bad in [lambda: gba.gba_layer_norm(x, w, w, x.half()), lambda: gba.gba_layer_norm(x, w[:15], w, x),
+                lambda: gba.gba_layer_norm(x, w, w.half(), x), lambda: gba.gba_layer_norm(x, w, w, x[:4]),
+                lambda: gba.gba_layer_norm(x, w, w, x, eps=-1.0), lambda: gba.gba_layer_norm(x, w, w, x, eps=float("nan")),
+                lambda: gba.gba_layer_norm(x, w, w, x, mean=s[:4]), lambda: gba.gba_layer_norm(x.T, w, w, x),
+                lambda: gba.gba_layer_norm(x[:, :0], w[:0], None, x[:, :0]), lambda: gba.gba_layer_norm(x.cpu(), w, w, x),
+                lambda: gba.gba_layer_norm_grad(x, x, s, s, w, x, w, w, ws[:-1]),
+                lambda: gba.gba_layer_norm_grad(x, x, s, s[:4], w, x, w, w, ws),
+                lambda: gba.gba_layer_norm_grad(x, x.half(), s, s, w, x, w, w, ws),
+                lambda: gba.gba_layer_norm_grad(x, x, s, s, w, x, w, w.half(), ws),
+                lambda: gba.gba_layer_norm_grad(wide[:, :16], x, s, s, w, wide.view(-1)[:80].view(5, 16), w, w, ws),
+                lambda: gba.gba_layer_norm_grad_workspace_size(-1, 16),
+                lambda: gba.gba_layer_norm_grad_workspace_size(5, (1 << 20) + 1)]:
+        with pytest.raises(gba.GBAError):
+            bad()
