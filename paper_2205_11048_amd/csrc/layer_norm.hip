@@ -1,4 +1,13 @@
 // Layer norm over the rows of a matrix and its gradient.
+//
+// A row stays in registers from its only read to its only write: 4 to 16
+// elements per thread, the row spread over 1 to 64 lanes of a wave or 2 to 16
+// waves, so that the mean, then the mean of the squared differences (forward)
+// or the two sums (backward) are taken from registers.  Blocks stay on the
+// chip and take rows in turn, so the weight and the bias are read once per
+// block, and the weight's gradient is added up in registers over all the
+// block's rows: one partial row per block goes to memory and a second launch
+// adds the blocks' rows up in order.  Bound by the bytes of the rows.
 #include <algorithm>
 
 #include "elements.hpp"
@@ -7,14 +16,308 @@
 
 namespace gba {
 
-constexpr int kNormRowBlock = 256;
+constexpr int kNormRowBlock = 256;           // rows read from memory again
 constexpr int kNormRowWaves = kNormRowBlock / kWave;
-constexpr int64_t kGradRowsPerBlock = 256;   // rows of a partial sum of the weight's gradient
+constexpr int64_t kGradRowsPerBlock = 256;   // ... of a partial sum of the weight's gradient
 constexpr int64_t kMaxRowGrid = 1 << 20;
+
+constexpr int kPerThread = 16;               // most elements of a row a thread holds
+constexpr int kRegBlock = 512;
+constexpr int kRegColumns = 1024 * kPerThread;   // widest row held in registers
+constexpr int64_t kRegGradBlocks = 512;      // most blocks of a gradient: two per compute unit
+constexpr int64_t kRegBlocks = 1024;         // ... of a forward call
 
 static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 static inline size_t align_up(size_t x) { return (x + 255) & ~size_t(255); }
 
+// ------------------------------------------------------ rows in registers
+// Adds x over each aligned group of W lanes (W a power of two); every lane
+// gets the sum.  Up to 16 lanes the exchange is a DPP operand of the addition.
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float x) {
+  const int y = __builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true);
+  return x + __int_as_float(y);
+}
+template <int W>
+__device__ __forceinline__ float lanes_sum(float x) {
+  if constexpr (W >= 2) x = dpp_add<0xB1>(x);    // lane ^ 1
+  if constexpr (W >= 4) x = dpp_add<0x4E>(x);    // lane ^ 2
+  if constexpr (W >= 8) x = dpp_add<0x141>(x);   // the other four of eight (all four hold one value)
+  if constexpr (W >= 16) x = dpp_add<0x140>(x);  // the other eight of sixteen
+  if constexpr (W >= 32) x += __shfl_xor(x, 16, kWave);
+  if constexpr (W >= 64) x += __shfl_xor(x, 32, kWave);
+  return x;
+}
+
+// How a row lies over the threads: LPR threads with NV vectors of V elements
+// each, vector k of thread t at column (k * LPR + t) * V.  The last vector may
+// pass the row's end: it is moved back to end there, its first `shift`
+// elements belong to other threads and count for nothing (all V of them in a
+// thread past the end); what is stored of them is what their owner stores.
+// RU rows per thread group at a time.
+template <typename T, int LPR, int NV>
+struct RowShape {
+  static constexpr int V = kVec<T>;
+  static constexpr int E = V * NV;
+  static constexpr int RU = kPerThread / E;
+  static constexpr int BLOCK = LPR > kRegBlock ? LPR : kRegBlock;
+  static constexpr int G = BLOCK / LPR;         // thread groups of a block
+  static constexpr int ROWS = G * RU;           // rows of a block at a time
+  static constexpr int WAVES = BLOCK / kWave;
+};
+
+template <typename T, int LPR, int NV>
+struct RowPlace {
+  static constexpr int V = kVec<T>;
+  int col[NV];     // first column of each vector
+  int shift;       // foreign elements of the last one
+  bool last;       // the last one holds elements of this thread
+  bool tiny;       // rows narrower than a vector (LPR = NV = 1): element by element
+  int D;
+  __device__ __forceinline__ RowPlace(int gl, int width) : D(width) {
+    tiny = width < V;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) col[k] = (k * LPR + gl) * V;
+    const int c = col[NV - 1];
+    last = c < width;
+    const int moved = tiny ? 0 : (c + V > width ? width - V : c);
+    shift = c - moved < V ? c - moved : V;
+    col[NV - 1] = moved;
+  }
+  __device__ __forceinline__ bool own(int k, int e) const {
+    return k + 1 < NV || (tiny ? e < D : e >= shift);
+  }
+  template <typename P>
+  __device__ __forceinline__ void load(const P* __restrict__ p, int k, float (&o)[V]) const {
+    if (tiny) load_part<P, V>(p, D, o);
+    else load_vec<P, V>(p + col[k], o);
+  }
+  __device__ __forceinline__ void load(const void* __restrict__ p, int type, int k, float (&o)[V]) const {
+    if (type == GBA_F32) load(static_cast<const float*>(p), k, o);
+    else if (type == GBA_BF16) load(static_cast<const bf16_t*>(p), k, o);
+    else load(static_cast<const f16_t*>(p), k, o);
+  }
+  __device__ __forceinline__ void store(T* __restrict__ p, int k, const float (&o)[V]) const {
+    if (tiny) store_part<T, V>(p, D, o);
+    else if (k + 1 < NV || last) store_vec<T, V>(p + col[k], o);
+  }
+};
+
+// Adds each of x[0..N) over the LPR threads of a row.  Rows of several waves
+// go through LDS, two buffers in turn so that one barrier a sum is enough.
+template <int LPR, int WAVES, int N>
+__device__ __forceinline__ void row_sum(float (&x)[N], float (*s)[N][WAVES], int& buffer) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = lanes_sum<(LPR < kWave ? LPR : kWave)>(x[i]);
+  if constexpr (LPR > kWave) {
+    constexpr int PER = LPR / kWave;
+    const int w = threadIdx.x / kWave, w0 = w / PER * PER;
+    if (lane_id() == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[buffer][i][w] = x[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float t = 0.0f;
+#pragma unroll
+      for (int k = 0; k < PER; ++k) t += s[buffer][i][w0 + k];
+      x[i] = t;
+    }
+    buffer ^= 1;
+  }
+}
+
+template <typename T, int LPR, int NV>
+__global__ void __launch_bounds__((RowShape<T, LPR, NV>::BLOCK))
+layer_norm_kernel(LayerNormArgs a) {
+  typedef RowShape<T, LPR, NV> S;
+  constexpr int V = S::V, RU = S::RU;
+  __shared__ float s_sum[2][RU][S::WAVES];
+  const int gl = threadIdx.x % LPR, grp = threadIdx.x / LPR;
+  const RowPlace<T, LPR, NV> at(gl, a.D);
+  float w[NV][V], b[NV][V];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      w[k][e] = 1.0f;
+      b[k][e] = 0.0f;
+    }
+    if (a.weight) at.load(a.weight, a.weight_type, k, w[k]);
+    if (a.bias) at.load(a.bias, a.weight_type, k, b[k]);
+  }
+  const float D = (float)a.D;
+  int buffer = 0;
+  for (int64_t r0 = (int64_t)blockIdx.x * S::ROWS; r0 < a.n; r0 += (int64_t)gridDim.x * S::ROWS) {
+    float x[RU][NV][V], sum[RU];
+#pragma unroll
+    for (int u = 0; u < RU; ++u) {
+      const int64_t r = r0 + u * S::G + grp;
+      const T* p = static_cast<const T*>(a.x) + (r < a.n ? r : a.n - 1) * a.x_stride;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) at.load(p, k, x[u][k]);
+    }
+#pragma unroll
+    for (int u = 0; u < RU; ++u) {
+      sum[u] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum[u] += at.own(k, e) ? x[u][k][e] : 0.0f;
+    }
+    row_sum<LPR, S::WAVES>(sum, s_sum, buffer);
+    float mean[RU];
+#pragma unroll
+    for (int u = 0; u < RU; ++u) {
+      mean[u] = sum[u] / D;
+      sum[u] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float d = at.own(k, e) ? x[u][k][e] - mean[u] : 0.0f;
+          sum[u] = __builtin_fmaf(d, d, sum[u]);
+        }
+    }
+    row_sum<LPR, S::WAVES>(sum, s_sum, buffer);
+#pragma unroll
+    for (int u = 0; u < RU; ++u) {
+      const int64_t r = r0 + u * S::G + grp;
+      if (r >= a.n) continue;
+      const float rstd = 1.0f / sqrtf(sum[u] / D + a.eps);
+      if (gl == 0) {
+        if (a.mean) a.mean[r] = mean[u];
+        if (a.rstd) a.rstd[r] = rstd;
+      }
+      T* q = static_cast<T*>(a.y) + r * a.y_stride;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        float y[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) y[e] = __builtin_fmaf((x[u][k][e] - mean[u]) * rstd, w[k][e], b[k][e]);
+        at.store(q, k, y);
+      }
+    }
+  }
+}
+
+template <typename T, int LPR, int NV>
+__global__ void __launch_bounds__((RowShape<T, LPR, NV>::BLOCK))
+layer_norm_grad_kernel(LayerNormGradArgs a, float* __restrict__ partial) {
+  typedef RowShape<T, LPR, NV> S;
+  constexpr int V = S::V, RU = S::RU;
+  // the block's sums of the weight's gradient: one row per wave or per group of several waves
+  constexpr int TEAM = LPR < kWave ? kWave : LPR;
+  constexpr int TEAMS = S::BLOCK / TEAM;
+  constexpr int COLS = LPR * S::E;
+  __shared__ float s_sum[2][2 * RU][S::WAVES];
+  __shared__ float s_part[TEAMS > 1 ? TEAMS * COLS : 1];
+  const int gl = threadIdx.x % LPR, grp = threadIdx.x / LPR;
+  const RowPlace<T, LPR, NV> at(gl, a.D);
+  float w[NV][V], dw[NV][V], db[NV][V];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      w[k][e] = 1.0f;
+      dw[k][e] = db[k][e] = 0.0f;
+    }
+    if (a.weight) at.load(a.weight, a.weight_type, k, w[k]);
+  }
+  const float D = (float)a.D;
+  int buffer = 0;
+  for (int64_t r0 = (int64_t)blockIdx.x * S::ROWS; r0 < a.n; r0 += (int64_t)gridDim.x * S::ROWS) {
+    float x[RU][NV][V], g[RU][NV][V], rstd[RU], mean[RU], sum[2 * RU];
+#pragma unroll
+    for (int u = 0; u < RU; ++u) {
+      const int64_t r = r0 + u * S::G + grp, rc = r < a.n ? r : a.n - 1;
+      mean[u] = a.mean[rc];
+      rstd[u] = a.rstd[rc];
+      const T* p = static_cast<const T*>(a.x) + rc * a.x_stride;
+      const T* q = static_cast<const T*>(a.dy) + rc * a.dy_stride;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        at.load(p, k, x[u][k]);
+        at.load(q, k, g[u][k]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < RU; ++u) {
+      const bool in = r0 + u * S::G + grp < a.n;
+      sum[2 * u] = sum[2 * u + 1] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float xh = (x[u][k][e] - mean[u]) * rstd[u];
+          const float gy = g[u][k][e];
+          x[u][k][e] = xh;
+          const float h = gy * w[k][e];
+          const bool own = at.own(k, e);
+          sum[2 * u] += own ? h : 0.0f;
+          sum[2 * u + 1] = own ? __builtin_fmaf(h, xh, sum[2 * u + 1]) : sum[2 * u + 1];
+          dw[k][e] = in ? __builtin_fmaf(gy, xh, dw[k][e]) : dw[k][e];
+          db[k][e] += in ? gy : 0.0f;
+          g[u][k][e] = h;
+        }
+    }
+    if (!a.dx) continue;
+    row_sum<LPR, S::WAVES>(sum, s_sum, buffer);
+#pragma unroll
+    for (int u = 0; u < RU; ++u) {
+      const int64_t r = r0 + u * S::G + grp;
+      if (r >= a.n) continue;
+      const float s1 = sum[2 * u] / D, s2 = sum[2 * u + 1] / D;
+      T* q = static_cast<T*>(a.dx) + r * a.dx_stride;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        float d[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) d[e] = rstd[u] * (g[u][k][e] - s1 - x[u][k][e] * s2);
+        at.store(q, k, d);
+      }
+    }
+  }
+  if (!a.dweight && !a.dbias) return;
+  float* out = partial + (int64_t)blockIdx.x * 2 * a.D;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    float(&acc)[NV][V] = which ? db : dw;
+    if constexpr (LPR < kWave) {
+#pragma unroll
+      for (int off = LPR; off < kWave; off <<= 1)
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[0][e] += __shfl_xor(acc[0][e], off, kWave);   // (NV is 1)
+    }
+    if constexpr (TEAMS > 1) {
+      if (which) __syncthreads();   // the first sums have been read
+      if ((int)(threadIdx.x % TEAM) < LPR) {
+        float* s = s_part + threadIdx.x / TEAM * COLS;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+          for (int e = 0; e < V; ++e)
+            if (at.own(k, e)) s[at.col[k] + e] = acc[k][e];
+      }
+      __syncthreads();
+      for (int c = threadIdx.x; c < a.D; c += S::BLOCK) {
+        float t = 0.0f;
+#pragma unroll
+        for (int m = 0; m < TEAMS; ++m) t += s_part[m * COLS + c];
+        out[which * a.D + c] = t;
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+          if (at.own(k, e)) out[which * a.D + at.col[k] + e] = acc[k][e];
+    }
+  }
+}
+
+// -------------------------------------------- rows read from memory again
 // Sums of two values over the block; every thread gets them.
 __device__ __forceinline__ void block_sum2(float& a, float& b, float (*s)[kNormRowWaves]) {
 #pragma unroll
@@ -179,27 +482,113 @@ layer_norm_columns_kernel(LayerNormGradArgs a, float* __restrict__ partial) {
   }
 }
 
-// dweight and dbias from the partial sums of `parts` blocks of rows.
-__global__ void __launch_bounds__(kNormRowBlock)
+// dweight and dbias from the partial sums of `parts` blocks of rows: 64
+// columns a block, each wave a share of the parts.
+constexpr int kJoinBlock = 1024;
+constexpr int kJoinWaves = kJoinBlock / kWave;
+__global__ void __launch_bounds__(kJoinBlock)
 layer_norm_join_kernel(const float* __restrict__ partial, int64_t parts, int32_t D, void* dweight, void* dbias,
                        int32_t type) {
-  const int64_t i = (int64_t)blockIdx.x * kNormRowBlock + threadIdx.x;
-  if (i >= 2 * (int64_t)D) return;
-  void* out = i < D ? dweight : dbias;
-  if (!out) return;
+  __shared__ float s_sum[kJoinWaves][kWave];
+  const int w = threadIdx.x / kWave, lane = lane_id();
+  const int64_t i = (int64_t)blockIdx.x * kWave + lane;
+  const int64_t width = 2 * (int64_t)D;
   float s[1] = {0.0f};
-  for (int64_t p = 0; p < parts; ++p) s[0] += partial[p * 2 * D + i];
-  store_part<1>(out, type, i < D ? i : i - D, 1, s);
+  if (i < width) {
+    for (int64_t p = w; p < parts; p += kJoinWaves) s[0] += partial[p * width + i];
+  }
+  s_sum[w][lane] = s[0];
+  __syncthreads();
+  if (w != 0 || i >= width) return;
+  s[0] = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kJoinWaves; ++k) s[0] += s_sum[k][lane];
+  void* out = i < D ? dweight : dbias;
+  if (out) store_part<1>(out, type, i < D ? i : i - D, 1, s);
 }
 
-static int64_t grad_parts(int64_t n) { return ceil_div(n, kGradRowsPerBlock); }
+// ------------------------------------------------------------- launching
+// Partial rows of a gradient: at most one per row, and per resident block.
+static int64_t grad_parts(int64_t n, int32_t D) {
+  return D <= kRegColumns ? std::min(n, kRegGradBlocks) : ceil_div(n, kGradRowsPerBlock);
+}
 
 size_t layer_norm_grad_workspace_bytes(int64_t n, int32_t D) {
-  return align_up((size_t)grad_parts(n) * 2 * (size_t)D * sizeof(float)) + 256;
+  return align_up((size_t)grad_parts(n, D) * 2 * (size_t)D * sizeof(float)) + 256;
+}
+
+template <typename T, int LPR, int NV>
+static hipError_t forward_in(const LayerNormArgs& a, hipStream_t stream) {
+  typedef RowShape<T, LPR, NV> S;
+  const int64_t blocks = std::min(ceil_div(a.n, S::ROWS), kRegBlocks);
+  hipLaunchKernelGGL((layer_norm_kernel<T, LPR, NV>), dim3((unsigned)blocks), dim3(S::BLOCK), 0, stream, a);
+  return hipGetLastError();
+}
+template <typename T, int LPR, int NV>
+static hipError_t backward_in(const LayerNormGradArgs& a, float* partial, int64_t* parts, hipStream_t stream) {
+  typedef RowShape<T, LPR, NV> S;
+  const int64_t blocks = std::min(ceil_div(a.n, S::ROWS), kRegGradBlocks);
+  *parts = blocks;
+  hipLaunchKernelGGL((layer_norm_grad_kernel<T, LPR, NV>), dim3((unsigned)blocks), dim3(S::BLOCK), 0, stream, a,
+                     partial);
+  return hipGetLastError();
+}
+
+// Calls f<LPR, NV>() for the shape of rows of D elements of T: as few threads
+// as hold the row, one vector each up to a wave (more rows per wave and more
+// of them in flight then), up to kPerThread elements each beyond.
+template <typename T, typename F>
+static hipError_t with_shape(int32_t D, const F& f) {
+  constexpr int V = kVec<T>;
+  constexpr int M = kPerThread / V;             // most vectors per thread
+  const int vecs = (D + V - 1) / V;
+  if (vecs <= 1) return f.template run<1, 1>();
+  if (vecs <= 2) return f.template run<2, 1>();
+  if (vecs <= 4) return f.template run<4, 1>();
+  if (vecs <= 8) return f.template run<8, 1>();
+  if (vecs <= 16) return f.template run<16, 1>();
+  if (vecs <= 32) return f.template run<32, 1>();
+  if (vecs <= 64) return f.template run<64, 1>();
+  if (vecs <= 128) return f.template run<64, 2>();
+  if constexpr (M > 2) {
+    if (vecs <= 192) return f.template run<64, 3>();
+    if (vecs <= 256) return f.template run<64, 4>();
+    if (vecs <= 384) return f.template run<128, 3>();
+    if (vecs <= 512) return f.template run<128, 4>();
+    if (vecs <= 768) return f.template run<256, 3>();
+    if (vecs <= 1024) return f.template run<256, 4>();
+    if (vecs <= 1536) return f.template run<512, 3>();
+    if (vecs <= 2048) return f.template run<512, 4>();
+    if (vecs <= 3 * 1024) return f.template run<1024, 3>();
+    return f.template run<1024, 4>();
+  } else {
+    if (vecs <= 256) return f.template run<128, 2>();
+    if (vecs <= 512) return f.template run<256, 2>();
+    if (vecs <= 1024) return f.template run<512, 2>();
+    return f.template run<1024, 2>();
+  }
 }
 
 template <typename T>
+struct ForwardCall {
+  const LayerNormArgs& a;
+  hipStream_t stream;
+  template <int LPR, int NV>
+  hipError_t run() const { return forward_in<T, LPR, NV>(a, stream); }
+};
+template <typename T>
+struct BackwardCall {
+  const LayerNormGradArgs& a;
+  float* partial;
+  int64_t* parts;
+  hipStream_t stream;
+  template <int LPR, int NV>
+  hipError_t run() const { return backward_in<T, LPR, NV>(a, partial, parts, stream); }
+};
+
+template <typename T>
 static hipError_t forward_as(const LayerNormArgs& a, hipStream_t stream) {
+  if (a.D <= kRegColumns) return with_shape<T>(a.D, ForwardCall<T>{a, stream});
   hipLaunchKernelGGL(layer_norm_wide_kernel<T>, dim3((unsigned)std::min(a.n, kMaxRowGrid)), dim3(kNormRowBlock), 0,
                      stream, a);
   return hipGetLastError();
@@ -213,12 +602,14 @@ hipError_t launch_layer_norm(const LayerNormArgs& a, hipStream_t stream) {
 }
 
 template <typename T>
-static hipError_t backward_as(const LayerNormGradArgs& a, float* partial, hipStream_t stream) {
+static hipError_t backward_as(const LayerNormGradArgs& a, float* partial, int64_t* parts, hipStream_t stream) {
+  if (a.D <= kRegColumns) return with_shape<T>(a.D, BackwardCall<T>{a, partial, parts, stream});
+  *parts = ceil_div(a.n, kGradRowsPerBlock);
   // the columns first: dx may take dy's place
   if (a.dweight || a.dbias) {
     const unsigned slices = (unsigned)ceil_div(a.D, kWave * kVec<T>);
-    hipLaunchKernelGGL(layer_norm_columns_kernel<T>, dim3((unsigned)grad_parts(a.n), slices), dim3(kNormRowBlock), 0,
-                       stream, a, partial);
+    hipLaunchKernelGGL(layer_norm_columns_kernel<T>, dim3((unsigned)*parts, slices), dim3(kNormRowBlock), 0, stream, a,
+                       partial);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -230,17 +621,16 @@ static hipError_t backward_as(const LayerNormGradArgs& a, float* partial, hipStr
 
 hipError_t launch_layer_norm_grad(const LayerNormGradArgs& a, void* ws, hipStream_t stream) {
   float* partial = static_cast<float*>(ws);
-  hipError_t e = hipSuccess;
-  if (a.n > 0) {
-    e = a.type == GBA_F32    ? backward_as<float>(a, partial, stream)
-        : a.type == GBA_BF16 ? backward_as<bf16_t>(a, partial, stream)
-                             : backward_as<f16_t>(a, partial, stream);
+  int64_t parts = 0;
+  if (a.n > 0 && (a.dx || a.dweight || a.dbias)) {
+    const hipError_t e = a.type == GBA_F32    ? backward_as<float>(a, partial, &parts, stream)
+                         : a.type == GBA_BF16 ? backward_as<bf16_t>(a, partial, &parts, stream)
+                                              : backward_as<f16_t>(a, partial, &parts, stream);
     if (e != hipSuccess) return e;
   }
   if (!a.dweight && !a.dbias) return hipSuccess;
-  hipLaunchKernelGGL(layer_norm_join_kernel, dim3((unsigned)ceil_div(2 * (int64_t)a.D, kNormRowBlock)),
-                     dim3(kNormRowBlock), 0, stream, (const float*)partial, grad_parts(a.n), a.D, a.dweight, a.dbias,
-                     a.grad_type);
+  hipLaunchKernelGGL(layer_norm_join_kernel, dim3((unsigned)ceil_div(2 * (int64_t)a.D, kWave)), dim3(kJoinBlock), 0,
+                     stream, (const float*)partial, parts, a.D, a.dweight, a.dbias, a.grad_type);
   return hipGetLastError();
 }
 
