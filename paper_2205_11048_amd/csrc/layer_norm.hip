@@ -21,9 +21,10 @@ constexpr int kNormRowWaves = kNormRowBlock / kWave;
 constexpr int64_t kGradRowsPerBlock = 256;   // ... of a partial sum of the weight's gradient
 constexpr int64_t kMaxRowGrid = 1 << 20;
 
-constexpr int kPerThread = 16;               // most elements of a row a thread holds
+constexpr int kPerThread = 16;               // elements of its rows a thread holds, forward
+constexpr int kGradVecs = 2;                 // most 16-byte vectors of a row a thread holds, backward
 constexpr int kRegBlock = 512;
-constexpr int kRegColumns = 1024 * kPerThread;   // widest row held in registers
+constexpr int kWidest = 1024;                // most threads of a row
 constexpr int64_t kRegGradBlocks = 512;      // most blocks of a gradient: two per compute unit
 constexpr int64_t kRegBlocks = 1024;         // ... of a forward call
 
@@ -59,11 +60,11 @@ template <typename T, int LPR, int NV>
 struct RowShape {
   static constexpr int V = kVec<T>;
   static constexpr int E = V * NV;
-  static constexpr int RU = kPerThread / E;
   static constexpr int BLOCK = LPR > kRegBlock ? LPR : kRegBlock;
   static constexpr int G = BLOCK / LPR;         // thread groups of a block
-  static constexpr int ROWS = G * RU;           // rows of a block at a time
   static constexpr int WAVES = BLOCK / kWave;
+  static constexpr int RU = kPerThread / E;             // forward
+  static constexpr int RU_GRAD = NV == 1 ? 2 : 1;       // backward
 };
 
 template <typename T, int LPR, int NV>
@@ -91,6 +92,17 @@ struct RowPlace {
   __device__ __forceinline__ void load(const P* __restrict__ p, int k, float (&o)[V]) const {
     if (tiny) load_part<P, V>(p, D, o);
     else load_vec<P, V>(p + col[k], o);
+  }
+  // as it is in memory
+  __device__ __forceinline__ typename VecOf<T, V>::type load_raw(const T* __restrict__ p, int k) const {
+    typename VecOf<T, V>::type v;
+    if (tiny) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[e] = e < D ? p[e] : (T)0.0f;
+    } else {
+      v = *reinterpret_cast<const typename VecOf<T, V>::type*>(p + col[k]);
+    }
+    return v;
   }
   __device__ __forceinline__ void load(const void* __restrict__ p, int type, int k, float (&o)[V]) const {
     if (type == GBA_F32) load(static_cast<const float*>(p), k, o);
@@ -132,7 +144,7 @@ template <typename T, int LPR, int NV>
 __global__ void __launch_bounds__((RowShape<T, LPR, NV>::BLOCK))
 layer_norm_kernel(LayerNormArgs a) {
   typedef RowShape<T, LPR, NV> S;
-  constexpr int V = S::V, RU = S::RU;
+  constexpr int V = S::V, RU = S::RU, ROWS = S::G * RU;
   __shared__ float s_sum[2][RU][S::WAVES];
   const int gl = threadIdx.x % LPR, grp = threadIdx.x / LPR;
   const RowPlace<T, LPR, NV> at(gl, a.D);
@@ -149,7 +161,7 @@ layer_norm_kernel(LayerNormArgs a) {
   }
   const float D = (float)a.D;
   int buffer = 0;
-  for (int64_t r0 = (int64_t)blockIdx.x * S::ROWS; r0 < a.n; r0 += (int64_t)gridDim.x * S::ROWS) {
+  for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < a.n; r0 += (int64_t)gridDim.x * ROWS) {
     float x[RU][NV][V], sum[RU];
 #pragma unroll
     for (int u = 0; u < RU; ++u) {
@@ -202,11 +214,14 @@ layer_norm_kernel(LayerNormArgs a) {
   }
 }
 
+// The rows are kept as they are in memory and widened twice, and the next rows
+// are asked for before the present ones are worked on.
 template <typename T, int LPR, int NV>
-__global__ void __launch_bounds__((RowShape<T, LPR, NV>::BLOCK))
+__global__ void __launch_bounds__((RowShape<T, LPR, NV>::BLOCK), 4)
 layer_norm_grad_kernel(LayerNormGradArgs a, float* __restrict__ partial) {
   typedef RowShape<T, LPR, NV> S;
-  constexpr int V = S::V, RU = S::RU;
+  typedef typename VecOf<T, S::V>::type vec;
+  constexpr int V = S::V, RU = S::RU_GRAD, ROWS = S::G * RU;
   // the block's sums of the weight's gradient: one row per wave or per group of several waves
   constexpr int TEAM = LPR < kWave ? kWave : LPR;
   constexpr int TEAMS = S::BLOCK / TEAM;
@@ -227,55 +242,78 @@ layer_norm_grad_kernel(LayerNormGradArgs a, float* __restrict__ partial) {
   }
   const float D = (float)a.D;
   int buffer = 0;
-  for (int64_t r0 = (int64_t)blockIdx.x * S::ROWS; r0 < a.n; r0 += (int64_t)gridDim.x * S::ROWS) {
-    float x[RU][NV][V], g[RU][NV][V], rstd[RU], mean[RU], sum[2 * RU];
+  vec x[RU][NV], g[RU][NV], xn[RU][NV], gn[RU][NV];
+  float mean[RU], rstd[RU], mn[RU], rn[RU];
+  auto load_rows = [&](int64_t r0, vec (&xv)[RU][NV], vec (&gv)[RU][NV], float (&m)[RU], float (&s)[RU]) {
 #pragma unroll
     for (int u = 0; u < RU; ++u) {
       const int64_t r = r0 + u * S::G + grp, rc = r < a.n ? r : a.n - 1;
-      mean[u] = a.mean[rc];
-      rstd[u] = a.rstd[rc];
       const T* p = static_cast<const T*>(a.x) + rc * a.x_stride;
       const T* q = static_cast<const T*>(a.dy) + rc * a.dy_stride;
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
-        at.load(p, k, x[u][k]);
-        at.load(q, k, g[u][k]);
+        xv[u][k] = at.load_raw(p, k);
+        gv[u][k] = at.load_raw(q, k);
       }
+      m[u] = a.mean[rc];
+      s[u] = a.rstd[rc];
     }
+  };
+  const int64_t step = (int64_t)gridDim.x * ROWS;
+  int64_t r0 = (int64_t)blockIdx.x * ROWS;
+  load_rows(r0, x, g, mean, rstd);
+  for (; r0 < a.n; r0 += step) {
+    const bool more = r0 + step < a.n;
+    if (more) load_rows(r0 + step, xn, gn, mn, rn);
+    float sum[2 * RU];
 #pragma unroll
     for (int u = 0; u < RU; ++u) {
-      const bool in = r0 + u * S::G + grp < a.n;
       sum[2 * u] = sum[2 * u + 1] = 0.0f;
+      if (r0 + u * S::G + grp >= a.n) continue;
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          const float xh = (x[u][k][e] - mean[u]) * rstd[u];
-          const float gy = g[u][k][e];
-          x[u][k][e] = xh;
+          const float xh = ((float)x[u][k][e] - mean[u]) * rstd[u];
+          // a foreign element adds 0 (what it adds to dw is not kept)
+          const float gy = at.own(k, e) ? (float)g[u][k][e] : 0.0f;
           const float h = gy * w[k][e];
-          const bool own = at.own(k, e);
-          sum[2 * u] += own ? h : 0.0f;
-          sum[2 * u + 1] = own ? __builtin_fmaf(h, xh, sum[2 * u + 1]) : sum[2 * u + 1];
-          dw[k][e] = in ? __builtin_fmaf(gy, xh, dw[k][e]) : dw[k][e];
-          db[k][e] += in ? gy : 0.0f;
-          g[u][k][e] = h;
+          sum[2 * u] += h;
+          sum[2 * u + 1] = __builtin_fmaf(h, xh, sum[2 * u + 1]);
+          dw[k][e] = __builtin_fmaf(gy, xh, dw[k][e]);
+          db[k][e] += gy;
         }
     }
-    if (!a.dx) continue;
-    row_sum<LPR, S::WAVES>(sum, s_sum, buffer);
+    if (a.dx) {
+      row_sum<LPR, S::WAVES>(sum, s_sum, buffer);
 #pragma unroll
-    for (int u = 0; u < RU; ++u) {
-      const int64_t r = r0 + u * S::G + grp;
-      if (r >= a.n) continue;
-      const float s1 = sum[2 * u] / D, s2 = sum[2 * u + 1] / D;
-      T* q = static_cast<T*>(a.dx) + r * a.dx_stride;
+      for (int u = 0; u < RU; ++u) {
+        const int64_t r = r0 + u * S::G + grp;
+        if (r >= a.n) continue;
+        const float s1 = sum[2 * u] / D, s2 = sum[2 * u + 1] / D;
+        T* q = static_cast<T*>(a.dx) + r * a.dx_stride;
 #pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        float d[V];
+        for (int k = 0; k < NV; ++k) {
+          float d[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) d[e] = rstd[u] * (g[u][k][e] - s1 - x[u][k][e] * s2);
-        at.store(q, k, d);
+          for (int e = 0; e < V; ++e) {
+            const float xh = ((float)x[u][k][e] - mean[u]) * rstd[u];
+            d[e] = rstd[u] * ((float)g[u][k][e] * w[k][e] - s1 - xh * s2);
+          }
+          at.store(q, k, d);
+        }
+      }
+    }
+    if (more) {
+#pragma unroll
+      for (int u = 0; u < RU; ++u) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          x[u][k] = xn[u][k];
+          g[u][k] = gn[u][k];
+        }
+        mean[u] = mn[u];
+        rstd[u] = rn[u];
       }
     }
   }
@@ -495,6 +533,7 @@ layer_norm_join_kernel(const float* __restrict__ partial, int64_t parts, int32_t
   const int64_t width = 2 * (int64_t)D;
   float s[1] = {0.0f};
   if (i < width) {
+#pragma unroll 8
     for (int64_t p = w; p < parts; p += kJoinWaves) s[0] += partial[p * width + i];
   }
   s_sum[w][lane] = s[0];
@@ -508,40 +547,39 @@ layer_norm_join_kernel(const float* __restrict__ partial, int64_t parts, int32_t
 }
 
 // ------------------------------------------------------------- launching
-// Partial rows of a gradient: at most one per row, and per resident block.
-static int64_t grad_parts(int64_t n, int32_t D) {
-  return D <= kRegColumns ? std::min(n, kRegGradBlocks) : ceil_div(n, kGradRowsPerBlock);
-}
+// Widest rows held in registers.
+constexpr int kForwardColumns = kWidest * kPerThread;
+constexpr int kGradColumns = kWidest * kGradVecs * kVec<float>;
 
+// Partial rows of a gradient: at most one per row and per resident block of
+// rows in registers, else one per kGradRowsPerBlock rows.
 size_t layer_norm_grad_workspace_bytes(int64_t n, int32_t D) {
-  return align_up((size_t)grad_parts(n, D) * 2 * (size_t)D * sizeof(float)) + 256;
+  const int64_t parts = D <= kGradColumns ? std::min(n, kRegGradBlocks) : ceil_div(n, kGradRowsPerBlock);
+  return align_up((size_t)parts * 2 * (size_t)D * sizeof(float)) + 256;
 }
 
 template <typename T, int LPR, int NV>
 static hipError_t forward_in(const LayerNormArgs& a, hipStream_t stream) {
   typedef RowShape<T, LPR, NV> S;
-  const int64_t blocks = std::min(ceil_div(a.n, S::ROWS), kRegBlocks);
+  const int64_t blocks = std::min(ceil_div(a.n, S::G * S::RU), kRegBlocks);
   hipLaunchKernelGGL((layer_norm_kernel<T, LPR, NV>), dim3((unsigned)blocks), dim3(S::BLOCK), 0, stream, a);
   return hipGetLastError();
 }
 template <typename T, int LPR, int NV>
 static hipError_t backward_in(const LayerNormGradArgs& a, float* partial, int64_t* parts, hipStream_t stream) {
   typedef RowShape<T, LPR, NV> S;
-  const int64_t blocks = std::min(ceil_div(a.n, S::ROWS), kRegGradBlocks);
+  const int64_t blocks = std::min(ceil_div(a.n, S::G * S::RU_GRAD), kRegGradBlocks);
   *parts = blocks;
   hipLaunchKernelGGL((layer_norm_grad_kernel<T, LPR, NV>), dim3((unsigned)blocks), dim3(S::BLOCK), 0, stream, a,
                      partial);
   return hipGetLastError();
 }
 
-// Calls f<LPR, NV>() for the shape of rows of D elements of T: as few threads
-// as hold the row, one vector each up to a wave (more rows per wave and more
-// of them in flight then), up to kPerThread elements each beyond.
-template <typename T, typename F>
-static hipError_t with_shape(int32_t D, const F& f) {
-  constexpr int V = kVec<T>;
-  constexpr int M = kPerThread / V;             // most vectors per thread
-  const int vecs = (D + V - 1) / V;
+// Calls f.run<LPR, NV>() for the shape of rows of `vecs` vectors: as few
+// threads as hold the row, one vector each up to a wave (more rows per wave
+// and more of them in flight then), up to M each beyond; MOST vectors at most.
+template <int M, int MOST, typename F>
+static hipError_t with_shape(int vecs, const F& f) {
   if (vecs <= 1) return f.template run<1, 1>();
   if (vecs <= 2) return f.template run<2, 1>();
   if (vecs <= 4) return f.template run<4, 1>();
@@ -550,7 +588,7 @@ static hipError_t with_shape(int32_t D, const F& f) {
   if (vecs <= 32) return f.template run<32, 1>();
   if (vecs <= 64) return f.template run<64, 1>();
   if (vecs <= 128) return f.template run<64, 2>();
-  if constexpr (M > 2) {
+  if constexpr (M == 4) {
     if (vecs <= 192) return f.template run<64, 3>();
     if (vecs <= 256) return f.template run<64, 4>();
     if (vecs <= 384) return f.template run<128, 3>();
@@ -562,10 +600,15 @@ static hipError_t with_shape(int32_t D, const F& f) {
     if (vecs <= 3 * 1024) return f.template run<1024, 3>();
     return f.template run<1024, 4>();
   } else {
+    static_assert(M == 2, "two vectors a thread, or four");
     if (vecs <= 256) return f.template run<128, 2>();
     if (vecs <= 512) return f.template run<256, 2>();
-    if (vecs <= 1024) return f.template run<512, 2>();
-    return f.template run<1024, 2>();
+    if constexpr (MOST <= 1024) {
+      return f.template run<512, 2>();
+    } else {
+      if (vecs <= 1024) return f.template run<512, 2>();
+      return f.template run<1024, 2>();
+    }
   }
 }
 
@@ -588,7 +631,8 @@ struct BackwardCall {
 
 template <typename T>
 static hipError_t forward_as(const LayerNormArgs& a, hipStream_t stream) {
-  if (a.D <= kRegColumns) return with_shape<T>(a.D, ForwardCall<T>{a, stream});
+  if (a.D <= kForwardColumns)
+    return with_shape<kPerThread / kVec<T>, kForwardColumns / kVec<T>>((int)ceil_div(a.D, kVec<T>), ForwardCall<T>{a, stream});
   hipLaunchKernelGGL(layer_norm_wide_kernel<T>, dim3((unsigned)std::min(a.n, kMaxRowGrid)), dim3(kNormRowBlock), 0,
                      stream, a);
   return hipGetLastError();
@@ -603,7 +647,8 @@ hipError_t launch_layer_norm(const LayerNormArgs& a, hipStream_t stream) {
 
 template <typename T>
 static hipError_t backward_as(const LayerNormGradArgs& a, float* partial, int64_t* parts, hipStream_t stream) {
-  if (a.D <= kRegColumns) return with_shape<T>(a.D, BackwardCall<T>{a, partial, parts, stream});
+  if (a.D <= kGradColumns)
+    return with_shape<kGradVecs, kGradColumns / kVec<T>>((int)ceil_div(a.D, kVec<T>), BackwardCall<T>{a, partial, parts, stream});
   *parts = ceil_div(a.n, kGradRowsPerBlock);
   // the columns first: dx may take dy's place
   if (a.dweight || a.dbias) {
