@@ -74,21 +74,24 @@ hipError_t launch_embedding_lookup(const LookupArgs& a, hipStream_t stream) {
 }
 
 // -------------------------------------------------------------- gradient
-// Positions of a lane group and of a block, for lpr lanes per row slice.
-constexpr int group_span(int lpr) { return lpr <= 8 ? 4 * lpr : 32; }
-constexpr int block_span(int lpr) { return kEmbBlock / lpr * group_span(lpr); }
-static_assert(block_span(1) == 1024 && block_span(8) == 1024 && block_span(64) == 128, "spans divide a run tile");
+constexpr int kRows = 8;             // gradient rows of a batch: as many loads in flight per lane group
+constexpr int kMaxPos = 1024;        // most positions of a block
+constexpr int64_t kMostBlocks = (int64_t(1) << 24) - 1;   // of a launch: 2^32 threads
 
 struct GradScratch {
   RunHeads heads;          // one row per distinct ID: where the blocks' numbering begins
   float* pieces;           // [blocks][2][D]: what the block's first ID adds to an ID of an earlier block, and the
                            // block's part of an ID that begins in it and goes on in the next
   uint32_t* tail_run;      // [blocks] the row of that second ID (one row per distinct ID)
+  int span;                // positions of a lane group
+  int pos;                 // ... and of a block: a power of two, at most kMaxPos
+  int slices;              // column slices
+  unsigned blocks;         // blocks of positions
 };
 
 // The first position whose key is not below `key` in keys[0, n): 64 probes a
 // step, by one wave.
-__device__ __forceinline__ int64_t wave_lower_bound(const uint32_t* __restrict__ keys, int64_t n, uint32_t key) {
+__device__ __forceinline__ int64_t wave_lower_bound(const uint32_t* __restrict__ keys, int64_t n, uint64_t key) {
   int64_t lo = 0, len = n;   // the answer is in [lo, lo + len]
   while (len > 0) {
     const int64_t step = (len + kWave - 1) / kWave;
@@ -104,20 +107,67 @@ __device__ __forceinline__ int64_t wave_lower_bound(const uint32_t* __restrict__
   return lo;
 }
 
+// Where a thread's V columns of a row lie.  The last vector of a row is moved
+// back to end with it: its first `shift` elements are another thread's, which
+// computes and stores the same values.
+template <int V>
+struct Columns {
+  int c, shift, D;
+  bool on;       // the thread has columns
+  bool tiny;     // rows narrower than a vector: element by element
+  __device__ __forceinline__ Columns(int first, int width) : D(width) {
+    on = first < width;
+    tiny = width < V;
+    c = tiny ? 0 : (first + V > width ? width - V : first);
+    shift = tiny ? 0 : first - c;
+  }
+};
+
 // out row `r` (scaled, rounded once), added to what is there if asked for.
 template <int V>
-__device__ __forceinline__ void write_row(const EmbeddingGradArgs& a, int64_t r, int c, const float (&acc)[V]) {
+__device__ __forceinline__ void write_row(const EmbeddingGradArgs& a, const Columns<V>& at, int64_t r,
+                                          const float (&acc)[V]) {
   float v[V];
-  const int64_t at = r * a.out_stride + c;
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] = acc[e] * a.scale;
+  int64_t o = r * a.out_stride + at.c;
   if (a.accumulate) {
-    load_part<V>(a.out, a.out_type, at, a.D - c, v);
+    // an element shared with another thread is added once, by its owner
 #pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = __builtin_fmaf(acc[e], a.scale, v[e]);
-  } else {
-#pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = acc[e] * a.scale;
+    for (int e = 0; e < V; ++e) {
+      float old[1];
+      if (e < at.shift || (at.tiny && e >= at.D)) continue;
+      load_part<1>(a.out, a.out_type, o + e, 1, old);
+      old[0] = __builtin_fmaf(acc[e], a.scale, old[0]);
+      store_part<1>(a.out, a.out_type, o + e, 1, old);
+    }
+    return;
   }
-  store_part<V>(a.out, a.out_type, at, a.D - c, v);
+  store_part<V>(a.out, a.out_type, o, at.tiny ? at.D : V, v);
+}
+
+// Clears the table, 16 bytes a thread: neighbouring blocks write neighbouring
+// bytes, which the memory takes fastest (100,000 x 4096 f32 217 us, 7.5 TB/s;
+// blocks of eight rows each that leave out the rows a token asked for, found
+// among the sorted IDs, 253 us, though they write 6 percent less).
+__global__ void __launch_bounds__(kEmbBlock)
+clear_table_kernel(EmbeddingGradArgs a) {
+  typedef VecOf<uint16_t, 8>::type vec;
+  const int size = a.out_type == GBA_F32 ? 2 : 1;   // in units of 2 bytes
+  const bool flat = a.out_stride == a.D;
+  const int64_t rows = flat ? 1 : a.R, units = (flat ? a.R : 1) * a.D * size;
+  const int64_t per_row = ceil_div(units, 8), total = rows * per_row;
+  uint16_t* out = static_cast<uint16_t*>(a.out);
+  for (int64_t i = (int64_t)blockIdx.x * kEmbBlock + threadIdx.x; i < total; i += (int64_t)gridDim.x * kEmbBlock) {
+    const int64_t row = flat ? 0 : i / per_row;
+    const int64_t c = (i - row * per_row) * 8;
+    uint16_t* p = out + row * a.out_stride * size + c;
+    if (c + 8 <= units) {
+      *reinterpret_cast<vec*>(p) = vec{};
+    } else {
+      for (int e = 0; e < (int)(units - c); ++e) p[e] = 0;
+    }
+  }
 }
 
 // ROWS: one row per distinct ID (else the whole table).
@@ -126,10 +176,8 @@ __global__ void __launch_bounds__(kEmbBlock)
 embedding_grad_kernel(EmbeddingGradArgs a, GradScratch g) {
   constexpr int V = kVec<T>;
   constexpr int G = kEmbBlock / LPR;
-  constexpr int S = group_span(LPR);
-  constexpr int POS = block_span(LPR);
-  constexpr int kRows = 8;                       // rows in flight per lane group
-  static_assert(S % 4 == 0, "whole batches");
+  constexpr int POS = G * 32 < kMaxPos ? G * 32 : kMaxPos;   // most positions of the block
+  typedef typename VecOf<T, V>::type vec;
   __shared__ uint32_t sk[POS];                   // the block's keys
   __shared__ uint32_t sv[POS];                   // ... their tokens
   __shared__ uint32_t srun[ROWS ? POS : 1];      // ... their rows of the output
@@ -138,8 +186,11 @@ embedding_grad_kernel(EmbeddingGradArgs a, GradScratch g) {
   __shared__ uint32_t s_group[kEmbWaves];
   __shared__ uint32_t s_pad;
 
-  const int64_t b0 = (int64_t)blockIdx.x * POS;
-  const int cnt = (int)(a.n - b0 < POS ? a.n - b0 : POS);
+  const unsigned block = blockIdx.x / g.slices;
+  const int slice = (int)(blockIdx.x - block * g.slices);
+  const int S = g.span;
+  const int64_t b0 = (int64_t)block * g.pos;
+  const int cnt = (int)(a.n - b0 < g.pos ? a.n - b0 : g.pos);
   const bool padded = a.padding >= 0 && a.padding < a.R;
   const uint32_t pad = (uint32_t)a.padding;
   // keys before the block and after it (there is none: no key is equal)
@@ -147,8 +198,9 @@ embedding_grad_kernel(EmbeddingGradArgs a, GradScratch g) {
   const uint32_t prev = has_prev ? a.keys[b0 - 1] : 0u;
   const uint32_t next = has_next ? a.keys[b0 + cnt] : 0u;
   for (int i = threadIdx.x; i < cnt; i += kEmbBlock) {
-    sk[i] = a.keys[b0 + i];
-    sv[i] = a.vals[b0 + i];
+    const uint32_t key = a.keys[b0 + i], val = a.vals[b0 + i];
+    sk[i] = key;
+    sv[i] = padded && key == pad ? 0u : val;   // (a padding token's row is not needed: one that is near)
   }
   if (ROWS) {
     // run heads in the block's tile before the block
@@ -195,7 +247,7 @@ embedding_grad_kernel(EmbeddingGradArgs a, GradScratch g) {
       const uint32_t key = sk[p];
       const uint32_t r = run - 1 - (hidden && key > pad ? 1u : 0u);
       srun[p] = r;
-      if (blockIdx.y == 0) {
+      if (slice == 0) {
         if (h[k] && !(padded && key == pad)) a.unique_ids[r] = (int64_t)key;
         if (b0 + p == a.n - 1) *a.num_unique = (int64_t)run - hidden;
       }
@@ -204,43 +256,61 @@ embedding_grad_kernel(EmbeddingGradArgs a, GradScratch g) {
   }
 
   const int grp = threadIdx.x / LPR, gl = threadIdx.x % LPR;
-  const int c = (int)blockIdx.y * (LPR * V) + gl * V;
-  const bool on = c < a.D;   // (a group's lanes past the row's end only wait at the barrier)
+  const Columns<V> at(slice * (LPR * V) + gl * V, a.D);
   const int first = grp * S, end = first + S < cnt ? first + S : cnt;
   auto next_is = [&](int p, uint32_t key) { return p + 1 < cnt ? sk[p + 1] == key : has_next && next == key; };
   auto prev_is = [&](int p, uint32_t key) { return p > 0 ? sk[p - 1] == key : has_prev && prev == key; };
   auto out_row = [&](int p) { return ROWS ? (int64_t)srun[p] : (int64_t)sk[p]; };
 
-  if (on && first < end) {
-    const T* grad = static_cast<const T*>(a.grad) + c;
-    const int count = a.D - c;
-    float acc[V] = {};
-    bool begins = !prev_is(first, sk[first]);
-    for (int p = first; p < end; p += kRows) {
-      float v[kRows][V];
+  // Bit i of a group's word: the ID at its position i ends there.  The
+  // positions of a wave's groups are adjacent: 64 a ballot.
+  uint32_t ends = 0;
+  {
+    constexpr int kGroups = kWave / LPR;   // lane groups of a wave
+    const int w0 = (int)(threadIdx.x / kWave) * kGroups * S;
+    const int mine = (grp % kGroups) * S;
+    for (int k = 0; k < kGroups * S; k += kWave) {
+      const int p = w0 + k + lane_id();
+      const bool stop = k + lane_id() < kGroups * S && p < cnt && !next_is(p, sk[p]);
+      const uint64_t m = __ballot(stop);
+      if (mine >= k && mine < k + kWave) ends = (uint32_t)(m >> (mine - k));
+    }
+  }
+
+  if (at.on && first < end) {
+    const T* grad = static_cast<const T*>(a.grad) + at.c;
+    auto load_batch = [&](int p, vec (&v)[kRows]) {
 #pragma unroll
       for (int u = 0; u < kRows; ++u) {
-        // past the end the last row again; a padding token's row is not looked at
-        const int q = p + u < end ? p + u : end - 1;
-        if (padded && sk[q] == pad) {
+        uint32_t row = sv[p + u < end ? p + u : end - 1];   // past the end the last row again
+        if constexpr (LPR == kWave) row = __builtin_amdgcn_readfirstlane(row);
+        const T* src = grad + (int64_t)row * a.grad_stride;
+        if (at.tiny) {
 #pragma unroll
-          for (int e = 0; e < V; ++e) v[u][e] = 0.0f;
+          for (int e = 0; e < V; ++e) v[u][e] = e < at.D ? src[e] : (T)0.0f;
         } else {
-          load_part<T, V>(grad + (int64_t)sv[q] * a.grad_stride, count, v[u]);
+          v[u] = *reinterpret_cast<const vec*>(src);
         }
       }
+    };
+    float acc[V] = {};
+    bool begins = !prev_is(first, sk[first]);
+    vec v[kRows], ahead[kRows];
+    load_batch(first, v);
+    for (int p = first; p < end; p += kRows) {
+      if (p + kRows < end) load_batch(p + kRows, ahead);
 #pragma unroll
       for (int u = 0; u < kRows; ++u) {
         const int q = p + u;
         if (q >= end) break;
 #pragma unroll
-        for (int e = 0; e < V; ++e) acc[e] += v[u][e];
+        for (int e = 0; e < V; ++e) acc[e] += (float)v[u][e];
+        const bool stop = ends >> (q - first) & 1u;
+        if (!stop && q + 1 < end) continue;
         const uint32_t key = sk[q];
-        const bool goes_on = next_is(q, key);
-        if (goes_on && q + 1 < end) continue;
         if (!(padded && key == pad)) {
-          if (begins && !goes_on) {
-            write_row<V>(a, out_row(q), c, acc);
+          if (begins && stop) {
+            write_row<V>(a, at, out_row(q), acc);
           } else {
 #pragma unroll
             for (int e = 0; e < V; ++e) s_piece[begins ? 1 : 0][grp][gl * V + e] = acc[e];
@@ -250,35 +320,35 @@ embedding_grad_kernel(EmbeddingGradArgs a, GradScratch g) {
 #pragma unroll
         for (int e = 0; e < V; ++e) acc[e] = 0.0f;
       }
+      if (p + kRows < end) {
+#pragma unroll
+        for (int u = 0; u < kRows; ++u) v[u] = ahead[u];
+      }
     }
   }
   __syncthreads();
-  if (!on || first >= end) return;
+  if (!at.on || first >= end) return;
 
-  // The sum of s_piece[0] over the groups after `j0` that hold `key`; *last is
-  // the last position of the key in the block.
-  auto chain = [&](int j0, uint32_t key, float (&acc)[V], int* last) {
-    int at = (j0 + 1) * S < cnt ? (j0 + 1) * S : cnt;   // first position not added yet
-    for (int j = j0 + 1; at < cnt && sk[at] == key; ++j) {
+  // Adds s_piece[0] of the groups after `j0` that hold `key` to acc; returns
+  // the last position of the key in the block, -1 if it is inside a group.
+  auto chain = [&](int j0, uint32_t key, float (&acc)[V]) {
+    int p = (j0 + 1) * S < cnt ? (j0 + 1) * S : cnt;   // first position not added yet
+    for (int j = j0 + 1; p < cnt && sk[p] == key; ++j) {
 #pragma unroll
       for (int e = 0; e < V; ++e) acc[e] += s_piece[0][j][gl * V + e];
-      at = (j + 1) * S < cnt ? (j + 1) * S : cnt;
-      if (sk[at - 1] != key) {   // ends inside the group
-        *last = -1;
-        return;
-      }
+      p = (j + 1) * S < cnt ? (j + 1) * S : cnt;
+      if (sk[p - 1] != key) return -1;
     }
-    *last = at - 1;
+    return p - 1;
   };
-  float* piece = g.pieces + (int64_t)blockIdx.x * 2 * a.D + c;
+  float* piece = g.pieces + (int64_t)block * 2 * a.D + at.c;
   if (grp == 0 && prev_is(0, sk[0]) && !(padded && sk[0] == pad)) {
     // the block's first ID began in an earlier block
     float acc[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) acc[e] = s_piece[0][0][gl * V + e];
-    int last;
-    if (sk[end - 1] == sk[0]) chain(0, sk[0], acc, &last);
-    store_part<float, V>(piece, a.D - c, acc);
+    if (sk[end - 1] == sk[0]) chain(0, sk[0], acc);
+    store_part<float, V>(piece, at.tiny ? at.D : V, acc);
   }
   const uint32_t key = sk[end - 1];
   if (!next_is(end - 1, key) || (padded && key == pad)) return;
@@ -286,46 +356,47 @@ embedding_grad_kernel(EmbeddingGradArgs a, GradScratch g) {
   float acc[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) acc[e] = s_piece[1][grp][gl * V + e];
-  int last;
-  chain(grp, key, acc, &last);
+  const int last = chain(grp, key, acc);
   if (last == cnt - 1 && has_next && next == key) {
-    store_part<float, V>(piece + a.D, a.D - c, acc);
-    if (ROWS && blockIdx.y == 0 && gl == 0) g.tail_run[blockIdx.x] = srun[end - 1];
+    store_part<float, V>(piece + a.D, at.tiny ? at.D : V, acc);
+    if (ROWS && slice == 0 && gl == 0) g.tail_run[block] = srun[end - 1];
   } else {
-    write_row<V>(a, out_row(end - 1), c, acc);
+    write_row<V>(a, at, out_row(end - 1), acc);
   }
 }
 
 // The IDs that cross blocks: by the block in which each begins.
 template <int V, int LPR, bool ROWS>
 __global__ void __launch_bounds__(kEmbBlock)
-embedding_grad_join_kernel(EmbeddingGradArgs a, GradScratch g, int pos) {
+embedding_grad_join_kernel(EmbeddingGradArgs a, GradScratch g) {
   constexpr int G = kEmbBlock / LPR;
   __shared__ float s_sum[G][LPR * V];
-  const int64_t b = blockIdx.x;
-  const int64_t at = (b + 1) * pos;              // the next block's first position (< n)
-  const uint32_t key = a.keys[at - 1];
-  if (a.keys[at] != key) return;
+  const int64_t b = blockIdx.x / g.slices;
+  const int slice = (int)(blockIdx.x - b * g.slices);
+  const int pos = g.pos;
+  const int64_t first = (b + 1) * pos;           // the next block's first position (< n)
+  const uint32_t key = a.keys[first - 1];
+  if (a.keys[first] != key) return;
   if (b > 0 && a.keys[b * pos] == key && a.keys[b * pos - 1] == key) return;   // began earlier
   if (a.padding >= 0 && (int64_t)key == a.padding) return;
   // blocks after b whose first key it is
   int64_t m = 1;
-  const int64_t blocks = (a.n + pos - 1) / pos;
   for (;;) {
     const int64_t j = b + 1 + m + lane_id();
-    const uint64_t same = __ballot(j < blocks && a.keys[j * pos] == key);
+    const uint64_t same = __ballot(j < (int64_t)g.blocks && a.keys[j * pos] == key);
     const int run = same == ~0ull ? kWave : __ffsll((unsigned long long)~same) - 1;
     m += run;
     if (run < kWave) break;
   }
   const int grp = threadIdx.x / LPR, gl = threadIdx.x % LPR;
-  const int c = (int)blockIdx.y * (LPR * V) + gl * V;
-  const bool on = c < a.D;
+  const Columns<V> at(slice * (LPR * V) + gl * V, a.D);
+  const int count = at.tiny ? at.D : V;
   float acc[V] = {};
-  if (on) {
+  if (at.on) {
+#pragma unroll 4
     for (int64_t j = grp; j < m; j += G) {
       float v[V];
-      load_part<float, V>(g.pieces + (b + 1 + j) * 2 * a.D + c, a.D - c, v);
+      load_part<float, V>(g.pieces + (b + 1 + j) * 2 * a.D + at.c, count, v);
 #pragma unroll
       for (int e = 0; e < V; ++e) acc[e] += v[e];
     }
@@ -333,38 +404,45 @@ embedding_grad_join_kernel(EmbeddingGradArgs a, GradScratch g, int pos) {
 #pragma unroll
   for (int e = 0; e < V; ++e) s_sum[grp][gl * V + e] = acc[e];
   __syncthreads();
-  if (grp != 0 || !on) return;
-  load_part<float, V>(g.pieces + (b * 2 + 1) * a.D + c, a.D - c, acc);
+  if (grp != 0 || !at.on) return;
+  load_part<float, V>(g.pieces + (b * 2 + 1) * a.D + at.c, count, acc);
   const int used = m < G ? (int)m : G;
   for (int j = 0; j < used; ++j) {
 #pragma unroll
     for (int e = 0; e < V; ++e) acc[e] += s_sum[j][gl * V + e];
   }
-  write_row<V>(a, ROWS ? (int64_t)g.tail_run[b] : (int64_t)key, c, acc);
-}
-
-__global__ void __launch_bounds__(kEmbBlock)
-zero_rows_kernel(EmbeddingGradArgs a) {
-  constexpr int V = 4;
-  const int64_t per_row = ceil_div(a.D, V);
-  const int64_t total = a.R * per_row;
-  const float zero[V] = {};
-  for (int64_t i = (int64_t)blockIdx.x * kEmbBlock + threadIdx.x; i < total; i += (int64_t)gridDim.x * kEmbBlock) {
-    const int64_t row = i / per_row;
-    const int c = (int)(i - row * per_row) * V;
-    store_part<V>(a.out, a.out_type, row * a.out_stride + c, a.D - c, zero);
-  }
+  write_row<V>(a, at, ROWS ? (int64_t)g.tail_run[b] : (int64_t)key, acc);
 }
 
 __global__ void no_rows_kernel(int64_t* __restrict__ num_unique) { *num_unique = 0; }
 
+// Positions of a lane group: the most a block's kMaxPos leave, 32 at most, or
+// fewer (kRows at least) while that makes less than kWavesWanted waves.
+constexpr int64_t kWavesWanted = 4096;
+static int most_span(int lpr) { return lpr < 8 ? 4 * lpr : 32; }
+static int group_span(int64_t n, int lpr, int64_t slices) {
+  int s = most_span(lpr);
+  while (s > kRows && n * slices * lpr < kWavesWanted * kWave * s) s >>= 1;
+  return s;
+}
+
 struct GradLayout {
   size_t off_pieces, off_tail, off_tile, off_group, bytes;
 };
-// Room for every size up to n and any element type.
+// Room for every size up to n and any element type: the most blocks that a
+// size up to n has at each span.
 static GradLayout grad_layout(int64_t n, int32_t D) {
-  // the fewest positions of a block: those of 4-byte elements (the most lanes a row)
-  const int64_t blocks = ceil_div(std::max<int64_t>(n, 1), block_span(lanes_for(D, kVec<float>)));
+  int64_t blocks = 1;
+  for (int v = kVec<float>; v <= kVec<bf16_t>; v += v) {
+    const int lpr = lanes_for(D, v);
+    const int64_t slices = ceil_div(D, (int64_t)lpr * v);
+    for (int s = most_span(lpr);; s >>= 1) {
+      int64_t most = n;
+      if (s < most_span(lpr)) most = std::min(n, ceil_div(kWavesWanted * kWave * 2 * s, slices * lpr));
+      blocks = std::max(blocks, ceil_div(most, kEmbBlock / lpr * s));
+      if (s <= kRows) break;
+    }
+  }
   const int64_t tiles = ceil_div(std::max<int64_t>(n, 1), kRunTile);
   GradLayout L{};
   size_t o = 0;
@@ -380,17 +458,21 @@ static GradLayout grad_layout(int64_t n, int32_t D) {
 size_t embedding_grad_workspace_bytes(int64_t n, int32_t D) { return grad_layout(n, D).bytes; }
 
 template <typename T, int LPR, bool ROWS>
-static hipError_t grad_as(const EmbeddingGradArgs& a, const GradScratch& g, hipStream_t stream) {
+static hipError_t grad_as(const EmbeddingGradArgs& a, GradScratch g, hipStream_t stream) {
   constexpr int V = kVec<T>;
-  constexpr int POS = block_span(LPR);
-  const int64_t blocks = ceil_div(a.n, POS);
-  const unsigned slices = (unsigned)ceil_div(a.D, LPR * V);
-  hipLaunchKernelGGL((embedding_grad_kernel<T, LPR, ROWS>), dim3((unsigned)blocks, slices), dim3(kEmbBlock), 0, stream,
-                     a, g);
+  g.slices = (int)ceil_div(a.D, LPR * V);
+  g.span = group_span(a.n, LPR, g.slices);
+  g.pos = kEmbBlock / LPR * g.span;
+  const int64_t blocks = ceil_div(a.n, g.pos);
+  g.blocks = (unsigned)blocks;
+  const int64_t grid = blocks * g.slices;
+  if (grid > kMostBlocks) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((embedding_grad_kernel<T, LPR, ROWS>), dim3((unsigned)grid),
+                     dim3(kEmbBlock), 0, stream, a, g);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || blocks == 1) return e;
-  hipLaunchKernelGGL((embedding_grad_join_kernel<V, LPR, ROWS>), dim3((unsigned)(blocks - 1), slices), dim3(kEmbBlock),
-                     0, stream, a, g, POS);
+  hipLaunchKernelGGL((embedding_grad_join_kernel<V, LPR, ROWS>), dim3((unsigned)((blocks - 1) * g.slices)),
+                     dim3(kEmbBlock), 0, stream, a, g);
   return hipGetLastError();
 }
 
@@ -408,21 +490,22 @@ static hipError_t grad_of(const EmbeddingGradArgs& a, const GradScratch& g, hipS
 }
 
 hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, void* ws, hipStream_t stream) {
-  const bool rows = a.unique_ids != nullptr || a.num_unique != nullptr;
+  const bool rows = a.num_unique != nullptr;
   if (rows && a.n == 0) {
     hipLaunchKernelGGL(no_rows_kernel, dim3(1), dim3(1), 0, stream, a.num_unique);
     return hipGetLastError();
   }
   if (!rows && !a.accumulate) {
-    const int64_t blocks = std::min(ceil_div(a.R * ceil_div(a.D, 4), kEmbBlock), kMaxGrid);
-    hipLaunchKernelGGL(zero_rows_kernel, dim3((unsigned)blocks), dim3(kEmbBlock), 0, stream, a);
+    const int64_t vecs = a.R * ceil_div((int64_t)a.D * (a.out_type == GBA_F32 ? 4 : 2), 16);
+    hipLaunchKernelGGL(clear_table_kernel, dim3((unsigned)std::min(ceil_div(vecs, kEmbBlock), kMaxGrid)),
+                       dim3(kEmbBlock), 0, stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   if (a.n == 0) return hipSuccess;
   const GradLayout L = grad_layout(a.n, a.D);
   char* base = static_cast<char*>(ws);
-  GradScratch g;
+  GradScratch g{};
   g.pieces = reinterpret_cast<float*>(base + L.off_pieces);
   g.tail_run = reinterpret_cast<uint32_t*>(base + L.off_tail);
   if (rows) {
