@@ -4,9 +4,9 @@
 // the sorted list is cut into blocks of positions whatever the IDs, so that a
 // frequent ID's tokens are shared among many lane groups.  A lane group adds
 // up the gradient rows of its positions; an ID that begins and ends inside the
-// group goes straight to the output, what crosses a group's edge is joined in
-// LDS by the group where the ID begins, and what crosses a block's edge by a
-// second launch, through 32-bit partial rows.  Every sum has one order, so the
+// group goes straight to the output, what crosses a group's edge is joined
+// within the block by the group where the ID begins, and what crosses a
+// block's edge by a second launch, through 32-bit partial rows.  Every sum has one order, so the
 // same inputs give the same bits, and no atomic is used.
 #include <algorithm>
 
@@ -171,17 +171,26 @@ clear_table_kernel(EmbeddingGradArgs a) {
 }
 
 // ROWS: one row per distinct ID (else the whole table).
+//
+// A lane group leaves at most two sums that are not finished: `head`, of an ID
+// that began before its first position, and `tail`, of one that begins in the
+// group and goes on after it.  What an ID gets from the groups after the one
+// it begins in is the sum of their heads, up to the first that does not go on
+// (`open`) into its next group: a suffix scan over the wave's groups in
+// registers, then over the block's waves through LDS.
 template <typename T, int LPR, bool ROWS>
 __global__ void __launch_bounds__(kEmbBlock)
 embedding_grad_kernel(EmbeddingGradArgs a, GradScratch g) {
   constexpr int V = kVec<T>;
   constexpr int G = kEmbBlock / LPR;
+  constexpr int kGroups = kWave / LPR;           // lane groups of a wave
   constexpr int POS = G * 32 < kMaxPos ? G * 32 : kMaxPos;   // most positions of the block
   typedef typename VecOf<T, V>::type vec;
   __shared__ uint32_t sk[POS];                   // the block's keys
   __shared__ uint32_t sv[POS];                   // ... their tokens
   __shared__ uint32_t srun[ROWS ? POS : 1];      // ... their rows of the output
-  __shared__ float s_piece[2][G][LPR * V];       // what crosses the groups' edges
+  __shared__ float s_head[kEmbWaves][LPR * V];   // what the waves' first groups give to an ID of an earlier wave
+  __shared__ uint32_t s_open[kEmbWaves];         // ... and whether it goes on into the next wave
   __shared__ uint32_t s_scan[kEmbWaves + 1];
   __shared__ uint32_t s_group[kEmbWaves];
   __shared__ uint32_t s_pad;
@@ -222,6 +231,30 @@ embedding_grad_kernel(EmbeddingGradArgs a, GradScratch g) {
     }
   }
   __syncthreads();
+
+  const int w = threadIdx.x / kWave;
+  const int grp = threadIdx.x / LPR, gl = threadIdx.x % LPR;
+  const Columns<V> at(slice * (LPR * V) + gl * V, a.D);
+  const int first = grp * S, end = first + S < cnt ? first + S : cnt;
+  const T* grad = static_cast<const T*>(a.grad) + at.c;
+  auto load_batch = [&](int p, vec (&v)[kRows]) {
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      uint32_t row = sv[p + u < end ? p + u : end - 1];   // past the end the last row again
+      if constexpr (LPR == kWave) row = __builtin_amdgcn_readfirstlane(row);
+      const T* src = grad + (int64_t)row * a.grad_stride;
+      if (at.tiny) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[u][e] = e < at.D ? src[e] : (T)0.0f;
+      } else {
+        v[u] = *reinterpret_cast<const vec*>(src);
+      }
+    }
+  };
+  vec v[kRows], ahead[kRows];
+  const bool busy = at.on && first < end;
+  if (busy) load_batch(first, v);   // in flight while the rows are numbered
+
   if (ROWS) {
     uint32_t base = g.heads.tile_prefix[b0 / kRunTile] + run_base_sum(s_group);
 #pragma unroll
@@ -255,9 +288,6 @@ embedding_grad_kernel(EmbeddingGradArgs a, GradScratch g) {
     __syncthreads();
   }
 
-  const int grp = threadIdx.x / LPR, gl = threadIdx.x % LPR;
-  const Columns<V> at(slice * (LPR * V) + gl * V, a.D);
-  const int first = grp * S, end = first + S < cnt ? first + S : cnt;
   auto next_is = [&](int p, uint32_t key) { return p + 1 < cnt ? sk[p + 1] == key : has_next && next == key; };
   auto prev_is = [&](int p, uint32_t key) { return p > 0 ? sk[p - 1] == key : has_prev && prev == key; };
   auto out_row = [&](int p) { return ROWS ? (int64_t)srun[p] : (int64_t)sk[p]; };
@@ -266,8 +296,7 @@ embedding_grad_kernel(EmbeddingGradArgs a, GradScratch g) {
   // positions of a wave's groups are adjacent: 64 a ballot.
   uint32_t ends = 0;
   {
-    constexpr int kGroups = kWave / LPR;   // lane groups of a wave
-    const int w0 = (int)(threadIdx.x / kWave) * kGroups * S;
+    const int w0 = w * kGroups * S;
     const int mine = (grp % kGroups) * S;
     for (int k = 0; k < kGroups * S; k += kWave) {
       const int p = w0 + k + lane_id();
@@ -277,26 +306,12 @@ embedding_grad_kernel(EmbeddingGradArgs a, GradScratch g) {
     }
   }
 
-  if (at.on && first < end) {
-    const T* grad = static_cast<const T*>(a.grad) + at.c;
-    auto load_batch = [&](int p, vec (&v)[kRows]) {
-#pragma unroll
-      for (int u = 0; u < kRows; ++u) {
-        uint32_t row = sv[p + u < end ? p + u : end - 1];   // past the end the last row again
-        if constexpr (LPR == kWave) row = __builtin_amdgcn_readfirstlane(row);
-        const T* src = grad + (int64_t)row * a.grad_stride;
-        if (at.tiny) {
-#pragma unroll
-          for (int e = 0; e < V; ++e) v[u][e] = e < at.D ? src[e] : (T)0.0f;
-        } else {
-          v[u] = *reinterpret_cast<const vec*>(src);
-        }
-      }
-    };
+  float head[V] = {}, tail[V] = {};
+  const bool some = first < end;
+  const bool has_head = some && prev_is(first, sk[some ? first : 0]);
+  if (busy) {
     float acc[V] = {};
-    bool begins = !prev_is(first, sk[first]);
-    vec v[kRows], ahead[kRows];
-    load_batch(first, v);
+    bool begins = !has_head;
     for (int p = first; p < end; p += kRows) {
       if (p + kRows < end) load_batch(p + kRows, ahead);
 #pragma unroll
@@ -305,16 +320,13 @@ embedding_grad_kernel(EmbeddingGradArgs a, GradScratch g) {
         if (q >= end) break;
 #pragma unroll
         for (int e = 0; e < V; ++e) acc[e] += (float)v[u][e];
-        const bool stop = ends >> (q - first) & 1u;
-        if (!stop && q + 1 < end) continue;
+        if (!(ends >> (q - first) & 1u)) continue;
         const uint32_t key = sk[q];
-        if (!(padded && key == pad)) {
-          if (begins && stop) {
-            write_row<V>(a, at, out_row(q), acc);
-          } else {
+        if (!begins) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) s_piece[begins ? 1 : 0][grp][gl * V + e] = acc[e];
-          }
+          for (int e = 0; e < V; ++e) head[e] = acc[e];
+        } else if (!(padded && key == pad)) {
+          write_row<V>(a, at, out_row(q), acc);
         }
         begins = true;
 #pragma unroll
@@ -325,43 +337,76 @@ embedding_grad_kernel(EmbeddingGradArgs a, GradScratch g) {
         for (int u = 0; u < kRows; ++u) v[u] = ahead[u];
       }
     }
-  }
-  __syncthreads();
-  if (!at.on || first >= end) return;
-
-  // Adds s_piece[0] of the groups after `j0` that hold `key` to acc; returns
-  // the last position of the key in the block, -1 if it is inside a group.
-  auto chain = [&](int j0, uint32_t key, float (&acc)[V]) {
-    int p = (j0 + 1) * S < cnt ? (j0 + 1) * S : cnt;   // first position not added yet
-    for (int j = j0 + 1; p < cnt && sk[p] == key; ++j) {
 #pragma unroll
-      for (int e = 0; e < V; ++e) acc[e] += s_piece[0][j][gl * V + e];
-      p = (j + 1) * S < cnt ? (j + 1) * S : cnt;
-      if (sk[p - 1] != key) return -1;
+    for (int e = 0; e < V; ++e) {
+      if (begins) tail[e] = acc[e];
+      else head[e] = acc[e];
     }
-    return p - 1;
+  }
+  const uint32_t key = sk[some ? end - 1 : 0];
+  const bool goes_on = some && !(ends >> (end - 1 - first) & 1u);
+  const uint32_t full = some ? ends & (uint32_t)((1ull << (end - first)) - 1) : 0u;
+  bool open = has_head && goes_on && full == 0;   // the group's only ID, from before it to after it
+  const bool has_tail = goes_on && !open;
+
+  // head becomes the sum of the heads from this group on
+#pragma unroll
+  for (int off = 1; off < kGroups; off <<= 1) {
+    const bool here = grp % kGroups + off < kGroups;
+    const bool then = __shfl_down((int)open, off * LPR, kWave) != 0;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float more = __shfl_down(head[e], off * LPR, kWave);
+      head[e] += open && here ? more : 0.0f;
+    }
+    if (here) open = open && then;
+  }
+  if (grp % kGroups == 0) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) s_head[w][gl * V + e] = head[e];
+    if (gl == 0) s_open[w] = open ? 1u : 0u;
+  }
+  // the group after this one, where it is in the wave (every lane takes part
+  // in the exchange: a lane that does not would give 0)
+  float after[V];
+  const bool last_group = grp % kGroups == kGroups - 1;
+  const int next_open = kGroups > 1 ? __shfl_down((int)open, LPR, kWave) : 0;
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    const float more = kGroups > 1 ? __shfl_down(head[e], LPR, kWave) : 0.0f;
+    after[e] = last_group ? 0.0f : more;
+  }
+  const bool after_open = last_group || next_open != 0;
+  __syncthreads();
+  if (!at.on || !some) return;
+
+  // adds the heads of the waves after this one; true: they go on past the block
+  auto add_waves = [&](float (&acc)[V]) {
+    for (int k = w + 1; k < kEmbWaves; ++k) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) acc[e] += s_head[k][gl * V + e];
+      if (!s_open[k]) return false;
+    }
+    return true;
   };
   float* piece = g.pieces + (int64_t)block * 2 * a.D + at.c;
-  if (grp == 0 && prev_is(0, sk[0]) && !(padded && sk[0] == pad)) {
+  if (grp == 0 && has_head && !(padded && sk[0] == pad)) {
     // the block's first ID began in an earlier block
-    float acc[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) acc[e] = s_piece[0][0][gl * V + e];
-    if (sk[end - 1] == sk[0]) chain(0, sk[0], acc);
-    store_part<float, V>(piece, at.tiny ? at.D : V, acc);
+    if (open) add_waves(head);
+    store_part<float, V>(piece, at.tiny ? at.D : V, head);
   }
-  const uint32_t key = sk[end - 1];
-  if (!next_is(end - 1, key) || (padded && key == pad)) return;
-  if (sk[first] == key && prev_is(first, key)) return;   // began in an earlier group
-  float acc[V];
+  if (!has_tail || (padded && key == pad)) return;
+  bool past = has_next && next == key && end == cnt;   // past the block
+  if (end < cnt) {
 #pragma unroll
-  for (int e = 0; e < V; ++e) acc[e] = s_piece[1][grp][gl * V + e];
-  const int last = chain(grp, key, acc);
-  if (last == cnt - 1 && has_next && next == key) {
-    store_part<float, V>(piece + a.D, at.tiny ? at.D : V, acc);
+    for (int e = 0; e < V; ++e) tail[e] += after[e];
+    past = after_open && add_waves(tail);
+  }
+  if (past) {
+    store_part<float, V>(piece + a.D, at.tiny ? at.D : V, tail);
     if (ROWS && slice == 0 && gl == 0) g.tail_run[block] = srun[end - 1];
   } else {
-    write_row<V>(a, at, out_row(end - 1), acc);
+    write_row<V>(a, at, out_row(end - 1), tail);
   }
 }
 
@@ -411,7 +456,8 @@ embedding_grad_join_kernel(EmbeddingGradArgs a, GradScratch g) {
 #pragma unroll
     for (int e = 0; e < V; ++e) acc[e] += s_sum[j][gl * V + e];
   }
-  write_row<V>(a, at, ROWS ? (int64_t)g.tail_run[b] : (int64_t)key, acc);
+  const int64_t row = ROWS ? (int64_t)g.tail_run[b] : (int64_t)key;
+  if (row < (ROWS ? a.n : a.R)) write_row<V>(a, at, row, acc);   // always, when the numbering is consistent
 }
 
 __global__ void no_rows_kernel(int64_t* __restrict__ num_unique) { *num_unique = 0; }
