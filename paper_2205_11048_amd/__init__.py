@@ -146,13 +146,18 @@ def _check(status: int):
 
 
 def _ptr(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
+
+
+# The current stream's handle as a number: 0.3 us, where making the stream
+# object first takes 2.7, a third of a small call's time on the host.
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _stream(stream):
     if stream is None:
-        stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
+        return _raw_stream(torch.cuda.current_device())
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
 def _need(t, dtype, name, numel=None):
@@ -542,18 +547,19 @@ def _matrix(t, name, n=None, D=None):
     """Checks a matrix on the GPU whose rows' elements are adjacent; returns its
     type and row stride.  With ``n`` and ``D``: at least n rows of D columns."""
     kind = _DTYPES.get(t.dtype)
-    if kind is None or not t.is_cuda or t.dim() != 2:
+    shape = t.shape
+    if kind is None or not t.is_cuda or len(shape) != 2:
         raise GBAError(f"{name}: expected a float32, bfloat16 or float16 matrix on the GPU")
-    rows, columns = t.shape
-    step, inner = t.stride()
+    rows, columns = shape
     if n is not None and (rows < n or columns != D):
-        raise GBAError(f"{name}: expected [{n}, {D}], got {list(t.shape)}")
-    if columns > 1 and inner != 1:
+        raise GBAError(f"{name}: expected [{n}, {D}], got {list(shape)}")
+    step, inner = t.stride()
+    if inner != 1 and columns > 1:
         raise GBAError(f"{name}: the elements of a row must be adjacent")
-    if rows <= 1:
-        step = max(step, columns)
     if step < columns:
-        raise GBAError(f"{name}: rows overlap")
+        if rows > 1:
+            raise GBAError(f"{name}: rows overlap")
+        step = columns
     return kind, step
 
 

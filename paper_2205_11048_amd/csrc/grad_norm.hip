@@ -86,15 +86,53 @@ __device__ __forceinline__ double block_sum(double x, double* s_wave) {
   return s;
 }
 
+// A chunk as a block holds it: 16-byte units, unit k * kNormBlock + t with
+// thread t, all asked for at once; what is left of a chunk that is not whole
+// units (fewer than eight elements) is one element a thread.
+typedef VecOf<uint16_t, 8>::type unit_t;
+constexpr int kUnits = kChunk * 4 / 16 / kNormBlock;   // of a thread, of 4-byte elements
+struct ChunkData {
+  unit_t unit[kUnits];
+  float rest;
+};
+
 template <typename T>
-__device__ __forceinline__ double chunk_squares(const T* __restrict__ g, int count) {
+__device__ __forceinline__ void load_chunk(const TensorChunk& c, int count, ChunkData& d) {
   constexpr int V = kVec<T>;
-  double s = 0.0;
-  for (int i = threadIdx.x * V; i < count; i += kNormBlock * V) {
-    float v[V];
-    load_part<T, V>(g + i, count - i, v);
+  const T* g = static_cast<const T*>(c.grad);
+  const int units = count / V;
 #pragma unroll
-    for (int e = 0; e < V; ++e) s = __builtin_fma((double)v[e], (double)v[e], s);
+  for (int k = 0; k < kChunk / V / kNormBlock; ++k) {
+    const int u = k * kNormBlock + threadIdx.x;
+    d.unit[k] = u < units ? *reinterpret_cast<const unit_t*>(g + u * V) : unit_t{};
+  }
+  const int left = units * V + threadIdx.x;
+  d.rest = left < count ? (float)g[left] : 0.0f;
+}
+__device__ __forceinline__ void load_chunk(const TensorChunk& c, int count, ChunkData& d) {
+  const int type = c.types & 255;
+  if (type == GBA_F32) load_chunk<float>(c, count, d);
+  else if (type == GBA_BF16) load_chunk<bf16_t>(c, count, d);
+  else load_chunk<f16_t>(c, count, d);
+}
+
+template <typename T>
+__device__ __forceinline__ void unpack(const unit_t& unit, float (&v)[kVec<T>]) {
+  typedef typename VecOf<T, kVec<T>>::type vec;
+  const vec x = __builtin_bit_cast(vec, unit);
+#pragma unroll
+  for (int e = 0; e < kVec<T>; ++e) v[e] = (float)x[e];
+}
+
+template <typename T>
+__device__ __forceinline__ double chunk_squares(const ChunkData& d) {
+  double s = (double)d.rest * (double)d.rest;
+#pragma unroll
+  for (int k = 0; k < kChunk / kVec<T> / kNormBlock; ++k) {
+    float v[kVec<T>];
+    unpack<T>(d.unit[k], v);
+#pragma unroll
+    for (int e = 0; e < kVec<T>; ++e) s = __builtin_fma((double)v[e], (double)v[e], s);
   }
   return s;
 }
@@ -105,11 +143,10 @@ grad_squares_kernel(const TensorChunk* __restrict__ list, int64_t chunks, double
   double s = 0.0;
   for (int64_t i = blockIdx.x; i < chunks; i += gridDim.x) {
     const TensorChunk c = list[i];
-    const int count = chunk_count(c);
     const int type = c.types & 255;
-    if (type == GBA_F32) s += chunk_squares(static_cast<const float*>(c.grad), count);
-    else if (type == GBA_BF16) s += chunk_squares(static_cast<const bf16_t*>(c.grad), count);
-    else s += chunk_squares(static_cast<const f16_t*>(c.grad), count);
+    ChunkData d;
+    load_chunk(c, chunk_count(c), d);
+    s += type == GBA_F32 ? chunk_squares<float>(d) : type == GBA_BF16 ? chunk_squares<bf16_t>(d) : chunk_squares<f16_t>(d);
   }
   s = block_sum(s, s_wave);
   if (threadIdx.x == 0) partial[blockIdx.x] = s;
@@ -134,45 +171,67 @@ grad_norm_kernel(const double* __restrict__ partial, int blocks, float* __restri
 }
 
 template <typename T, typename O>
-__device__ __forceinline__ void clip_chunk(const T* __restrict__ g, O* __restrict__ out, int count, float coef) {
+__device__ __forceinline__ void write_chunk(const ChunkData& d, O* __restrict__ out, int count, float coef) {
   constexpr int V = kVec<T>;
-  for (int i = threadIdx.x * V; i < count; i += kNormBlock * V) {
+  const int units = count / V;
+#pragma unroll
+  for (int k = 0; k < kChunk / V / kNormBlock; ++k) {
+    const int u = k * kNormBlock + threadIdx.x;
     float v[V];
-    load_part<T, V>(g + i, count - i, v);
+    unpack<T>(d.unit[k], v);
 #pragma unroll
     for (int e = 0; e < V; ++e) v[e] *= coef;
-    store_part<O, V>(out + i, count - i, v);
+    if (u < units) store_vec<O, V>(out + u * V, v);
   }
+  const int left = units * V + threadIdx.x;
+  if (left < count) out[left] = (O)(d.rest * coef);
 }
 template <typename T>
-__device__ __forceinline__ void clip_chunk(const T* __restrict__ g, void* __restrict__ out, int type, int count,
-                                           float coef) {
-  if (type == GBA_F32) clip_chunk(g, static_cast<float*>(out), count, coef);
-  else if (type == GBA_BF16) clip_chunk(g, static_cast<bf16_t*>(out), count, coef);
-  else clip_chunk(g, static_cast<f16_t*>(out), count, coef);
+__device__ __forceinline__ void write_chunk(const ChunkData& d, const TensorChunk& c, int count, float coef) {
+  const int type = c.types >> 8 & 255;
+  if (type == GBA_F32) write_chunk<T>(d, static_cast<float*>(c.out), count, coef);
+  else if (type == GBA_BF16) write_chunk<T>(d, static_cast<bf16_t*>(c.out), count, coef);
+  else write_chunk<T>(d, static_cast<f16_t*>(c.out), count, coef);
 }
 
+// The chunks are taken from the last to the first: those that the sum read
+// last are still in the caches.  A block asks for its first chunk before it
+// adds up the partial sums.
 __global__ void __launch_bounds__(kNormBlock)
 clip_kernel(const TensorChunk* __restrict__ list, int64_t chunks, const double* __restrict__ partial, int blocks,
             double max_norm, float* __restrict__ norm, float* __restrict__ coef_out, int32_t* err) {
   __shared__ double s_wave[kNormWaves];
-  const double n = sqrt(total_squares(partial, blocks, s_wave));
-  const bool finite = isfinite(n);
-  const float coef = !finite ? 0.0f : n > max_norm ? (float)(max_norm / n) : 1.0f;
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
-    *norm = (float)n;
-    if (coef_out) *coef_out = coef;
-    if (!finite) raise_error(err, GBA_DERR_NONFINITE);
-  }
-  if (!finite) return;
-  for (int64_t i = blockIdx.x; i < chunks; i += gridDim.x) {
-    const TensorChunk c = list[i];
-    if (!c.out || (coef == 1.0f && c.types >> 16)) continue;   // in place and nothing to scale
-    const int count = chunk_count(c);
-    const int type = c.types & 255, out_type = c.types >> 8 & 255;
-    if (type == GBA_F32) clip_chunk(static_cast<const float*>(c.grad), c.out, out_type, count, coef);
-    else if (type == GBA_BF16) clip_chunk(static_cast<const bf16_t*>(c.grad), c.out, out_type, count, coef);
-    else clip_chunk(static_cast<const f16_t*>(c.grad), c.out, out_type, count, coef);
+  float coef = 1.0f;
+  bool known = false;
+  for (int64_t i = blockIdx.x; i < chunks || !known; i += gridDim.x) {
+    TensorChunk c{};
+    int count = 0;
+    ChunkData d;
+    if (i < chunks) {
+      c = list[chunks - 1 - i];
+      if (c.out && !(known && coef == 1.0f && c.types >> 16)) {   // (in place with nothing to scale is skipped)
+        count = chunk_count(c);
+        load_chunk(c, count, d);
+      }
+    }
+    if (!known) {
+      known = true;
+      const double n = sqrt(total_squares(partial, blocks, s_wave));
+      const bool finite = isfinite(n);
+      coef = !finite ? 0.0f : n > max_norm ? (float)(max_norm / n) : 1.0f;
+      if (blockIdx.x == 0 && threadIdx.x == 0) {
+        *norm = (float)n;
+        if (coef_out) *coef_out = coef;
+        if (!finite) raise_error(err, GBA_DERR_NONFINITE);
+      }
+      if (!finite) return;
+      if (coef == 1.0f && c.types >> 16) count = 0;
+    }
+    if (count == 0) continue;
+    const int type = c.types & 255;
+    if (type == GBA_F32) write_chunk<float>(d, c, count, coef);
+    else if (type == GBA_BF16) write_chunk<bf16_t>(d, c, count, coef);
+    else write_chunk<f16_t>(d, c, count, coef);
   }
 }
 
