@@ -3,7 +3,7 @@
 // order matters at the 1e-16 level only), chunk by chunk in a fixed order, and
 // every tensor is scaled by min(1, max_norm / norm) on its way out.
 //
-// The list of tensors is cut into chunks of kChunk elements on the host, once:
+// The list of tensors is cut into chunks of kChunkBytes on the host, once:
 // a chunk's record holds all a block needs, so a block's first load already
 // leads to its data and tensors of any sizes give even work.
 #include <algorithm>
@@ -18,8 +18,8 @@ namespace gba {
 
 constexpr int kNormBlock = 256;
 constexpr int kNormWaves = kNormBlock / kWave;
-constexpr int kChunk = 8192;           // elements of a chunk
-constexpr int64_t kNormMaxBlocks = 2048;
+constexpr int kChunkBytes = 1 << 15;   // of a chunk, as it is read
+constexpr int64_t kNormMaxBlocks = 512;   // two a compute unit: 421 us at 200 M f32 elements, 1024 447, 2048 489
 
 // One chunk of one tensor, in the device list.
 struct TensorChunk {
@@ -37,9 +37,11 @@ static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 static int64_t norm_blocks(int64_t chunks) { return std::min(chunks, kNormMaxBlocks); }
 
+static int size_of(int type) { return type == GBA_F32 ? 4 : 2; }
+
 int64_t tensor_chunks(const gba_tensor* t, int32_t T) {
   int64_t c = 0;
-  for (int32_t i = 0; i < T; ++i) c += ceil_div(t[i].n, kChunk);
+  for (int32_t i = 0; i < T; ++i) c += ceil_div(t[i].n * size_of(t[i].grad_type), kChunkBytes);
   return c;
 }
 size_t tensor_list_bytes(int64_t chunks) { return (size_t)chunks * sizeof(TensorChunk); }
@@ -47,15 +49,15 @@ size_t grad_norm_workspace_bytes(int64_t chunks) { return (size_t)(norm_blocks(c
 
 void fill_tensor_list(const gba_tensor* t, int32_t T, void* list) {
   TensorChunk* c = static_cast<TensorChunk*>(list);
-  auto size = [](int type) { return type == GBA_F32 ? 4 : 2; };
   for (int32_t i = 0; i < T; ++i) {
-    for (int64_t at = 0; at < t[i].n; at += kChunk, ++c) {
-      c->grad = static_cast<const char*>(t[i].grad) + at * size(t[i].grad_type);
-      c->out = t[i].out ? static_cast<char*>(t[i].out) + at * size(t[i].out_type) : nullptr;
+    const int64_t most = kChunkBytes / size_of(t[i].grad_type);
+    for (int64_t at = 0; at < t[i].n; at += most, ++c) {
+      c->grad = static_cast<const char*>(t[i].grad) + at * size_of(t[i].grad_type);
+      c->out = t[i].out ? static_cast<char*>(t[i].out) + at * size_of(t[i].out_type) : nullptr;
       c->rows = t[i].rows;
       c->at = at;
       c->width = t[i].rows ? t[i].width : 1;
-      c->count = (int32_t)std::min<int64_t>(kChunk, t[i].n - at);
+      c->count = (int32_t)std::min(most, t[i].n - at);
       const bool in_place = t[i].out == t[i].grad;
       c->types = t[i].grad_type | t[i].out_type << 8 | (in_place ? 1 : 0) << 16;
     }
@@ -86,55 +88,61 @@ __device__ __forceinline__ double block_sum(double x, double* s_wave) {
   return s;
 }
 
-// A chunk as a block holds it: 16-byte units, unit k * kNormBlock + t with
-// thread t, all asked for at once; what is left of a chunk that is not whole
-// units (fewer than eight elements) is one element a thread.
-typedef VecOf<uint16_t, 8>::type unit_t;
-constexpr int kUnits = kChunk * 4 / 16 / kNormBlock;   // of a thread, of 4-byte elements
+// A chunk as a block holds it, in vectors of V elements: vector k * kNormBlock
+// + t with thread t, all asked for at once; what is left of a chunk that is
+// not whole vectors is one element a thread.
+template <typename T, int V>
 struct ChunkData {
-  unit_t unit[kUnits];
-  float rest;
+  static constexpr int N = kChunkBytes / (int)sizeof(T) / V / kNormBlock;   // vectors of a thread
+  typename VecOf<T, V>::type x[N];
+  T rest;
+
+  __device__ __forceinline__ void load(const void* grad, int count) {
+    const T* g = static_cast<const T*>(grad);
+    const int whole = count / V;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int u = k * kNormBlock + threadIdx.x;
+      x[k] = u < whole ? *reinterpret_cast<const typename VecOf<T, V>::type*>(g + u * V) : typename VecOf<T, V>::type{};
+    }
+    const int left = whole * V + threadIdx.x;
+    rest = left < count ? g[left] : (T)0.0f;
+  }
+  __device__ __forceinline__ double squares() const {
+    double s = (double)(float)rest * (double)(float)rest;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const double v = (double)(float)x[k][e];
+        s = __builtin_fma(v, v, s);
+      }
+    return s;
+  }
+  // (past the caches, which then keep what is still to be read: 200 M f32 elements 421 us, 432 through them)
+  template <typename O>
+  __device__ __forceinline__ void store(void* to, int count, float coef) const {
+    O* out = static_cast<O*>(to);
+    const int whole = count / V;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int u = k * kNormBlock + threadIdx.x;
+      typename VecOf<O, V>::type y;
+#pragma unroll
+      for (int e = 0; e < V; ++e) y[e] = (O)((float)x[k][e] * coef);
+      typename VecOf<O, V>::type* p = reinterpret_cast<typename VecOf<O, V>::type*>(out + u * V);
+      if (u < whole) __builtin_nontemporal_store(y, p);
+    }
+    const int left = whole * V + threadIdx.x;
+    if (left < count) out[left] = (O)((float)rest * coef);
+  }
 };
 
 template <typename T>
-__device__ __forceinline__ void load_chunk(const TensorChunk& c, int count, ChunkData& d) {
-  constexpr int V = kVec<T>;
-  const T* g = static_cast<const T*>(c.grad);
-  const int units = count / V;
-#pragma unroll
-  for (int k = 0; k < kChunk / V / kNormBlock; ++k) {
-    const int u = k * kNormBlock + threadIdx.x;
-    d.unit[k] = u < units ? *reinterpret_cast<const unit_t*>(g + u * V) : unit_t{};
-  }
-  const int left = units * V + threadIdx.x;
-  d.rest = left < count ? (float)g[left] : 0.0f;
-}
-__device__ __forceinline__ void load_chunk(const TensorChunk& c, int count, ChunkData& d) {
-  const int type = c.types & 255;
-  if (type == GBA_F32) load_chunk<float>(c, count, d);
-  else if (type == GBA_BF16) load_chunk<bf16_t>(c, count, d);
-  else load_chunk<f16_t>(c, count, d);
-}
-
-template <typename T>
-__device__ __forceinline__ void unpack(const unit_t& unit, float (&v)[kVec<T>]) {
-  typedef typename VecOf<T, kVec<T>>::type vec;
-  const vec x = __builtin_bit_cast(vec, unit);
-#pragma unroll
-  for (int e = 0; e < kVec<T>; ++e) v[e] = (float)x[e];
-}
-
-template <typename T>
-__device__ __forceinline__ double chunk_squares(const ChunkData& d) {
-  double s = (double)d.rest * (double)d.rest;
-#pragma unroll
-  for (int k = 0; k < kChunk / kVec<T> / kNormBlock; ++k) {
-    float v[kVec<T>];
-    unpack<T>(d.unit[k], v);
-#pragma unroll
-    for (int e = 0; e < kVec<T>; ++e) s = __builtin_fma((double)v[e], (double)v[e], s);
-  }
-  return s;
+__device__ __forceinline__ double chunk_squares(const TensorChunk& c, int count) {
+  ChunkData<T, kVec<T>> d;
+  d.load(c.grad, count);
+  return d.squares();
 }
 
 __global__ void __launch_bounds__(kNormBlock)
@@ -143,10 +151,10 @@ grad_squares_kernel(const TensorChunk* __restrict__ list, int64_t chunks, double
   double s = 0.0;
   for (int64_t i = blockIdx.x; i < chunks; i += gridDim.x) {
     const TensorChunk c = list[i];
-    const int type = c.types & 255;
-    ChunkData d;
-    load_chunk(c, chunk_count(c), d);
-    s += type == GBA_F32 ? chunk_squares<float>(d) : type == GBA_BF16 ? chunk_squares<bf16_t>(d) : chunk_squares<f16_t>(d);
+    const int count = chunk_count(c), type = c.types & 255;
+    if (type == GBA_F32) s += chunk_squares<float>(c, count);
+    else if (type == GBA_BF16) s += chunk_squares<bf16_t>(c, count);
+    else s += chunk_squares<f16_t>(c, count);
   }
   s = block_sum(s, s_wave);
   if (threadIdx.x == 0) partial[blockIdx.x] = s;
@@ -170,69 +178,71 @@ grad_norm_kernel(const double* __restrict__ partial, int blocks, float* __restri
   }
 }
 
-template <typename T, typename O>
-__device__ __forceinline__ void write_chunk(const ChunkData& d, O* __restrict__ out, int count, float coef) {
-  constexpr int V = kVec<T>;
-  const int units = count / V;
-#pragma unroll
-  for (int k = 0; k < kChunk / V / kNormBlock; ++k) {
-    const int u = k * kNormBlock + threadIdx.x;
-    float v[V];
-    unpack<T>(d.unit[k], v);
-#pragma unroll
-    for (int e = 0; e < V; ++e) v[e] *= coef;
-    if (u < units) store_vec<O, V>(out + u * V, v);
+// What the coefficient is waited for: the first chunk of a block is on its way
+// when the block adds up the partial sums.
+struct Coefficient {
+  const double* partial;
+  int blocks;
+  double max_norm;
+  float* norm;
+  float* coef_out;
+  int32_t* err;
+  double* s_wave;
+  float value;
+  bool known, finite;
+  __device__ __forceinline__ void get() {
+    if (known) return;
+    known = true;
+    const double n = sqrt(total_squares(partial, blocks, s_wave));
+    finite = isfinite(n);
+    value = !finite ? 0.0f : n > max_norm ? (float)(max_norm / n) : 1.0f;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+      *norm = (float)n;
+      if (coef_out) *coef_out = value;
+      if (!finite) raise_error(err, GBA_DERR_NONFINITE);
+    }
   }
-  const int left = units * V + threadIdx.x;
-  if (left < count) out[left] = (O)(d.rest * coef);
+};
+
+// The vectors have 16 bytes in the wider of the two types, so that both the
+// loads and the stores of a wave are without gaps.
+template <typename T, typename O>
+__device__ __forceinline__ void clip_chunk(const TensorChunk& c, int count, Coefficient& f) {
+  constexpr int V = kVec<T> < kVec<O> ? kVec<T> : kVec<O>;
+  ChunkData<T, V> d;
+  d.load(c.grad, count);
+  f.get();
+  if (f.finite && !(f.value == 1.0f && c.types >> 16))   // (in place with nothing to scale)
+    d.template store<O>(c.out, count, f.value);
 }
 template <typename T>
-__device__ __forceinline__ void write_chunk(const ChunkData& d, const TensorChunk& c, int count, float coef) {
+__device__ __forceinline__ void clip_chunk(const TensorChunk& c, int count, Coefficient& f) {
   const int type = c.types >> 8 & 255;
-  if (type == GBA_F32) write_chunk<T>(d, static_cast<float*>(c.out), count, coef);
-  else if (type == GBA_BF16) write_chunk<T>(d, static_cast<bf16_t*>(c.out), count, coef);
-  else write_chunk<T>(d, static_cast<f16_t*>(c.out), count, coef);
+  if (type == GBA_F32) clip_chunk<T, float>(c, count, f);
+  else if (type == GBA_BF16) clip_chunk<T, bf16_t>(c, count, f);
+  else clip_chunk<T, f16_t>(c, count, f);
 }
 
-// The chunks are taken from the last to the first: those that the sum read
-// last are still in the caches.  A block asks for its first chunk before it
-// adds up the partial sums.
+// A block takes the chunks that the same block of the sum took (their bytes
+// are in the caches of its part of the chip, if anywhere), the last first.
 __global__ void __launch_bounds__(kNormBlock)
 clip_kernel(const TensorChunk* __restrict__ list, int64_t chunks, const double* __restrict__ partial, int blocks,
             double max_norm, float* __restrict__ norm, float* __restrict__ coef_out, int32_t* err) {
   __shared__ double s_wave[kNormWaves];
-  float coef = 1.0f;
-  bool known = false;
-  for (int64_t i = blockIdx.x; i < chunks || !known; i += gridDim.x) {
-    TensorChunk c{};
-    int count = 0;
-    ChunkData d;
-    if (i < chunks) {
-      c = list[chunks - 1 - i];
-      if (c.out && !(known && coef == 1.0f && c.types >> 16)) {   // (in place with nothing to scale is skipped)
-        count = chunk_count(c);
-        load_chunk(c, count, d);
-      }
-    }
-    if (!known) {
-      known = true;
-      const double n = sqrt(total_squares(partial, blocks, s_wave));
-      const bool finite = isfinite(n);
-      coef = !finite ? 0.0f : n > max_norm ? (float)(max_norm / n) : 1.0f;
-      if (blockIdx.x == 0 && threadIdx.x == 0) {
-        *norm = (float)n;
-        if (coef_out) *coef_out = coef;
-        if (!finite) raise_error(err, GBA_DERR_NONFINITE);
-      }
-      if (!finite) return;
-      if (coef == 1.0f && c.types >> 16) count = 0;
-    }
-    if (count == 0) continue;
-    const int type = c.types & 255;
-    if (type == GBA_F32) write_chunk<float>(d, c, count, coef);
-    else if (type == GBA_BF16) write_chunk<bf16_t>(d, c, count, coef);
-    else write_chunk<f16_t>(d, c, count, coef);
+  Coefficient f{partial, blocks, max_norm, norm, coef_out, err, s_wave, 1.0f, false, true};
+  const int64_t rounds = (chunks + gridDim.x - 1) / gridDim.x;
+  for (int64_t r = rounds - 1; r >= 0; --r) {
+    const int64_t i = r * gridDim.x + blockIdx.x;
+    if (i >= chunks) continue;
+    const TensorChunk c = list[i];
+    if (!c.out || (f.known && f.value == 1.0f && c.types >> 16)) continue;
+    const int count = chunk_count(c), type = c.types & 255;
+    if (type == GBA_F32) clip_chunk<float>(c, count, f);
+    else if (type == GBA_BF16) clip_chunk<bf16_t>(c, count, f);
+    else clip_chunk<f16_t>(c, count, f);
+    if (!f.finite) return;
   }
+  f.get();
 }
 
 static hipError_t launch_squares(const void* list, int64_t chunks, double* partial, hipStream_t stream) {
