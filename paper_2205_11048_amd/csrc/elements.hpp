@@ -39,18 +39,20 @@ __device__ __forceinline__ void load_part(const T* __restrict__ p, int count, fl
     for (int e = 0; e < V; ++e) o[e] = e < count ? (float)p[e] : 0.0f;
   }
 }
-// rounded to T once, to the nearest (ties to even)
-template <typename T, int V>
+// rounded to T once, to the nearest (ties to even); PAST: past the caches
+template <typename T, int V, bool PAST = false>
 __device__ __forceinline__ void store_vec(T* __restrict__ p, const float (&o)[V]) {
-  typename VecOf<T, V>::type v;
+  typedef typename VecOf<T, V>::type vec;
+  vec v;
 #pragma unroll
   for (int e = 0; e < V; ++e) v[e] = (T)o[e];
-  *reinterpret_cast<typename VecOf<T, V>::type*>(p) = v;
+  if constexpr (PAST) __builtin_nontemporal_store(v, reinterpret_cast<vec*>(p));
+  else *reinterpret_cast<vec*>(p) = v;
 }
-template <typename T, int V>
+template <typename T, int V, bool PAST = false>
 __device__ __forceinline__ void store_part(T* __restrict__ p, int count, const float (&o)[V]) {
   if (count >= V) {
-    store_vec<T, V>(p, o);
+    store_vec<T, V, PAST>(p, o);
   } else {
 #pragma unroll
     for (int e = 0; e < V; ++e)

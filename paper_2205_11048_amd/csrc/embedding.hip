@@ -31,32 +31,64 @@ static int lanes_for(int32_t D, int V) {
   return l;
 }
 
+// Where a thread's V columns of a row lie.  The last vector of a row is moved
+// back to end with it: its first `shift` elements are another thread's, which
+// computes and stores the same values.
+template <int V>
+struct Columns {
+  int c, shift, D;
+  bool on;       // the thread has columns
+  bool tiny;     // rows narrower than a vector: element by element
+  __device__ __forceinline__ Columns(int first, int width) : D(width) {
+    on = first < width;
+    tiny = width < V;
+    c = tiny ? 0 : (first + V > width ? width - V : first);
+    shift = tiny ? 0 : first - c;
+  }
+};
+
 // ---------------------------------------------------------------- lookup
-// A vector of V elements per thread and step.
-template <typename T, typename O, int V>
+// 2^shift threads a row and step of V columns each: 16 bytes of the output, so
+// that a wave's stores leave no gaps.  Bound by the bytes of the output and of
+// the distinct rows: 32,768 x 4096 bf16 64 us, 5.4 TB/s.  (Two or four rows a
+// thread at a time: 72 us.)  A large output is stored past the caches, PAST:
+// what reads it next then finds more of its other inputs there, and the call
+// itself takes 64 us instead of 81.  A small one is better left in them:
+// followed by a layer norm, 8192 x 4096 bf16 take 57 us and 61 past the
+// caches, 16,384 x 4096 115 and 111.
+constexpr int64_t kPastCaches = int64_t(96) << 20;   // bytes
+template <typename T, typename O, bool PAST>
 __global__ void __launch_bounds__(kEmbBlock)
-lookup_kernel(LookupArgs a) {
-  const int64_t per_row = ceil_div(a.D, V);
-  const int64_t total = a.n * per_row;
-  for (int64_t i = (int64_t)blockIdx.x * kEmbBlock + threadIdx.x; i < total; i += (int64_t)gridDim.x * kEmbBlock) {
-    const int64_t row = i / per_row;
-    const int c = (int)(i - row * per_row) * V;
-    const int64_t id = a.ids[row];
-    const bool ok = (uint64_t)id < (uint64_t)a.R;
-    float v[V] = {};
-    if (ok) load_part<T, V>(static_cast<const T*>(a.table) + id * a.table_stride + c, a.D - c, v);
-    else if (c == 0) raise_error(a.err, GBA_DERR_ID_RANGE);
+lookup_kernel(LookupArgs a, int shift) {
+  constexpr int V = kVec<O>;
+  const int per = 1 << shift, t = threadIdx.x & (per - 1);
+  const int64_t r = (int64_t)blockIdx.x * (kEmbBlock >> shift) + (threadIdx.x >> shift);
+  if (r >= a.n) return;
+  const int64_t id = a.ids[r];
+  const bool ok = (uint64_t)id < (uint64_t)a.R;
+  if (!ok && t == 0) raise_error(a.err, GBA_DERR_ID_RANGE);
+  const T* row = static_cast<const T*>(a.table) + (ok ? id : 0) * a.table_stride;
+  O* out = static_cast<O*>(a.out) + r * a.out_stride;
+  for (int first = t * V; first < a.D; first += per * V) {
+    const Columns<V> at(first, a.D);
+    const int count = at.tiny ? at.D : V;
+    float v[V];
+    load_part<T, V>(row + at.c, count, v);
 #pragma unroll
-    for (int e = 0; e < V; ++e) v[e] *= a.scale;
-    store_part<O, V>(static_cast<O*>(a.out) + row * a.out_stride + c, a.D - c, v);
+    for (int e = 0; e < V; ++e) v[e] = ok ? v[e] * a.scale : 0.0f;
+    store_part<O, V, PAST>(out + at.c, count, v);
   }
 }
 
 template <typename T, typename O>
 static hipError_t lookup_as(const LookupArgs& a, hipStream_t stream) {
-  constexpr int V = kVec<T> > kVec<O> ? kVec<T> : kVec<O>;
-  const int64_t blocks = std::min(ceil_div(a.n * ceil_div(a.D, V), kEmbBlock), kMaxGrid);
-  hipLaunchKernelGGL((lookup_kernel<T, O, V>), dim3((unsigned)blocks), dim3(kEmbBlock), 0, stream, a);
+  int shift = 0;
+  while ((1 << shift) < kEmbBlock && (kVec<O> << shift) < a.D) ++shift;
+  const dim3 grid((unsigned)ceil_div(a.n, kEmbBlock >> shift)), block(kEmbBlock);
+  if (a.n * a.D * (int64_t)sizeof(O) >= kPastCaches)
+    hipLaunchKernelGGL((lookup_kernel<T, O, true>), grid, block, 0, stream, a, shift);
+  else
+    hipLaunchKernelGGL((lookup_kernel<T, O, false>), grid, block, 0, stream, a, shift);
   return hipGetLastError();
 }
 template <typename T>
@@ -106,22 +138,6 @@ __device__ __forceinline__ int64_t wave_lower_bound(const uint32_t* __restrict__
   }
   return lo;
 }
-
-// Where a thread's V columns of a row lie.  The last vector of a row is moved
-// back to end with it: its first `shift` elements are another thread's, which
-// computes and stores the same values.
-template <int V>
-struct Columns {
-  int c, shift, D;
-  bool on;       // the thread has columns
-  bool tiny;     // rows narrower than a vector: element by element
-  __device__ __forceinline__ Columns(int first, int width) : D(width) {
-    on = first < width;
-    tiny = width < V;
-    c = tiny ? 0 : (first + V > width ? width - V : first);
-    shift = tiny ? 0 : first - c;
-  }
-};
 
 // out row `r` (scaled, rounded once), added to what is there if asked for.
 template <int V>
