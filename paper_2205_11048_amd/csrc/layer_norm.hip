@@ -26,7 +26,7 @@ constexpr int kGradVecs = 2;                 // most 16-byte vectors of a row a 
 constexpr int kRegBlock = 512;
 constexpr int kWidest = 1024;                // most threads of a row
 constexpr int64_t kRegGradBlocks = 512;      // most blocks of a gradient: two per compute unit
-constexpr int64_t kRegBlocks = 1024;         // ... of a forward call
+constexpr int64_t kRegBlocks = 2048;         // ... of a forward call
 
 static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 static inline size_t align_up(size_t x) { return (x + 255) & ~size_t(255); }
@@ -109,9 +109,11 @@ struct RowPlace {
     else if (type == GBA_BF16) load(static_cast<const bf16_t*>(p), k, o);
     else load(static_cast<const f16_t*>(p), k, o);
   }
+  // (past the caches: 20,011 x 1001 f32 forward 27 us, 32 through them; two
+  // calls in a row that share an array take the same time either way)
   __device__ __forceinline__ void store(T* __restrict__ p, int k, const float (&o)[V]) const {
     if (tiny) store_part<T, V>(p, D, o);
-    else if (k + 1 < NV || last) store_vec<T, V>(p + col[k], o);
+    else if (k + 1 < NV || last) store_vec<T, V, true>(p + col[k], o);
   }
 };
 
