@@ -166,15 +166,14 @@ __device__ __forceinline__ void write_row(const EmbeddingGradArgs& a, const Colu
 // bytes, which the memory takes fastest (100,000 x 4096 f32 217 us, 7.5 TB/s;
 // blocks of eight rows each that leave out the rows a token asked for, found
 // among the sorted IDs, 253 us, though they write 6 percent less).
-__global__ void __launch_bounds__(kEmbBlock)
-clear_table_kernel(EmbeddingGradArgs a) {
+__device__ __forceinline__ void clear_table(const EmbeddingGradArgs& a, int64_t block, int64_t blocks) {
   typedef VecOf<uint16_t, 8>::type vec;
   const int size = a.out_type == GBA_F32 ? 2 : 1;   // in units of 2 bytes
   const bool flat = a.out_stride == a.D;
   const int64_t rows = flat ? 1 : a.R, units = (flat ? a.R : 1) * a.D * size;
   const int64_t per_row = ceil_div(units, 8), total = rows * per_row;
   uint16_t* out = static_cast<uint16_t*>(a.out);
-  for (int64_t i = (int64_t)blockIdx.x * kEmbBlock + threadIdx.x; i < total; i += (int64_t)gridDim.x * kEmbBlock) {
+  for (int64_t i = block * blockDim.x + threadIdx.x; i < total; i += blocks * blockDim.x) {
     const int64_t row = flat ? 0 : i / per_row;
     const int64_t c = (i - row * per_row) * 8;
     uint16_t* p = out + row * a.out_stride * size + c;
@@ -184,6 +183,74 @@ clear_table_kernel(EmbeddingGradArgs a) {
       for (int e = 0; e < (int)(units - c); ++e) p[e] = 0;
     }
   }
+}
+__global__ void __launch_bounds__(kEmbBlock)
+clear_table_kernel(EmbeddingGradArgs a) {
+  clear_table(a, blockIdx.x, gridDim.x);
+}
+
+// The sort of a few tokens, in one launch: a token's place is the number of
+// tokens with a smaller ID, and of those before it with the same.  A block
+// places 64 tokens, a lane each; its waves share out the tokens they are
+// compared with, which come through the scalar cache.  Bound by the
+// comparisons, n^2 of them: 2000 tokens 8 us, 4000 12, 8000 16, where the
+// radix sort's two or three launches take no longer (a gradient of 2000 rows
+// 21 us and 26, of 4000 27 and 29, of 8000 33 and 31).  The blocks past those
+// clear the table, which does not wait for the sort then.
+constexpr int kRankBlock = 1024;
+constexpr int kRankWaves = kRankBlock / kWave;
+constexpr int64_t kRankMost = 4096;
+__global__ void __launch_bounds__(kRankBlock)
+rank_kernel(const int64_t* __restrict__ ids, int n, int64_t R, uint32_t* __restrict__ keys, uint32_t* __restrict__ vals,
+            int32_t* err, int rank_blocks, EmbeddingGradArgs a) {
+  __shared__ uint32_t s_count[kRankWaves][kWave];
+  if ((int)blockIdx.x >= rank_blocks) {
+    clear_table(a, (int64_t)blockIdx.x - rank_blocks, (int64_t)gridDim.x - rank_blocks);
+    return;
+  }
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
+  const int i0 = (int)blockIdx.x * kWave, i = i0 + lane;
+  // by the low words: an ID outside the table is reported, and where it is
+  // sorted does not matter
+  const int64_t id = ids[i < n ? i : n - 1];
+  const uint32_t mine = (uint32_t)id;
+  const int share = (n + kRankWaves - 1) / kRankWaves;
+  const int j0 = w * share < n ? w * share : n, j1 = j0 + share < n ? j0 + share : n;
+  const int before = i0 < j1 ? (i0 > j0 ? i0 : j0) : j1;
+  const int after = i0 + kWave < j1 ? (i0 + kWave > j0 ? i0 + kWave : j0) : j1;
+  uint32_t count = 0;
+  constexpr int U = 16;
+  int j = j0;
+  for (; j + U <= before; j += U) {   // before the block's tokens: the same ID comes first
+    uint32_t k[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) k[u] = (uint32_t)ids[j + u];
+#pragma unroll
+    for (int u = 0; u < U; ++u) count += k[u] <= mine ? 1u : 0u;
+  }
+  for (; j < before; ++j) count += (uint32_t)ids[j] <= mine ? 1u : 0u;
+  for (; j < after; ++j) {
+    const uint32_t k = (uint32_t)ids[j];
+    count += k < mine || (k == mine && j < i) ? 1u : 0u;
+  }
+  for (; j + U <= j1; j += U) {
+    uint32_t k[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) k[u] = (uint32_t)ids[j + u];
+#pragma unroll
+    for (int u = 0; u < U; ++u) count += k[u] < mine ? 1u : 0u;
+  }
+  for (; j < j1; ++j) count += (uint32_t)ids[j] < mine ? 1u : 0u;
+  s_count[w][lane] = count;
+  __syncthreads();
+  if (w != 0 || i >= n) return;
+  uint32_t place = 0;
+#pragma unroll
+  for (int k = 0; k < kRankWaves; ++k) place += s_count[k][lane];
+  const bool in = (uint64_t)id < (uint64_t)R;
+  if (!in) raise_error(err, GBA_DERR_ID_RANGE);
+  keys[place] = in ? mine : 0u;
+  vals[place] = (uint32_t)i;
 }
 
 // ROWS: one row per distinct ID (else the whole table).
@@ -227,17 +294,20 @@ embedding_grad_kernel(EmbeddingGradArgs a, GradScratch g) {
     sk[i] = key;
     sv[i] = padded && key == pad ? 0u : val;   // (a padding token's row is not needed: one that is near)
   }
+  const bool tiled = g.heads.tile_prefix != nullptr;
   if (ROWS) {
-    // run heads in the block's tile before the block
+    // run heads in the block's tile before the block, or in all of a few tokens
     constexpr int kEarlier = (int)(kRunTile / kEmbBlock);
     const int64_t tile = b0 / kRunTile;
     uint32_t earlier = 0;
+    for (int64_t t = tiled ? tile : 0; t <= tile; ++t) {
 #pragma unroll
-    for (int k = 0; k < kEarlier; ++k) {
-      const int64_t q = tile * kRunTile + k * kEmbBlock + threadIdx.x;
-      if (q < b0) earlier += (q == 0 || a.keys[q] != a.keys[q - 1]) ? 1u : 0u;
+      for (int k = 0; k < kEarlier; ++k) {
+        const int64_t q = t * kRunTile + k * kEmbBlock + threadIdx.x;
+        if (q < b0) earlier += (q == 0 || a.keys[q] != a.keys[q - 1]) ? 1u : 0u;
+      }
     }
-    run_base(g.heads, tile, s_group);
+    if (tiled) run_base(g.heads, tile, s_group);
     earlier = wave_sum(earlier);
     if (lane_id() == 0) s_scan[threadIdx.x / kWave] = earlier;
     // does the padding ID occur?  Its run is not numbered.
@@ -272,7 +342,7 @@ embedding_grad_kernel(EmbeddingGradArgs a, GradScratch g) {
   if (busy) load_batch(first, v);   // in flight while the rows are numbered
 
   if (ROWS) {
-    uint32_t base = g.heads.tile_prefix[b0 / kRunTile] + run_base_sum(s_group);
+    uint32_t base = tiled ? g.heads.tile_prefix[b0 / kRunTile] + run_base_sum(s_group) : 0u;
 #pragma unroll
     for (int k = 0; k < kEmbWaves; ++k) base += s_scan[k];
     __syncthreads();
@@ -517,7 +587,14 @@ static GradLayout grad_layout(int64_t n, int32_t D) {
   return L;
 }
 
-size_t embedding_grad_workspace_bytes(int64_t n, int32_t D) { return grad_layout(n, D).bytes; }
+// The sorted IDs' part of the workspace.
+static size_t sort_bytes(int64_t n, int64_t R) {
+  return std::max(align_up(plan_sort(n, R).bytes), 2 * align_up((size_t)std::min(n, kRankMost) * 4));
+}
+
+size_t embedding_grad_workspace_bytes(int64_t n, int32_t D, int64_t R) {
+  return sort_bytes(n, R) + grad_layout(n, D).bytes;
+}
 
 template <typename T, int LPR, bool ROWS>
 static hipError_t grad_as(const EmbeddingGradArgs& a, GradScratch g, hipStream_t stream) {
@@ -551,29 +628,48 @@ static hipError_t grad_of(const EmbeddingGradArgs& a, const GradScratch& g, hipS
   }
 }
 
-hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, void* ws, hipStream_t stream) {
+hipError_t launch_embedding_grad(const int64_t* ids, EmbeddingGradArgs a, void* ws, int32_t* err, hipStream_t stream) {
   const bool rows = a.num_unique != nullptr;
+  const bool clear = !rows && !a.accumulate;
   if (rows && a.n == 0) {
     hipLaunchKernelGGL(no_rows_kernel, dim3(1), dim3(1), 0, stream, a.num_unique);
     return hipGetLastError();
   }
-  if (!rows && !a.accumulate) {
-    const int64_t vecs = a.R * ceil_div((int64_t)a.D * (a.out_type == GBA_F32 ? 4 : 2), 16);
-    hipLaunchKernelGGL(clear_table_kernel, dim3((unsigned)std::min(ceil_div(vecs, kEmbBlock), kMaxGrid)),
-                       dim3(kEmbBlock), 0, stream, a);
-    const hipError_t e = hipGetLastError();
+  const int64_t vecs = clear ? a.R * ceil_div((int64_t)a.D * (a.out_type == GBA_F32 ? 4 : 2), 16) : 0;
+  char* base = static_cast<char*>(ws);
+  hipError_t e;
+  if (a.n > 0 && a.n <= kRankMost) {
+    uint32_t* keys = reinterpret_cast<uint32_t*>(base);
+    uint32_t* vals = reinterpret_cast<uint32_t*>(base + align_up((size_t)a.n * 4));
+    const int64_t ranks = ceil_div(a.n, kWave), clears = std::min(ceil_div(vecs, kRankBlock), kMaxGrid);
+    hipLaunchKernelGGL(rank_kernel, dim3((unsigned)(ranks + clears)), dim3(kRankBlock), 0, stream, ids, (int)a.n, a.R,
+                       keys, vals, err, (int)ranks, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    a.keys = keys;
+    a.vals = vals;
+  } else {
+    if (clear) {
+      hipLaunchKernelGGL(clear_table_kernel, dim3((unsigned)std::min(ceil_div(vecs, kEmbBlock), kMaxGrid)),
+                         dim3(kEmbBlock), 0, stream, a);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (a.n == 0) return hipSuccess;
+    e = launch_sort_ids(ids, a.n, a.R, plan_sort(a.n, a.R), ws, &a.keys, &a.vals, err, stream);
     if (e != hipSuccess) return e;
   }
-  if (a.n == 0) return hipSuccess;
   const GradLayout L = grad_layout(a.n, a.D);
-  char* base = static_cast<char*>(ws);
+  base += sort_bytes(a.n, a.R);
   GradScratch g{};
   g.pieces = reinterpret_cast<float*>(base + L.off_pieces);
   g.tail_run = reinterpret_cast<uint32_t*>(base + L.off_tail);
   if (rows) {
-    const hipError_t e = launch_run_heads(a.keys, a.n, reinterpret_cast<uint32_t*>(base + L.off_tile),
-                                          reinterpret_cast<uint32_t*>(base + L.off_group), &g.heads, stream);
-    if (e != hipSuccess) return e;
+    // (of a few tokens the blocks count the run heads before them themselves:
+    // 4000 tokens 28 us, 29 with a launch that counts for them)
+    if (a.n > kRankMost) {
+      e = launch_run_heads(a.keys, a.n, reinterpret_cast<uint32_t*>(base + L.off_tile),
+                           reinterpret_cast<uint32_t*>(base + L.off_group), &g.heads, stream);
+      if (e != hipSuccess) return e;
+    }
     if (a.grad_type == GBA_F32) return grad_of<float, true>(a, g, stream);
     if (a.grad_type == GBA_BF16) return grad_of<bf16_t, true>(a, g, stream);
     return grad_of<f16_t, true>(a, g, stream);

@@ -535,22 +535,16 @@ gba_status gba_embedding_lookup(const int64_t* ids, int64_t n, const void* table
 gba_status gba_embedding_grad_workspace_size(int64_t n, int32_t D, int64_t R, size_t* bytes) {
   if (!bytes) return GBA_ERR_NULL;
   if (n < 0 || n > kMaxN || R < 1 || R > (int64_t(1) << 32) || !columns_ok(D)) return GBA_ERR_INVALID_ARG;
-  *bytes = align_up(plan_sort(n, R).bytes) + align_up(embedding_grad_workspace_bytes(n, D));
+  *bytes = align_up(embedding_grad_workspace_bytes(n, D, R));
   return GBA_OK;
 }
 
 // The two forms of the gradient: a holds the outputs.
 static gba_status embedding_grad_call(const int64_t* ids, const void* grad, size_t workspace_bytes, void* workspace,
                                       int32_t* err, EmbeddingGradArgs& a, hipStream_t stream) {
-  const SortPlan plan = plan_sort(a.n, a.R);
-  const size_t sort_bytes = align_up(plan.bytes);
-  if (workspace_bytes < sort_bytes + align_up(embedding_grad_workspace_bytes(a.n, a.D))) return GBA_ERR_WORKSPACE;
-  char* ws = static_cast<char*>(workspace);
-  a.keys = a.vals = nullptr;
+  if (workspace_bytes < align_up(embedding_grad_workspace_bytes(a.n, a.D, a.R))) return GBA_ERR_WORKSPACE;
   a.grad = grad;
-  if (a.n > 0 && launch_sort_ids(ids, a.n, a.R, plan, ws, &a.keys, &a.vals, err, stream) != hipSuccess)
-    return GBA_ERR_HIP;
-  return from_hip(launch_embedding_grad(a, ws + sort_bytes, stream));
+  return from_hip(launch_embedding_grad(ids, a, workspace, err, stream));
 }
 
 // Checks of the arguments that the two forms share.

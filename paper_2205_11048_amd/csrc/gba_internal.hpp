@@ -218,8 +218,10 @@ struct EmbeddingGradArgs {
   int64_t out_stride;
   int32_t out_type;
 };
-size_t embedding_grad_workspace_bytes(int64_t n, int32_t D);
-hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, void* ws, hipStream_t stream);
+// (the most of any n up to this one)
+size_t embedding_grad_workspace_bytes(int64_t n, int32_t D, int64_t R);
+// Sorts the IDs and adds the rows up; a.keys and a.vals are set here.
+hipError_t launch_embedding_grad(const int64_t* ids, EmbeddingGradArgs a, void* ws, int32_t* err, hipStream_t stream);
 
 // ---- layer norm and its gradient
 struct LayerNormArgs {
