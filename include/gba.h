@@ -469,14 +469,16 @@ gba_status gba_hash_rehash(const int64_t* old_slot_ids, const int32_t* old_slot_
 
 /*
  * Embedding lookup with scaling: out[i][c] = scale * table[ids[i]][c].
- *   ids     [n] int64.
+ *   ids     [n] integers of id_bytes bytes: 8 (int64), or 4 (int32), as the
+ *           inverse map of gba_pull_rows, with the pulled rows for a table.
  *   table   [R][D] of table_type, out [n][D] of out_type.
  *   err     GBA_DERR_ID_RANGE for an ID outside [0, R) (its output row is 0).
  * Limits: 0 <= n < 2^31, 1 <= R <= 2^32, 1 <= D <= 2^20.
  */
-gba_status gba_embedding_lookup(const int64_t* ids, int64_t n, const void* table, gba_dtype table_type,
-                                int64_t table_stride, int64_t R, int32_t D, float scale, void* out,
-                                gba_dtype out_type, int64_t out_stride, int32_t* err, hipStream_t stream);
+gba_status gba_embedding_lookup(const void* ids, int32_t id_bytes, int64_t n, const void* table,
+                                gba_dtype table_type, int64_t table_stride, int64_t R, int32_t D, float scale,
+                                void* out, gba_dtype out_type, int64_t out_stride, int32_t* err,
+                                hipStream_t stream);
 
 /*
  * The lookup's gradient, by sorted tokens: for each row r of the table

@@ -101,7 +101,7 @@ _SIGNATURES = {
     "gba_apply_adagrad": ([_P, _P, _P, _P, _P, _P, _I64, _I32, _I64, _F64, _F64, _P, _P], _I32),
     "gba_apply_adam": ([_P, _P, _P, _P, _P, _P, _P, _I64, _I32, _I64, _F64, _F64, _F64, _F64, _I64,
                         _P, _P], _I32),
-    "gba_embedding_lookup": ([_P, _I64, _P, _I32, _I64, _I64, _I32, _F32, _P, _I32, _I64, _P, _P], _I32),
+    "gba_embedding_lookup": ([_P, _I32, _I64, _P, _I32, _I64, _I64, _I32, _F32, _P, _I32, _I64, _P, _P], _I32),
     "gba_embedding_grad_workspace_size": ([_I64, _I32, _I64, ctypes.POINTER(_SIZE)], _I32),
     "gba_embedding_grad_rows": ([_P, _I64, _P, _I32, _I64, _I32, _I64, _F32, _I64, _P, _P, _I64, _P, _P, _SIZE, _P, _P],
                                 _I32),
@@ -572,15 +572,17 @@ def _vector(t, name, D):
 
 def gba_embedding_lookup(ids, table, out, scale=1.0, err=None, stream=None):
     """out[i] = scale * table[ids[i]], for float32, bfloat16 or float16 matrices
-    with any row stride; ``table`` and ``out`` may differ in type."""
+    with any row stride; ``table`` and ``out`` may differ in type.  ``ids``: int64,
+    or int32 as the inverse map of gba_pull_rows."""
     n = ids.numel()
-    _need(ids, torch.int64, "ids")
+    short = ids.dtype == torch.int32
+    _need(ids, torch.int32 if short else torch.int64, "ids")
     _need(err, torch.int32, "err", 1)
     kind, step = _matrix(table, "table")
     R, D = table.shape
     out_kind, out_step = _matrix(out, "out", n, D)
-    _check(lib().gba_embedding_lookup(_ptr(ids), n, _ptr(table), kind, step, R, D, scale, _ptr(out), out_kind, out_step,
-                                      _ptr(err), _stream(stream)))
+    _check(lib().gba_embedding_lookup(_ptr(ids), 4 if short else 8, n, _ptr(table), kind, step, R, D, scale, _ptr(out),
+                                      out_kind, out_step, _ptr(err), _stream(stream)))
 
 
 def gba_embedding_grad_workspace_size(n, D, R) -> int:

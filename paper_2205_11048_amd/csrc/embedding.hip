@@ -64,7 +64,7 @@ lookup_kernel(LookupArgs a, int shift) {
   const int per = 1 << shift, t = threadIdx.x & (per - 1);
   const int64_t r = (int64_t)blockIdx.x * (kEmbBlock >> shift) + (threadIdx.x >> shift);
   if (r >= a.n) return;
-  const int64_t id = a.ids[r];
+  const int64_t id = a.id_bytes == 8 ? static_cast<const int64_t*>(a.ids)[r] : static_cast<const int32_t*>(a.ids)[r];
   const bool ok = (uint64_t)id < (uint64_t)a.R;
   if (!ok && t == 0) raise_error(a.err, GBA_DERR_ID_RANGE);
   const T* row = static_cast<const T*>(a.table) + (ok ? id : 0) * a.table_stride;

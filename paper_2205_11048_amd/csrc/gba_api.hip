@@ -505,19 +505,22 @@ static bool element_aligned(const void* p, int32_t type) {
   return (reinterpret_cast<uintptr_t>(p) & (type == GBA_F32 ? 3u : 1u)) == 0;
 }
 
-gba_status gba_embedding_lookup(const int64_t* ids, int64_t n, const void* table, gba_dtype table_type,
-                                int64_t table_stride, int64_t R, int32_t D, float scale, void* out,
-                                gba_dtype out_type, int64_t out_stride, int32_t* err, hipStream_t stream) {
+gba_status gba_embedding_lookup(const void* ids, int32_t id_bytes, int64_t n, const void* table,
+                                gba_dtype table_type, int64_t table_stride, int64_t R, int32_t D, float scale,
+                                void* out, gba_dtype out_type, int64_t out_stride, int32_t* err,
+                                hipStream_t stream) {
+  if (id_bytes != 4 && id_bytes != 8) return GBA_ERR_INVALID_ARG;
   if (n < 0 || n > INT32_MAX || R < 1 || R > (int64_t(1) << 32) || !columns_ok(D)) return GBA_ERR_INVALID_ARG;
   if (!dtype_ok(table_type) || !dtype_ok(out_type) || !stride_ok(table_stride, D) || !stride_ok(out_stride, D))
     return GBA_ERR_INVALID_ARG;
   if (n == 0) return GBA_OK;
   if (!ids || !table || !out) return GBA_ERR_NULL;
   if (!element_aligned(table, table_type) || !element_aligned(out, out_type) ||
-      (reinterpret_cast<uintptr_t>(ids) & 7u) != 0)
+      (reinterpret_cast<uintptr_t>(ids) & (uintptr_t)(id_bytes - 1)) != 0)
     return GBA_ERR_INVALID_ARG;
   LookupArgs a;
   a.ids = ids;
+  a.id_bytes = id_bytes;
   a.table = table;
   a.out = out;
   a.n = n;

@@ -192,11 +192,11 @@ hipError_t launch_hash_rehash(const int64_t* old_ids, const int32_t* old_rows, i
 
 // ---- embedding lookup and its gradient
 struct LookupArgs {
-  const int64_t* ids;    // [n]
+  const void* ids;       // [n] integers of id_bytes bytes
   const void* table;     // [R][D]
   void* out;             // [n][D]
   int64_t n, R, table_stride, out_stride;
-  int32_t D, table_type, out_type;
+  int32_t id_bytes, D, table_type, out_type;
   float scale;
   int32_t* err;
 };

@@ -1,0 +1,87 @@
+"""A worker's embedding block, from token IDs to activations and from their
+gradients to the contribution it pushes, through the C ABI.
+
+Alg. 1 (worker) of the paper: the worker pulls the rows of its batch, computes
+a gradient and pushes it.  The block at the bottom of the worker's model is
+the embedding: the rows are pulled once per distinct ID, expanded to the
+batch's tokens and scaled, and layer-normalised.  On the way back the layer
+norm's gradient gives the gradient of the expanded rows, which is added up by
+ID; then every gradient of the model is scaled by the global norm over all of
+them, the rows included, into what a push takes: one flat float32 vector of
+dense gradients, the distinct IDs and one float32 row each.
+
+The class owns the block's outputs and scratch (allocated once, reused every
+step); the rows, the parameters and the model's other gradients are the
+caller's tensors.  All calls are enqueued on one stream; the number of distinct
+IDs stays on the GPU until ``contribution`` reads it for the message's length.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import (gba_clip_grads, gba_embedding_grad_rows, gba_embedding_grad_workspace_size, gba_embedding_lookup,
+               gba_grad_norm_workspace_size, gba_layer_norm, gba_layer_norm_grad, gba_layer_norm_grad_workspace_size,
+               gba_pull_rows, gba_pull_workspace_size, gba_tensor_list)
+
+
+class EmbeddingBlock:
+    """``n`` tokens a batch, rows of width ``D`` of a table of ``R`` rows;
+    activations of ``dtype``.  ``dense_grads``: the gradient tensors of the rest of
+    the model (float32, bfloat16 or float16, kept where they are), which are
+    clipped with the block's own and follow them in the contribution:
+    [dweight, dbias, *dense_grads]."""
+
+    def __init__(self, n: int, D: int, R: int, dense_grads=(), dtype=torch.bfloat16, scale: float = 1.0,
+                 padding_id: int = -1, eps: float = 1e-5, max_norm: float = 1.0, device="cuda"):
+        self.n, self.D, self.R = n, D, R
+        self.scale, self.padding_id, self.eps, self.max_norm = scale, padding_id, eps, max_norm
+        dev = torch.device(device)
+
+        def new(*shape, kind=torch.float32):
+            return torch.empty(shape, dtype=kind, device=dev)
+
+        self.err = torch.zeros(1, dtype=torch.int32, device=dev)
+        # forward
+        self.pulled_ids, self.inverse = new(n, kind=torch.int64), new(n, kind=torch.int32)
+        self.pulled, self.num_pulled = new(n, D), new(1, kind=torch.int64)
+        self.x, self.y = new(n, D, kind=dtype), new(n, D, kind=dtype)
+        self.mean, self.rstd = new(n), new(n)
+        # backward
+        self.dx, self.dweight, self.dbias = new(n, D, kind=dtype), new(D), new(D)
+        self.unique_ids, self.num_unique, self.rows = new(n, kind=torch.int64), new(1, kind=torch.int64), new(n, D)
+        # the contribution
+        self.grads = [self.dweight, self.dbias, *dense_grads]
+        self.P = sum(g.numel() for g in self.grads)
+        self.flat, self.norm, self.coef = new(self.P), new(1), new(1)
+        places = list(self.flat.split([g.numel() for g in self.grads]))
+        self.list = gba_tensor_list([*self.grads, self.rows], [*places, self.rows],
+                                    [*[None] * len(self.grads), self.num_unique])
+        # one scratch for all calls: they follow each other on the stream
+        size = max(gba_pull_workspace_size(n, R), gba_layer_norm_grad_workspace_size(n, D),
+                   gba_embedding_grad_workspace_size(n, D, R), gba_grad_norm_workspace_size(self.list))
+        self.workspace = new(size, kind=torch.uint8)
+
+    def forward(self, ids, table, weight, bias=None, stream=None):
+        """The batch's activations, [n, D]: layer_norm(scale * table[ids])."""
+        gba_pull_rows(ids, table, self.pulled_ids, self.inverse, self.pulled, self.num_pulled, self.workspace, self.err,
+                      stream=stream)
+        gba_embedding_lookup(self.inverse, self.pulled, self.x, self.scale, self.err, stream=stream)
+        gba_layer_norm(self.x, weight, bias, self.y, self.eps, self.mean, self.rstd, stream=stream)
+        return self.y
+
+    def backward(self, ids, dy, weight, stream=None):
+        """From the activations' gradient: dweight, dbias, and the rows' gradient by ID."""
+        gba_layer_norm_grad(dy, self.x, self.mean, self.rstd, weight, self.dx, self.dweight, self.dbias, self.workspace,
+                            stream=stream)
+        gba_embedding_grad_rows(ids, self.dx, self.R, self.unique_ids, self.rows, self.num_unique, self.workspace,
+                                self.scale, self.padding_id, self.err, stream=stream)
+
+    def clip(self, stream=None):
+        """Every gradient scaled by min(1, max_norm / norm): the dense ones into
+        ``flat``, the rows in place."""
+        gba_clip_grads(self.list, self.max_norm, self.norm, self.workspace, self.coef, self.err, stream=stream)
+
+    def contribution(self):
+        """(flat [P], IDs [U], rows [U, D]) to push; reads U, and so waits for the stream."""
+        U = int(self.num_unique.item())
+        return self.flat, self.unique_ids[:U], self.rows[:U]

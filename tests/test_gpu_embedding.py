@@ -66,6 +66,9 @@ def test_lookup(n, D, table_type, out_type, pad):
     ref = t64[ids] * float(scale)
     _close(out, ref, (1.01 * U32 + ROUND[out_type]) * np.abs(ref) * 1.01 + TINY[out_type], "lookup")
     assert int(err.item()) == 0
+    again = torch.empty_like(out)   # the same from 32-bit IDs
+    gba.gba_embedding_lookup(torch.from_numpy(ids.astype(np.int32)).to(DEV), table, again, scale=float(scale), err=err)
+    assert torch.equal(again, out) and int(err.item()) == 0
     if pad:
         assert torch.isnan(wide[:, D:]).all()
 
@@ -157,6 +160,10 @@ GRADS = [
     (700, 700, 1001, F16, BF16, "padding", 3, 7),
     (900, 64, 2048, F32, BF16, "zipf", 1, 0),
     (1500, 30, 4100, BF16, F32, "runs", -1, 0),
+    (4095, 2000, 24, F16, F32, "zipf", 0, 1),
+    (4096, 70, 40, F32, F32, "runs", -1, 0),
+    (4097, 1 << 20, 12, BF16, F32, "distinct", 17, 0),
+    (9001, 50, 130, F32, F16, "zipf", 2, 0),
 ]
 
 
@@ -289,7 +296,7 @@ def test_refusals():
     table = torch.zeros((20, 16), device=DEV)
     ws = _workspace(8, 16, 20)
     num, unique = torch.zeros(1, dtype=torch.int64, device=DEV), torch.zeros(8, dtype=torch.int64, device=DEV)
-    for bad in [lambda: gba.gba_embedding_lookup(ids.int(), table, g), lambda: gba.gba_embedding_lookup(ids, table, g[:7]),
+    for bad in [lambda: gba.gba_embedding_lookup(ids.short(), table, g), lambda: gba.gba_embedding_lookup(ids, table, g[:7]),
                 lambda: gba.gba_embedding_lookup(ids, table, g[:, :8]), lambda: gba.gba_embedding_lookup(ids, table.double(), g),
                 lambda: gba.gba_embedding_lookup(ids, table.T, g), lambda: gba.gba_embedding_lookup(ids, table[:0], g),
                 lambda: gba.gba_embedding_lookup(ids, table.cpu(), g),

@@ -27,8 +27,8 @@ def fake(i, offset=0):
     return P((1 << 20) * (i + 1) + offset)
 
 
-def _lookup(L, n=5, R=100, D=16, t=F32, ts=16, o=F32, os=16, ids=fake(0), table=fake(1), out=fake(2)):
-    return L.gba_embedding_lookup(ids, n, table, t, ts, R, D, 1.0, out, o, os, None, None)
+def _lookup(L, n=5, R=100, D=16, t=F32, ts=16, o=F32, os=16, ids=fake(0), table=fake(1), out=fake(2), width=8):
+    return L.gba_embedding_lookup(ids, width, n, table, t, ts, R, D, 1.0, out, o, os, None, None)
 
 
 @no_gpu
@@ -38,13 +38,14 @@ def test_lookup_host_path():
     assert _lookup(L, n=0, ids=None, table=None, out=None) == OK
     assert _lookup(L, n=(1 << 31) - 1, R=1 << 32, D=1 << 20, ts=1 << 20, os=1 << 40) == HIP
     assert _lookup(L, table=fake(1, 2), t=BF16) == HIP          # an element's alignment is enough
+    assert _lookup(L, ids=fake(0, 4), width=4) == HIP
 
 
 def test_lookup_refusals():
     L = gba.lib()
     for kw in (dict(n=-1), dict(n=1 << 31), dict(R=0), dict(R=(1 << 32) + 1), dict(D=0), dict(D=(1 << 20) + 1, ts=1 << 21),
                dict(ts=15), dict(os=15), dict(t=3), dict(o=-1), dict(table=fake(1, 2)), dict(out=fake(2, 1), o=BF16),
-               dict(ids=fake(0, 4))):
+               dict(ids=fake(0, 4)), dict(ids=fake(0, 2), width=4), dict(width=2), dict(width=16)):
         assert _lookup(L, **kw) == INVALID, kw
     for kw in (dict(ids=None), dict(table=None), dict(out=None)):
         assert _lookup(L, **kw) == NULL, kw
