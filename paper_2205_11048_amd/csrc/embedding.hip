@@ -20,6 +20,7 @@ namespace gba {
 constexpr int kEmbBlock = 256;
 constexpr int kEmbWaves = kEmbBlock / kWave;
 constexpr int64_t kMaxGrid = 1 << 20;
+constexpr int64_t kMostBlocks = (int64_t(1) << 24) - 1;   // of a launch: 2^32 threads
 
 __host__ __device__ static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 static inline size_t align_up(size_t x) { return (x + 255) & ~size_t(255); }
@@ -81,15 +82,23 @@ lookup_kernel(LookupArgs a, int shift) {
 }
 
 template <typename T, typename O>
-static hipError_t lookup_as(const LookupArgs& a, hipStream_t stream) {
+static hipError_t lookup_as(LookupArgs a, hipStream_t stream) {
   int shift = 0;
   while ((1 << shift) < kEmbBlock && (kVec<O> << shift) < a.D) ++shift;
-  const dim3 grid((unsigned)ceil_div(a.n, kEmbBlock >> shift)), block(kEmbBlock);
-  if (a.n * a.D * (int64_t)sizeof(O) >= kPastCaches)
-    hipLaunchKernelGGL((lookup_kernel<T, O, true>), grid, block, 0, stream, a, shift);
-  else
-    hipLaunchKernelGGL((lookup_kernel<T, O, false>), grid, block, 0, stream, a, shift);
-  return hipGetLastError();
+  const bool past = a.n * a.D * (int64_t)sizeof(O) >= kPastCaches;
+  // (wide rows of more than 2^24 tokens are more blocks than a launch takes)
+  const int64_t most = kMostBlocks * (kEmbBlock >> shift), n = a.n;
+  for (int64_t at = 0; at < n; at += most) {
+    a.n = std::min(most, n - at);
+    const dim3 grid((unsigned)ceil_div(a.n, kEmbBlock >> shift)), block(kEmbBlock);
+    if (past) hipLaunchKernelGGL((lookup_kernel<T, O, true>), grid, block, 0, stream, a, shift);
+    else hipLaunchKernelGGL((lookup_kernel<T, O, false>), grid, block, 0, stream, a, shift);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    a.ids = static_cast<const char*>(a.ids) + most * a.id_bytes;
+    a.out = static_cast<O*>(a.out) + most * a.out_stride;
+  }
+  return hipSuccess;
 }
 template <typename T>
 static hipError_t lookup_from(const LookupArgs& a, hipStream_t stream) {
@@ -108,7 +117,6 @@ hipError_t launch_embedding_lookup(const LookupArgs& a, hipStream_t stream) {
 // -------------------------------------------------------------- gradient
 constexpr int kRows = 4;             // gradient rows of a batch: twice as many loads in flight per lane group
 constexpr int kMaxPos = 1024;        // most positions of a block
-constexpr int64_t kMostBlocks = (int64_t(1) << 24) - 1;   // of a launch: 2^32 threads
 
 struct GradScratch {
   RunHeads heads;          // one row per distinct ID: where the blocks' numbering begins

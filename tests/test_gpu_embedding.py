@@ -84,6 +84,17 @@ def test_lookup_without_scaling_keeps_the_bits(dtype):
     assert torch.equal(out.view(torch.uint8), table[ids].contiguous().view(torch.uint8))
 
 
+def test_lookup_of_more_rows_than_a_launch_has_blocks():
+    """Just over 2^24 rows of more than a block's columns: 34 GB of output."""
+    n, D, R = (1 << 24) + 5, 1032, 11
+    table = torch.arange(R, device=DEV, dtype=BF16)[:, None].expand(R, D).contiguous()
+    ids = torch.arange(n, device=DEV, dtype=torch.int32) % R
+    out = torch.full((n, D), float("nan"), device=DEV, dtype=BF16)
+    gba.gba_embedding_lookup(ids, table, out)
+    for at in range(0, n, 1 << 20):
+        assert bool((out[at:at + (1 << 20)] == ids[at:at + (1 << 20), None]).all()), at
+
+
 def test_lookup_of_no_tokens_and_bad_ids():
     table = torch.ones((10, 12), device=DEV)
     out = torch.full((4, 12), 5.0, device=DEV)
