@@ -178,7 +178,16 @@ __device__ __forceinline__ void write_row(const EmbeddingGradArgs& a, const Colu
 // Clears the table, 16 bytes a thread: neighbouring blocks write neighbouring
 // bytes, which the memory takes fastest (100,000 x 4096 f32 217 us, 7.5 TB/s;
 // blocks of eight rows each that leave out the rows a token asked for, found
-// among the sorted IDs, 253 us, though they write 6 percent less).
+// among the sorted IDs, 253 us, though they write 6 percent less).  A table
+// larger than the caches is stored past them: the gradient rows read next need
+// not wait then for what is cleared to leave the caches (16,384 x 4096 bf16 into
+// this table 329 us and 299, 12,000 x 2048 into 50,000 rows 108 and 99; 8192 x
+// 2048 into 20,000 rows, 164 MB, 56 and 59).
+constexpr int64_t kClearPast = int64_t(1) << 28;   // bytes
+__host__ __device__ static inline int64_t table_bytes(const EmbeddingGradArgs& a) {
+  return a.R * a.D * (a.out_type == GBA_F32 ? 4 : 2);
+}
+template <bool PAST>
 __device__ __forceinline__ void clear_table(const EmbeddingGradArgs& a, int64_t block, int64_t blocks) {
   typedef VecOf<uint16_t, 8>::type vec;
   const int size = a.out_type == GBA_F32 ? 2 : 1;   // in units of 2 bytes
@@ -191,34 +200,56 @@ __device__ __forceinline__ void clear_table(const EmbeddingGradArgs& a, int64_t 
     const int64_t c = (i - row * per_row) * 8;
     uint16_t* p = out + row * a.out_stride * size + c;
     if (c + 8 <= units) {
-      *reinterpret_cast<vec*>(p) = vec{};
+      if constexpr (PAST) __builtin_nontemporal_store(vec{}, reinterpret_cast<vec*>(p));
+      else *reinterpret_cast<vec*>(p) = vec{};
     } else {
       for (int e = 0; e < (int)(units - c); ++e) p[e] = 0;
     }
   }
 }
+template <bool PAST>
 __global__ void __launch_bounds__(kEmbBlock)
 clear_table_kernel(EmbeddingGradArgs a) {
-  clear_table(a, blockIdx.x, gridDim.x);
+  clear_table<PAST>(a, blockIdx.x, gridDim.x);
 }
 
 // The sort of a few tokens, in one launch: a token's place is the number of
 // tokens with a smaller ID, and of those before it with the same.  A block
 // places 64 tokens, a lane each; its waves share out the tokens they are
 // compared with, which come through the scalar cache.  Bound by the
-// comparisons, n^2 of them: 2000 tokens 8 us, 4000 12, 8000 16, where the
-// radix sort's two or three launches take no longer (a gradient of 2000 rows
-// 21 us and 26, of 4000 27 and 29, of 8000 33 and 31).  The blocks past those
-// clear the table, which does not wait for the sort then.
-constexpr int kRankBlock = 1024;
-constexpr int kRankWaves = kRankBlock / kWave;
-constexpr int64_t kRankMost = 4096;
-__global__ void __launch_bounds__(kRankBlock)
+// comparisons, n^2 of them: with 16 waves 2000 tokens 8 us, 4000 12, 8000 16,
+// where the radix sort's two or three launches take no longer (a gradient of
+// 2000 rows 21 us and 26, of 4000 27 and 29, of 8000 33 and 31).
+//
+// The blocks past those clear the table, which does not wait for the sort
+// then: with a table to clear the comparisons take the time of a launch that
+// is bound by memory, and more tokens than kRankMost are sorted this way.
+// Fewer waves a block take longer to compare (16,384 tokens 55 us with 8 and
+// 100 with 4) but leave the clear more of the chip, so the block's size goes
+// by the bytes to clear per token.  Whole calls in us, the radix sort and 16, 8
+// and 4 waves: 16,384 tokens and 1638 MB 299 302 277 268, 410 MB 100 97 89 115,
+// 205 MB 68 69 71 113; 8192 and 819 MB 158 144 136 135, 205 MB 59 50 48 63, 82 MB
+// 41 34 43 61; 6000 and 205 MB 56 46 44 45, 82 MB 38 30 32 46.
+constexpr int64_t kRankMost = 4096, kRankMostClearing = 16384;
+// Threads of a block, 0: the radix sort.  (Few tokens and a table that the
+// caches hold: 509 tokens and 16 MB 14.8 us with 16 waves, 16.0 with 8; 1500 and
+// 80 MB 24.9 and 26.1 with 4.)
+static int rank_block(const EmbeddingGradArgs& a, bool clear) {
+  const int64_t bytes = clear ? table_bytes(a) : 0, per_token = bytes / a.n;
+  if (a.n > kRankMostClearing) return 0;
+  if (a.n <= kRankMost && bytes < kClearPast) return 1024;
+  if (per_token >= 40000) return 256;
+  if (per_token >= 20000) return 512;
+  return per_token >= 12000 ? 1024 : 0;
+}
+template <int BLOCK, bool PAST>
+__global__ void __launch_bounds__(BLOCK)
 rank_kernel(const int64_t* __restrict__ ids, int n, int64_t R, uint32_t* __restrict__ keys, uint32_t* __restrict__ vals,
             int32_t* err, int rank_blocks, EmbeddingGradArgs a) {
-  __shared__ uint32_t s_count[kRankWaves][kWave];
+  constexpr int WAVES = BLOCK / kWave;
+  __shared__ uint32_t s_count[WAVES][kWave];
   if ((int)blockIdx.x >= rank_blocks) {
-    clear_table(a, (int64_t)blockIdx.x - rank_blocks, (int64_t)gridDim.x - rank_blocks);
+    clear_table<PAST>(a, (int64_t)blockIdx.x - rank_blocks, (int64_t)gridDim.x - rank_blocks);
     return;
   }
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
@@ -227,7 +258,7 @@ rank_kernel(const int64_t* __restrict__ ids, int n, int64_t R, uint32_t* __restr
   // sorted does not matter
   const int64_t id = ids[i < n ? i : n - 1];
   const uint32_t mine = (uint32_t)id;
-  const int share = (n + kRankWaves - 1) / kRankWaves;
+  const int share = (n + WAVES - 1) / WAVES;
   const int j0 = w * share < n ? w * share : n, j1 = j0 + share < n ? j0 + share : n;
   const int before = i0 < j1 ? (i0 > j0 ? i0 : j0) : j1;
   const int after = i0 + kWave < j1 ? (i0 + kWave > j0 ? i0 + kWave : j0) : j1;
@@ -259,7 +290,7 @@ rank_kernel(const int64_t* __restrict__ ids, int n, int64_t R, uint32_t* __restr
   if (w != 0 || i >= n) return;
   uint32_t place = 0;
 #pragma unroll
-  for (int k = 0; k < kRankWaves; ++k) place += s_count[k][lane];
+  for (int k = 0; k < WAVES; ++k) place += s_count[k][lane];
   const bool in = (uint64_t)id < (uint64_t)R;
   if (!in) raise_error(err, GBA_DERR_ID_RANGE);
   keys[place] = in ? mine : 0u;
@@ -604,7 +635,7 @@ static GradLayout grad_layout(int64_t n, int32_t D) {
 
 // The sorted IDs' part of the workspace.
 static size_t sort_bytes(int64_t n, int64_t R) {
-  return std::max(align_up(plan_sort(n, R).bytes), 2 * align_up((size_t)std::min(n, kRankMost) * 4));
+  return std::max(align_up(plan_sort(n, R).bytes), 2 * align_up((size_t)std::min(n, kRankMostClearing) * 4));
 }
 
 size_t embedding_grad_workspace_bytes(int64_t n, int32_t D, int64_t R) {
@@ -653,19 +684,25 @@ hipError_t launch_embedding_grad(const int64_t* ids, EmbeddingGradArgs a, void* 
   const int64_t vecs = clear ? a.R * ceil_div((int64_t)a.D * (a.out_type == GBA_F32 ? 4 : 2), 16) : 0;
   char* base = static_cast<char*>(ws);
   hipError_t e;
-  if (a.n > 0 && a.n <= kRankMost) {
+  const int size = a.n > 0 ? rank_block(a, clear) : 0;
+  if (size > 0) {
     uint32_t* keys = reinterpret_cast<uint32_t*>(base);
     uint32_t* vals = reinterpret_cast<uint32_t*>(base + align_up((size_t)a.n * 4));
-    const int64_t ranks = ceil_div(a.n, kWave), clears = std::min(ceil_div(vecs, kRankBlock), kMaxGrid);
-    hipLaunchKernelGGL(rank_kernel, dim3((unsigned)(ranks + clears)), dim3(kRankBlock), 0, stream, ids, (int)a.n, a.R,
-                       keys, vals, err, (int)ranks, a);
+    const int64_t ranks = ceil_div(a.n, kWave), clears = std::min(ceil_div(vecs, size), kMaxGrid);
+    const dim3 grid((unsigned)(ranks + clears)), block((unsigned)size);
+    const bool past = clear && table_bytes(a) >= kClearPast;
+    const auto kernel = size == 256   ? (past ? rank_kernel<256, true> : rank_kernel<256, false>)
+                        : size == 512 ? (past ? rank_kernel<512, true> : rank_kernel<512, false>)
+                                      : (past ? rank_kernel<1024, true> : rank_kernel<1024, false>);
+    hipLaunchKernelGGL(kernel, grid, block, 0, stream, ids, (int)a.n, a.R, keys, vals, err, (int)ranks, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     a.keys = keys;
     a.vals = vals;
   } else {
     if (clear) {
-      hipLaunchKernelGGL(clear_table_kernel, dim3((unsigned)std::min(ceil_div(vecs, kEmbBlock), kMaxGrid)),
-                         dim3(kEmbBlock), 0, stream, a);
+      const dim3 grid((unsigned)std::min(ceil_div(vecs, kEmbBlock), kMaxGrid)), block(kEmbBlock);
+      if (table_bytes(a) >= kClearPast) hipLaunchKernelGGL(clear_table_kernel<true>, grid, block, 0, stream, a);
+      else hipLaunchKernelGGL(clear_table_kernel<false>, grid, block, 0, stream, a);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (a.n == 0) return hipSuccess;

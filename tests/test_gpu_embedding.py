@@ -235,6 +235,30 @@ def test_gradient(n, R, D, dtype, out_type, pattern, padding, pad):
     assert int(err.item()) == 0
 
 
+@pytest.mark.parametrize("n,R,D,out_type,pad", [
+    (4100, 376_000, 33, F32, 0), (4097, 640_000, 33, F32, 0), (5003, 1_600_000, 33, F32, 0), (16_384, 2_100_000, 33, F32, 3),
+    (16_384, 400_000, 1003, BF16, 0), (16_385, 400_000, 1003, BF16, 0), (3, 5000, 40, F32, 1), (777, 20_000, 250, BF16, 0),
+    (64, 1_100_000, 130, F16, 2)])
+def test_gradient_of_a_large_table(n, R, D, out_type, pad):
+    """The sorts that share their launch with the clear, by the bytes to clear per token; tables around 256 MB."""
+    rng = np.random.default_rng(n + R)
+    ids = (rng.zipf(1.1, n).astype(np.uint64) * 40_503 % R).astype(np.int64)
+    ids[::9] = 4
+    ids[1::50] = R - 1
+    grad, g64 = _matrix(rng, n, D, BF16, pad)
+    unique, place, count = np.unique(ids, return_inverse=True, return_counts=True)
+    G, mag, _ = _reference(place, g64, len(unique), -1, 1.0)
+    wide, table = _out(R, D, out_type, pad)
+    err = _err()
+    gba.gba_embedding_grad_dense(torch.from_numpy(ids).to(DEV), grad, table, _workspace(n, D, R), err=err)
+    at = torch.from_numpy(unique).to(DEV)
+    _close(table[at], G, _bound(G, mag, count, out_type), "touched rows")
+    if pad:
+        assert torch.isnan(wide[:, D:]).all()
+    table[at] = 0.0
+    assert int(table.count_nonzero()) == 0 and int(err.item()) == 0
+
+
 def test_gradient_of_no_tokens():
     ids = torch.zeros(0, dtype=torch.int64, device=DEV)
     g = torch.zeros((0, 12), device=DEV)
