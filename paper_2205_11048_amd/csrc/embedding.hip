@@ -305,7 +305,10 @@ rank_kernel(const int64_t* __restrict__ ids, int n, int64_t R, uint32_t* __restr
 // it begins in is the sum of their heads, up to the first that does not go on
 // (`open`) into its next group: a suffix scan over the wave's groups in
 // registers, then over the block's waves through LDS.
-template <typename T, int LPR, bool ROWS>
+//
+// ONE: one block per column slice for at most kOneMost tokens, which it sorts
+// itself.
+template <typename T, int LPR, bool ROWS, bool ONE>
 __global__ void __launch_bounds__(kEmbBlock)
 embedding_grad_kernel(EmbeddingGradArgs a, GradScratch g) {
   constexpr int V = kVec<T>;
@@ -330,15 +333,37 @@ embedding_grad_kernel(EmbeddingGradArgs a, GradScratch g) {
   const bool padded = a.padding >= 0 && a.padding < a.R;
   const uint32_t pad = (uint32_t)a.padding;
   // keys before the block and after it (there is none: no key is equal)
-  const bool has_prev = b0 > 0, has_next = b0 + cnt < a.n;
+  const bool has_prev = !ONE && b0 > 0, has_next = !ONE && b0 + cnt < a.n;
   const uint32_t prev = has_prev ? a.keys[b0 - 1] : 0u;
   const uint32_t next = has_next ? a.keys[b0 + cnt] : 0u;
-  for (int i = threadIdx.x; i < cnt; i += kEmbBlock) {
-    const uint32_t key = a.keys[b0 + i], val = a.vals[b0 + i];
-    sk[i] = key;
-    sv[i] = padded && key == pad ? 0u : val;   // (a padding token's row is not needed: one that is near)
+  if constexpr (ONE) {
+    // by the number of smaller IDs and of the same before it
+    const int i = threadIdx.x;
+    const int64_t id = i < cnt ? a.ids[i] : 0;
+    const bool in = (uint64_t)id < (uint64_t)a.R;
+    const uint32_t key = in ? (uint32_t)id : 0u;
+    if (!in) raise_error(a.err, GBA_DERR_ID_RANGE);
+    if (i < cnt) sv[i] = key;
+    if (i == 0) s_pad = 0u;
+    __syncthreads();
+    int place = 0;
+#pragma unroll 8
+    for (int j = 0; j < cnt; ++j) place += sv[j] < key || (sv[j] == key && j < i) ? 1 : 0;
+    __syncthreads();
+    if (i < cnt) {
+      const bool hide = padded && key == pad;
+      if (hide) s_pad = 1u;
+      sk[place] = key;
+      sv[place] = hide ? 0u : (uint32_t)i;
+    }
+  } else {
+    for (int i = threadIdx.x; i < cnt; i += kEmbBlock) {
+      const uint32_t key = a.keys[b0 + i], val = a.vals[b0 + i];
+      sk[i] = key;
+      sv[i] = padded && key == pad ? 0u : val;   // (a padding token's row is not needed: one that is near)
+    }
   }
-  const bool tiled = g.heads.tile_prefix != nullptr;
+  const bool tiled = !ONE && g.heads.tile_prefix != nullptr;
   if (ROWS) {
     // run heads in the block's tile before the block, or in all of a few tokens
     constexpr int kEarlier = (int)(kRunTile / kEmbBlock);
@@ -355,7 +380,7 @@ embedding_grad_kernel(EmbeddingGradArgs a, GradScratch g) {
     earlier = wave_sum(earlier);
     if (lane_id() == 0) s_scan[threadIdx.x / kWave] = earlier;
     // does the padding ID occur?  Its run is not numbered.
-    if (padded && threadIdx.x < kWave) {
+    if (!ONE && padded && threadIdx.x < kWave) {
       const int64_t at = wave_lower_bound(a.keys, a.n, pad);
       if (threadIdx.x == 0) s_pad = at < a.n && a.keys[at] == pad ? 1u : 0u;
     }
@@ -604,6 +629,15 @@ static int group_span(int64_t n, int lpr, int64_t slices) {
   return s;
 }
 
+// A few tokens in one launch, as far as the spans stay at kOneSpan: 4 tokens
+// of 64 floats 8.3 us and 10.9 with a launch that sorts, 32 of 2048 9.1 and 13.5
+// (60 in spans of 16 13.0 and 13.1; 200 of 64 14.3 and 13.4: the comparisons of
+// one block take longer than those of many).
+constexpr int kOneMost = kWave, kOneSpan = 8;
+static bool one_block(int64_t n, int lpr) {
+  return n <= kOneMost && n <= (int64_t)kOneSpan * kEmbBlock / lpr;
+}
+
 struct GradLayout {
   size_t off_pieces, off_tail, off_tile, off_group, bytes;
 };
@@ -647,12 +681,21 @@ static hipError_t grad_as(const EmbeddingGradArgs& a, GradScratch g, hipStream_t
   constexpr int V = kVec<T>;
   g.slices = (int)ceil_div(a.D, LPR * V);
   g.span = group_span(a.n, LPR, g.slices);
+  if (a.ids) {
+    g.span = kRows;
+    while (kEmbBlock / LPR * g.span < a.n) g.span <<= 1;
+    g.pos = kEmbBlock / LPR * g.span;
+    g.blocks = 1;
+    hipLaunchKernelGGL((embedding_grad_kernel<T, LPR, ROWS, true>), dim3((unsigned)g.slices), dim3(kEmbBlock), 0,
+                       stream, a, g);
+    return hipGetLastError();
+  }
   g.pos = kEmbBlock / LPR * g.span;
   const int64_t blocks = ceil_div(a.n, g.pos);
   g.blocks = (unsigned)blocks;
   const int64_t grid = blocks * g.slices;
   if (grid > kMostBlocks) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((embedding_grad_kernel<T, LPR, ROWS>), dim3((unsigned)grid),
+  hipLaunchKernelGGL((embedding_grad_kernel<T, LPR, ROWS, false>), dim3((unsigned)grid),
                      dim3(kEmbBlock), 0, stream, a, g);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || blocks == 1) return e;
@@ -681,11 +724,17 @@ hipError_t launch_embedding_grad(const int64_t* ids, EmbeddingGradArgs a, void* 
     hipLaunchKernelGGL(no_rows_kernel, dim3(1), dim3(1), 0, stream, a.num_unique);
     return hipGetLastError();
   }
+  const int64_t lpr = lanes_for(a.D, a.grad_type == GBA_F32 ? kVec<float> : kVec<bf16_t>);
+  const bool one = !clear && a.n > 0 && one_block(a.n, (int)lpr);
+  a.ids = one ? ids : nullptr;
+  a.err = err;
   const int64_t vecs = clear ? a.R * ceil_div((int64_t)a.D * (a.out_type == GBA_F32 ? 4 : 2), 16) : 0;
   char* base = static_cast<char*>(ws);
   hipError_t e;
-  const int size = a.n > 0 ? rank_block(a, clear) : 0;
-  if (size > 0) {
+  const int size = a.n > 0 && !one ? rank_block(a, clear) : 0;
+  if (one) {
+    a.keys = a.vals = nullptr;
+  } else if (size > 0) {
     uint32_t* keys = reinterpret_cast<uint32_t*>(base);
     uint32_t* vals = reinterpret_cast<uint32_t*>(base + align_up((size_t)a.n * 4));
     const int64_t ranks = ceil_div(a.n, kWave), clears = std::min(ceil_div(vecs, size), kMaxGrid);

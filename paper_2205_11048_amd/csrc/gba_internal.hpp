@@ -203,6 +203,8 @@ struct LookupArgs {
 hipError_t launch_embedding_lookup(const LookupArgs& a, hipStream_t stream);
 
 struct EmbeddingGradArgs {
+  const int64_t* ids;    // [n], where the adding launch sorts them itself (else null)
+  int32_t* err;
   const uint32_t* keys;  // sorted IDs [n]
   const uint32_t* vals;  // token of each sorted entry [n]
   const void* grad;      // [n][D]
@@ -220,7 +222,7 @@ struct EmbeddingGradArgs {
 };
 // (the most of any n up to this one)
 size_t embedding_grad_workspace_bytes(int64_t n, int32_t D, int64_t R);
-// Sorts the IDs and adds the rows up; a.keys and a.vals are set here.
+// Sorts the IDs and adds the rows up; a.ids, a.err, a.keys and a.vals are set here.
 hipError_t launch_embedding_grad(const int64_t* ids, EmbeddingGradArgs a, void* ws, int32_t* err, hipStream_t stream);
 
 // ---- layer norm and its gradient

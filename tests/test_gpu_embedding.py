@@ -235,6 +235,30 @@ def test_gradient(n, R, D, dtype, out_type, pattern, padding, pad):
     assert int(err.item()) == 0
 
 
+@pytest.mark.parametrize("n,R,D,dtype,out_type,pattern,padding,pad", [
+    (5, 9, 8192, BF16, F32, "zipf", -1, 0), (63, 7, 1800, BF16, F32, "zipf", 3, 2), (64, 64, 600, F16, F32, "distinct", 0, 0),
+    (64, 3000, 4096, F32, F32, "zipf", 1, 0), (32, 700, 2048, BF16, F32, "zipf", 1, 0), (33, 70, 1500, BF16, F32, "runs", 6, 0), (65, 40, 2048, BF16, BF16, "zipf", 39, 0), (127, 3, 256, BF16, F32, "same", 1, 0),
+    (128, 500, 250, BF16, F32, "runs", 2, 1), (129, 500, 256, F16, F16, "zipf", -1, 0), (255, 11, 12, F32, F32, "zipf", 10, 0),
+    (256, 300, 100, BF16, F32, "distinct", -1, 0), (256, 256, 1, F32, F32, "zipf", 0, 0), (257, 60, 31, F32, F32, "zipf", 4, 3),
+    (200, 90, 64, BF16, F32, "padding", 8, 0)])
+def test_gradient_of_few_tokens(n, R, D, dtype, out_type, pattern, padding, pad):
+    """Sizes at and around those that one launch sorts and adds up."""
+    test_gradient(n, R, D, dtype, out_type, pattern, padding, pad)
+
+
+def test_few_tokens_outside_the_table_are_reported():
+    ids = torch.tensor([1, 50, -2, 1], device=DEV)
+    g = torch.ones((4, 8), device=DEV)
+    rows, unique = torch.full((6, 8), 5.0, device=DEV), torch.full((6,), -7, dtype=torch.int64, device=DEV)
+    num, err = torch.zeros(1, dtype=torch.int64, device=DEV), _err()
+    gba.gba_embedding_grad_rows(ids, g, 50, unique, rows, num, _workspace(4, 8, 50), err=err)
+    assert int(err.item()) == gba.DERR_ID_RANGE
+    assert (rows[4:] == 5.0).all() and (unique[4:] == -7).all()
+    table, err = torch.full((50, 8), 2.0, device=DEV), _err()
+    gba.gba_embedding_grad_dense(ids, g, table, _workspace(4, 8, 50), accumulate=True, err=err)
+    assert int(err.item()) == gba.DERR_ID_RANGE
+
+
 @pytest.mark.parametrize("n,R,D,out_type,pad", [
     (4100, 376_000, 33, F32, 0), (4097, 640_000, 33, F32, 0), (5003, 1_600_000, 33, F32, 0), (16_384, 2_100_000, 33, F32, 3),
     (16_384, 400_000, 1003, BF16, 0), (16_385, 400_000, 1003, BF16, 0), (3, 5000, 40, F32, 1), (777, 20_000, 250, BF16, 0),
