@@ -151,12 +151,12 @@ def _ptr(t):
 
 # The current stream's handle as a number: 0.3 us, where making the stream
 # object first takes 2.7, a third of a small call's time on the host.
-_raw_stream = torch._C._cuda_getCurrentRawStream
+_raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
 def _stream(stream):
     if stream is None:
-        return _raw_stream(torch.cuda.current_device())
+        return _raw_stream(_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 

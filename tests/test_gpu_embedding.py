@@ -239,11 +239,25 @@ def test_gradient(n, R, D, dtype, out_type, pattern, padding, pad):
     (5, 9, 8192, BF16, F32, "zipf", -1, 0), (63, 7, 1800, BF16, F32, "zipf", 3, 2), (64, 64, 600, F16, F32, "distinct", 0, 0),
     (64, 3000, 4096, F32, F32, "zipf", 1, 0), (32, 700, 2048, BF16, F32, "zipf", 1, 0), (33, 70, 1500, BF16, F32, "runs", 6, 0), (65, 40, 2048, BF16, BF16, "zipf", 39, 0), (127, 3, 256, BF16, F32, "same", 1, 0),
     (128, 500, 250, BF16, F32, "runs", 2, 1), (129, 500, 256, F16, F16, "zipf", -1, 0), (255, 11, 12, F32, F32, "zipf", 10, 0),
-    (256, 300, 100, BF16, F32, "distinct", -1, 0), (256, 256, 1, F32, F32, "zipf", 0, 0), (257, 60, 31, F32, F32, "zipf", 4, 3),
+    (256, 300, 100, BF16, F32, "distinct", -1, 0), (256, 256, 1, F32, F32, "zipf", 0, 0), (257, 60, 31, F32, F32, "zipf", 4, 3), (191, 1 << 16, 64, BF16, F32, "distinct", -1, 0), (254, 5, 8, F16, F32, "zipf", 2, 0),
+    (130, 130, 30, F32, F32, "distinct", 129, 0),
     (200, 90, 64, BF16, F32, "padding", 8, 0)])
 def test_gradient_of_few_tokens(n, R, D, dtype, out_type, pattern, padding, pad):
     """Sizes at and around those that one launch sorts and adds up."""
     test_gradient(n, R, D, dtype, out_type, pattern, padding, pad)
+
+
+def test_few_tokens_of_the_largest_ids():
+    """Rows up to 2^32 - 1, whose number fills 32 bits."""
+    R = 1 << 32
+    ids = torch.tensor([R - 1, 5, R - 1, R - 2, 0, R - 1, 5], device=DEV).repeat(27)[:187]
+    g = torch.ones((187, 8), device=DEV)
+    unique, rows = torch.full((187,), -7, dtype=torch.int64, device=DEV), torch.empty((187, 8), device=DEV)
+    num, err = torch.zeros(1, dtype=torch.int64, device=DEV), _err()
+    gba.gba_embedding_grad_rows(ids, g, R, unique, rows, num, _workspace(187, 8, R), err=err)
+    want, count = torch.unique(ids, return_counts=True)
+    assert int(err.item()) == 0 and int(num.item()) == 4
+    assert torch.equal(unique[:4], want) and torch.equal(rows[:4], count[:, None].float().expand(4, 8))
 
 
 def test_few_tokens_outside_the_table_are_reported():
