@@ -219,29 +219,35 @@ clear_table_kernel(EmbeddingGradArgs a) {
 // places 64 tokens, a lane each; its waves share out the tokens they are
 // compared with, which come through the scalar cache.  Bound by the
 // comparisons, n^2 of them: with 16 waves 2000 tokens 8 us, 4000 12, 8000 16,
-// where the radix sort's two or three launches take no longer (a gradient of
-// 2000 rows 21 us and 26, of 4000 27 and 29, of 8000 33 and 31).
+// where the radix sort's two or three launches take 20 to 27.  Whole calls in
+// us, the radix sort and this: 2000 tokens 26 and 21, 4500 of 17-bit IDs 28.7
+// and 26.9, of 27-bit IDs 34.8 and 26.7, 6000 29.2 and 29.4, 35.4 and 29.2, 8192
+// 29.7 and 31.4, of 21-bit IDs 31.9 and 31.4, of 27-bit IDs 36.5 and 31.9.
 //
 // The blocks past those clear the table, which does not wait for the sort
 // then: with a table to clear the comparisons take the time of a launch that
-// is bound by memory, and more tokens than kRankMost are sorted this way.
+// is bound by memory, and more tokens than that are sorted this way.
 // Fewer waves a block take longer to compare (16,384 tokens 55 us with 8 and
 // 100 with 4) but leave the clear more of the chip, so the block's size goes
 // by the bytes to clear per token.  Whole calls in us, the radix sort and 16, 8
 // and 4 waves: 16,384 tokens and 1638 MB 299 302 277 268, 410 MB 100 97 89 115,
 // 205 MB 68 69 71 113; 8192 and 819 MB 158 144 136 135, 205 MB 59 50 48 63, 82 MB
 // 41 34 43 61; 6000 and 205 MB 56 46 44 45, 82 MB 38 30 32 46.
-constexpr int64_t kRankMost = 4096, kRankMostClearing = 16384;
+constexpr int64_t kRankMost = 6144, kRankMostWide = 8192, kRankMostClearing = 16384;
+constexpr int64_t kRankWideRows = int64_t(1) << 18;   // IDs of more than two 9-bit digits
+// (A table to clear makes it pay to 8192 for any IDs: into 30,000 x 32, 6000
+// tokens 23.6 and 22.6, into 200,000 x 32, 8192 29.0 and 26.5.)
 // Threads of a block, 0: the radix sort.  (Few tokens and a table that the
 // caches hold: 509 tokens and 16 MB 14.8 us with 16 waves, 16.0 with 8; 1500 and
 // 80 MB 24.9 and 26.1 with 4.)
 static int rank_block(const EmbeddingGradArgs& a, bool clear) {
   const int64_t bytes = clear ? table_bytes(a) : 0, per_token = bytes / a.n;
   if (a.n > kRankMostClearing) return 0;
-  if (a.n <= kRankMost && bytes < kClearPast) return 1024;
-  if (per_token >= 40000) return 256;
-  if (per_token >= 20000) return 512;
-  return per_token >= 12000 ? 1024 : 0;
+  if (a.n > 4096 || bytes >= kClearPast) {
+    if (per_token >= 40000) return 256;
+    if (per_token >= 20000) return 512;
+  }
+  return a.n <= (clear || a.R > kRankWideRows ? kRankMostWide : kRankMost) || per_token >= 12000 ? 1024 : 0;
 }
 template <int BLOCK, bool PAST>
 __global__ void __launch_bounds__(BLOCK)
@@ -623,6 +629,7 @@ embedding_grad_join_kernel(EmbeddingGradArgs a, GradScratch g) {
   if (row < (ROWS ? a.n : a.R)) write_row<V>(a, at, row, acc);   // always, when the numbering is consistent
 }
 
+constexpr int64_t kCountMost = 4096;   // tokens whose run heads every block counts
 __global__ void no_rows_kernel(int64_t* __restrict__ num_unique) { *num_unique = 0; }
 
 // Positions of a lane group: the most a block's kMaxPos leave, 32 at most, or
@@ -773,8 +780,9 @@ hipError_t launch_embedding_grad(const int64_t* ids, EmbeddingGradArgs a, void* 
   g.tail_run = reinterpret_cast<uint32_t*>(base + L.off_tail);
   if (rows) {
     // (of a few tokens the blocks count the run heads before them themselves:
-    // 4000 tokens 28 us, 29 with a launch that counts for them)
-    if (a.n > kRankMost) {
+    // 4500 tokens 28.2 us, 28.7 with a launch that counts for them, 6000 30.1 and
+    // 29.2)
+    if (a.n > kCountMost) {
       e = launch_run_heads(a.keys, a.n, reinterpret_cast<uint32_t*>(base + L.off_tile),
                            reinterpret_cast<uint32_t*>(base + L.off_group), &g.heads, stream);
       if (e != hipSuccess) return e;

@@ -247,6 +247,15 @@ def test_gradient_of_few_tokens(n, R, D, dtype, out_type, pattern, padding, pad)
     test_gradient(n, R, D, dtype, out_type, pattern, padding, pad)
 
 
+@pytest.mark.parametrize("n,R,D,dtype,out_type,pattern,padding,pad", [
+    (6144, 1 << 18, 9, F32, F32, "zipf", 3, 0), (6145, 1 << 18, 9, F32, F32, "runs", 3, 0),
+    (8192, (1 << 18) + 1, 20, BF16, F32, "zipf", 0, 0), (8193, (1 << 18) + 1, 20, BF16, F32, "distinct", 0, 0),
+    (8191, 300_000, 33, F16, F16, "runs", -1, 1), (7000, 400, 64, BF16, F32, "same", 2, 0)])
+def test_gradient_around_the_counting_sort(n, R, D, dtype, out_type, pattern, padding, pad):
+    """Sizes at the limits of the sort in one launch, with run heads counted by a launch of their own."""
+    test_gradient(n, R, D, dtype, out_type, pattern, padding, pad)
+
+
 def test_few_tokens_of_the_largest_ids():
     """Rows up to 2^32 - 1, whose number fills 32 bits."""
     R = 1 << 32
