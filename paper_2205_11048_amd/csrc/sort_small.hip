@@ -13,7 +13,7 @@
 //    pass are as fast or faster (small_sort_takes).
 // Bound by the launches' latency, not by bytes.  Measured: 20,480 17-bit keys
 // 18.6 us (34 with three launches per byte), 26,624 24-bit keys 27.5 (41),
-// 256,000 27-bit keys 47 (53, and four launches more between), 300,007 21-bit
+// 256,000 27-bit keys 44 (53, and four launches more between), 300,007 21-bit
 // keys 37 (42), 851,968 24-bit keys 50 (56).
 #include <algorithm>
 
@@ -506,6 +506,13 @@ static_assert(kSmallSortBelow == int64_t(4) << 20, "one pass");
 // The widest digit of any key for n keys.
 static int widest_digit(int64_t n) { return n < kDigit11Below ? 11 : (n < kDigit10Below ? 10 : 9); }
 
+// Most keys of tiles of 512 keys (half as many where a digit has 11 bits) and
+// of 1024.  A whole embedding gradient of rows of 32, us, with tiles of 2048, 1024
+// and 512 keys: 40,000 24-bit keys 45.0 40.5 37.9, 65,000 18-bit 39.1 35.8 34.1,
+// 130,000 24-bit 51.0 47.7 44.5, of 21 bits (11-bit digits) 48.2 45.9 48.3; 256,000
+// 27-bit 57.0 54.1, 400,000 18-bit 54.0 52.7, 12-bit 43.6 43.9.
+constexpr int64_t kEighthMost = int64_t(1) << 17, kQuarterMost = int64_t(1) << 18;
+
 static SmallPlan small_plan(int64_t n, int key_bits) {
   SmallPlan p{};
   p.self = n <= kSelfMost;
@@ -520,10 +527,11 @@ static SmallPlan small_plan(int64_t n, int key_bits) {
     if (p.bits[k] > widest) widest = p.bits[k];
   }
   p.bins_log2 = widest;   // the rows' width: 256 counters at least
-  // 2048-key tiles below 2^20 keys (blocks for every compute unit), 4096 above (longer runs)
-  p.items = n < kDigit10Below ? 8 : 16;
+  // blocks for every compute unit, each ranking few keys one after the other: tiles of 512 and 1024 keys while that
+  // makes no more than 256 of them, of 2048 below 2^20 keys, of 4096 above (longer runs)
+  p.items = n <= (widest > 10 ? kEighthMost / 2 : kEighthMost) ? 2 : n <= kQuarterMost ? 4 : n < kDigit10Below ? 8 : 16;
   p.tiles = ceil_div(n > 0 ? n : 1, (int64_t)kMidBlock * p.items);
-  p.chunk_shift = p.tiles <= kFourTileChunks ? 2 : 3;   // at most 128 chunk rows for a scatter block to add up
+  p.chunk_shift = p.items > 4 && p.tiles <= kFourTileChunks ? 2 : 3;   // at most 128 chunk rows for a scatter block to add up
   p.chunks = ceil_div(p.tiles, int64_t(1) << p.chunk_shift);
   return p;
 }
@@ -556,7 +564,7 @@ size_t small_sort_count_room(int64_t n) {
     return L.bytes - L.off_hist;
   };
   size_t most = counts(n);
-  for (const int64_t end : {kDigit11Below - 1, kDigit10Below - 1, kFourTileChunks * kMidBlock * 16})
+  for (const int64_t end : {kEighthMost, kQuarterMost, kDigit11Below - 1, kDigit10Below - 1, kFourTileChunks * kMidBlock * 16})
     if (end < n) most = std::max(most, counts(end));
   return most;
 }
@@ -612,7 +620,21 @@ hipError_t launch_small_sort(const int64_t* ids, int64_t n, int64_t R, int key_b
                      p.tiles, err)
     // (from 2^20 keys small_sort_takes leaves keys with a 9-bit digit only)
 #define GBA_MID_HIST_BITS(F)                             \
-  if (p.items == 16) {                                   \
+  if (p.items == 2) {                                    \
+    switch (p.bins_log2) {                               \
+      case 8: GBA_MID_HIST(F, 2, 8, 8); break;           \
+      case 9: GBA_MID_HIST(F, 2, 9, 8); break;           \
+      case 10: GBA_MID_HIST(F, 2, 10, 8); break;         \
+      default: GBA_MID_HIST(F, 2, 11, 8); break;         \
+    }                                                    \
+  } else if (p.items == 4) {                             \
+    switch (p.bins_log2) {                               \
+      case 8: GBA_MID_HIST(F, 4, 8, 8); break;           \
+      case 9: GBA_MID_HIST(F, 4, 9, 8); break;           \
+      case 10: GBA_MID_HIST(F, 4, 10, 8); break;         \
+      default: GBA_MID_HIST(F, 4, 11, 8); break;         \
+    }                                                    \
+  } else if (p.items == 16) {                            \
     if (p.chunk_shift == 2) GBA_MID_HIST(F, 16, 9, 4);   \
     else GBA_MID_HIST(F, 16, 9, 8);                      \
   } else {                                               \
@@ -635,7 +657,21 @@ hipError_t launch_small_sort(const int64_t* ids, int64_t n, int64_t R, int key_b
   hipLaunchKernelGGL((mid_scatter_kernel<F, IT, B>), grid, block, 0, stream, kin, vin, keys[out], vals[out], n, shift, \
                      mask, R, (const uint32_t*)hist, (const uint32_t*)chunk, (int)p.chunks, p.chunk_shift)
 #define GBA_MID_BITS(F)                          \
-  if (p.items == 8) {                            \
+  if (p.items == 2) {                            \
+    switch (p.bins_log2) {                       \
+      case 8: GBA_MID(F, 2, 8); break;           \
+      case 9: GBA_MID(F, 2, 9); break;           \
+      case 10: GBA_MID(F, 2, 10); break;         \
+      default: GBA_MID(F, 2, 11); break;         \
+    }                                            \
+  } else if (p.items == 4) {                     \
+    switch (p.bins_log2) {                       \
+      case 8: GBA_MID(F, 4, 8); break;           \
+      case 9: GBA_MID(F, 4, 9); break;           \
+      case 10: GBA_MID(F, 4, 10); break;         \
+      default: GBA_MID(F, 4, 11); break;         \
+    }                                            \
+  } else if (p.items == 8) {                     \
     switch (p.bins_log2) {                       \
       case 8: GBA_MID(F, 8, 8); break;           \
       case 9: GBA_MID(F, 8, 9); break;           \
