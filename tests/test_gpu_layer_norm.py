@@ -158,6 +158,7 @@ def test_backward(n, D, dtype, wtype, which, pad, shift):
 @pytest.mark.parametrize("n,D,dtype,wtype,which,pad,shift", [
     (1, 3, F32, F32, "wb", 0, 0.0), (8, 4096, BF16, F32, "wb", 0, 0.5), (9, 4096, BF16, F32, "wb", 0, 0.5),
     (16, 2048, BF16, BF16, "wb", 3, 0.0), (17, 2048, F16, F16, "w", 0, 0.0), (128, 256, BF16, F32, "wb", 0, 0.0),
+    (1, 8000, BF16, F32, "wb", 0, 0.0), (1, 8192, F32, F32, "wb", 0, 0.0), (1, 7001, F16, F16, "w", 3, 0.0),
     (129, 256, BF16, F32, "b", 0, 1.0), (511, 33, F32, F32, "wb", 1, 0.0), (2, 8000, F32, F32, "wb", 0, 0.0),
     (4, 1001, F32, BF16, "wb", 0, 0.0), (4096, 8, BF16, F32, "wb", 0, 0.0), (4097, 5, F32, F32, "wb", 0, 0.0)])
 def test_backward_of_few_rows(n, D, dtype, wtype, which, pad, shift):
