@@ -185,6 +185,11 @@ __device__ __forceinline__ void write_row(const EmbeddingGradArgs& a, const Colu
 // this table 329 us and 299, 12,000 x 2048 into 50,000 rows 108 and 99; 8192 x
 // 2048 into 20,000 rows, 164 MB, 56 and 59).
 constexpr int64_t kClearPast = int64_t(1) << 28;   // bytes
+// LDS that the clear asks for and does not use, so that a compute unit holds
+// four of its blocks: stores past the caches from fewer waves come nearer one
+// another (100,000 x 4096 f32 233 us, 252 with eight blocks, 364 with two; 2048
+// or 512 blocks that go on to further vectors 377 and 331).
+constexpr unsigned kClearLds = 40960;
 __host__ __device__ static inline int64_t table_bytes(const EmbeddingGradArgs& a) {
   return a.R * a.D * (a.out_type == GBA_F32 ? 4 : 2);
 }
@@ -739,17 +744,19 @@ hipError_t launch_embedding_grad(const int64_t* ids, EmbeddingGradArgs a, void* 
     hipLaunchKernelGGL(no_rows_kernel, dim3(1), dim3(1), 0, stream, a.num_unique);
     return hipGetLastError();
   }
-  const int64_t lpr = lanes_for(a.D, a.grad_type == GBA_F32 ? kVec<float> : kVec<bf16_t>);
-  const bool one = !clear && a.n > 0 && one_block(a.n, (int)lpr);
+  // A table to clear takes a launch before the one that adds up; sorting there
+  // costs none, so one block pays where it saves the join: 20 rows of 2048 into
+  // 1000 12.4 us and 10.3, 32 into 10,000 21.9 and 20.1.
+  const int V = a.grad_type == GBA_F32 ? kVec<float> : kVec<bf16_t>, lpr = lanes_for(a.D, V);
+  const bool joins = a.n > (int64_t)kEmbBlock / lpr * group_span(a.n, lpr, ceil_div(a.D, lpr * V));
+  const bool one = a.n > 0 && one_block(a.n, lpr) && (!clear || (joins && table_bytes(a) < kClearPast));
   a.ids = one ? ids : nullptr;
   a.err = err;
   const int64_t vecs = clear ? a.R * ceil_div((int64_t)a.D * (a.out_type == GBA_F32 ? 4 : 2), 16) : 0;
   char* base = static_cast<char*>(ws);
   hipError_t e;
   const int size = a.n > 0 && !one ? rank_block(a, clear) : 0;
-  if (one) {
-    a.keys = a.vals = nullptr;
-  } else if (size > 0) {
+  if (size > 0) {
     uint32_t* keys = reinterpret_cast<uint32_t*>(base);
     uint32_t* vals = reinterpret_cast<uint32_t*>(base + align_up((size_t)a.n * 4));
     const int64_t ranks = ceil_div(a.n, kWave), clears = std::min(ceil_div(vecs, size), kMaxGrid);
@@ -765,13 +772,15 @@ hipError_t launch_embedding_grad(const int64_t* ids, EmbeddingGradArgs a, void* 
   } else {
     if (clear) {
       const dim3 grid((unsigned)std::min(ceil_div(vecs, kEmbBlock), kMaxGrid)), block(kEmbBlock);
-      if (table_bytes(a) >= kClearPast) hipLaunchKernelGGL(clear_table_kernel<true>, grid, block, 0, stream, a);
+      if (table_bytes(a) >= kClearPast) hipLaunchKernelGGL(clear_table_kernel<true>, grid, block, kClearLds, stream, a);
       else hipLaunchKernelGGL(clear_table_kernel<false>, grid, block, 0, stream, a);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (a.n == 0) return hipSuccess;
-    e = launch_sort_ids(ids, a.n, a.R, plan_sort(a.n, a.R), ws, &a.keys, &a.vals, err, stream);
-    if (e != hipSuccess) return e;
+    if (!one) {
+      e = launch_sort_ids(ids, a.n, a.R, plan_sort(a.n, a.R), ws, &a.keys, &a.vals, err, stream);
+      if (e != hipSuccess) return e;
+    }
   }
   const GradLayout L = grad_layout(a.n, a.D);
   base += sort_bytes(a.n, a.R);

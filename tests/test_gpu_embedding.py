@@ -237,7 +237,8 @@ def test_gradient(n, R, D, dtype, out_type, pattern, padding, pad):
 
 @pytest.mark.parametrize("n,R,D,dtype,out_type,pattern,padding,pad", [
     (5, 9, 8192, BF16, F32, "zipf", -1, 0), (63, 7, 1800, BF16, F32, "zipf", 3, 2), (64, 64, 600, F16, F32, "distinct", 0, 0),
-    (64, 3000, 4096, F32, F32, "zipf", 1, 0), (32, 700, 2048, BF16, F32, "zipf", 1, 0), (33, 70, 1500, BF16, F32, "runs", 6, 0), (65, 40, 2048, BF16, BF16, "zipf", 39, 0), (127, 3, 256, BF16, F32, "same", 1, 0),
+    (64, 3000, 4096, F32, F32, "zipf", 1, 0), (32, 700, 2048, BF16, F32, "zipf", 1, 0), (33, 70, 1500, BF16, F32, "runs", 6, 0), (17, 30, 4096, F32, BF16, "zipf", 2, 1),
+    (64, 50, 200, BF16, F32, "zipf", 2, 0), (40, 50, 250, F16, F16, "same", 3, 3), (31, 400, 8200, BF16, F32, "runs", -1, 0), (65, 40, 2048, BF16, BF16, "zipf", 39, 0), (127, 3, 256, BF16, F32, "same", 1, 0),
     (128, 500, 250, BF16, F32, "runs", 2, 1), (129, 500, 256, F16, F16, "zipf", -1, 0), (255, 11, 12, F32, F32, "zipf", 10, 0),
     (256, 300, 100, BF16, F32, "distinct", -1, 0), (256, 256, 1, F32, F32, "zipf", 0, 0), (257, 60, 31, F32, F32, "zipf", 4, 3), (191, 1 << 16, 64, BF16, F32, "distinct", -1, 0), (254, 5, 8, F16, F32, "zipf", 2, 0),
     (130, 130, 30, F32, F32, "distinct", 129, 0),
