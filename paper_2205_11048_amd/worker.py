@@ -19,7 +19,7 @@ from __future__ import annotations
 
 import torch
 
-from . import (gba_clip_grads, gba_embedding_grad_rows, gba_embedding_grad_workspace_size, gba_embedding_lookup,
+from . import (GBAError, gba_clip_grads, gba_embedding_grad_rows, gba_embedding_grad_workspace_size, gba_embedding_lookup,
                gba_grad_norm_workspace_size, gba_layer_norm, gba_layer_norm_grad, gba_layer_norm_grad_workspace_size,
                gba_pull_rows, gba_pull_workspace_size, gba_tensor_list)
 
@@ -29,11 +29,15 @@ class EmbeddingBlock:
     activations of ``dtype``.  ``dense_grads``: the gradient tensors of the rest of
     the model (float32, bfloat16 or float16, kept where they are), which are
     clipped with the block's own and follow them in the contribution:
-    [dweight, dbias, *dense_grads]."""
+    [dweight, dbias, *dense_grads].  ``weight``, ``bias``: whether the layer norm has
+    them; one that it lacks has no gradient, no part in the norm and no place in
+    the contribution."""
 
     def __init__(self, n: int, D: int, R: int, dense_grads=(), dtype=torch.bfloat16, scale: float = 1.0,
-                 padding_id: int = -1, eps: float = 1e-5, max_norm: float = 1.0, device="cuda"):
+                 padding_id: int = -1, eps: float = 1e-5, max_norm: float = 1.0, device="cuda", weight: bool = True,
+                 bias: bool = True):
         self.n, self.D, self.R = n, D, R
+        self.weight, self.bias = bool(weight), bool(bias)
         self.scale, self.padding_id, self.eps, self.max_norm = scale, padding_id, eps, max_norm
         dev = torch.device(device)
 
@@ -47,10 +51,11 @@ class EmbeddingBlock:
         self.x, self.y = new(n, D, kind=dtype), new(n, D, kind=dtype)
         self.mean, self.rstd = new(n), new(n)
         # backward
-        self.dx, self.dweight, self.dbias = new(n, D, kind=dtype), new(D), new(D)
+        self.dx = new(n, D, kind=dtype)
+        self.dweight, self.dbias = new(D) if weight else None, new(D) if bias else None
         self.unique_ids, self.num_unique, self.rows = new(n, kind=torch.int64), new(1, kind=torch.int64), new(n, D)
         # the contribution
-        self.grads = [self.dweight, self.dbias, *dense_grads]
+        self.grads = [*[g for g in (self.dweight, self.dbias) if g is not None], *dense_grads]
         self.P = sum(g.numel() for g in self.grads)
         self.flat, self.norm, self.coef = new(self.P), new(1), new(1)
         places = list(self.flat.split([g.numel() for g in self.grads]))
@@ -61,16 +66,24 @@ class EmbeddingBlock:
                    gba_embedding_grad_workspace_size(n, D, R), gba_grad_norm_workspace_size(self.list))
         self.workspace = new(size, kind=torch.uint8)
 
-    def forward(self, ids, table, weight, bias=None, stream=None):
+    def _parameter(self, name, given, has):
+        # else its gradient would be missing from the norm, or be that of a parameter which is not there
+        if (given is not None) != has:
+            raise GBAError(f"{name}: the block was made {'with' if has else 'without'} one ({name}={has})")
+
+    def forward(self, ids, table, weight=None, bias=None, stream=None):
         """The batch's activations, [n, D]: layer_norm(scale * table[ids])."""
+        self._parameter("weight", weight, self.weight)
+        self._parameter("bias", bias, self.bias)
         gba_pull_rows(ids, table, self.pulled_ids, self.inverse, self.pulled, self.num_pulled, self.workspace, self.err,
                       stream=stream)
         gba_embedding_lookup(self.inverse, self.pulled, self.x, self.scale, self.err, stream=stream)
         gba_layer_norm(self.x, weight, bias, self.y, self.eps, self.mean, self.rstd, stream=stream)
         return self.y
 
-    def backward(self, ids, dy, weight, stream=None):
+    def backward(self, ids, dy, weight=None, stream=None):
         """From the activations' gradient: dweight, dbias, and the rows' gradient by ID."""
+        self._parameter("weight", weight, self.weight)
         gba_layer_norm_grad(dy, self.x, self.mean, self.rstd, weight, self.dx, self.dweight, self.dbias, self.workspace,
                             stream=stream)
         gba_embedding_grad_rows(ids, self.dx, self.R, self.unique_ids, self.rows, self.num_unique, self.workspace,

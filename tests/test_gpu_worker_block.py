@@ -1,0 +1,94 @@
+"""A worker's embedding block where a step is not the plain one: a layer norm
+that lacks a parameter, against float64.
+
+Tolerances.  The activations are float32, so what the block computes is a few
+hundred float32 roundings (u = 2^-24): sums over rows of 64 elements, over 300
+tokens of an ID and over 700 rows.  1e-5 of each output's largest magnitude
+(170 u) is above what they add up to and far below any wrong term."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2205_11048_amd as gba
+from paper_2205_11048_amd.worker import EmbeddingBlock
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+N, D, R, EPS, PAD, SCALE = 700, 64, 900, 1e-5, 7, 8.0
+
+
+def _dev(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).to(DEV)
+
+
+def _inputs(seed):
+    """IDs, the activations' gradient (its mean is not 0: dbias is large), table, weight, bias, another gradient."""
+    rng = np.random.default_rng(seed)
+    ids = (rng.zipf(1.3, N) * 31) % R
+    ids[rng.random(N) < 0.1] = PAD
+    return (ids.astype(np.int64), rng.normal(0.1, 1, (N, D)).astype(np.float32),
+            rng.normal(0, 0.05, (R, D)).astype(np.float32), (1 + 0.1 * rng.normal(size=D)).astype(np.float32),
+            (0.1 * rng.normal(size=D)).astype(np.float32), rng.normal(0, 0.3, 4097).astype(np.float32))
+
+
+def _exact(ids, dy, table, w, b, other, max_norm=1.0):
+    """(y, flat, distinct IDs, their rows, norm) in float64; w, b None: the layer norm has none."""
+    x = SCALE * table[ids].astype(np.float64)
+    m = x.mean(1, keepdims=True)
+    r = 1 / np.sqrt(((x - m) ** 2).mean(1, keepdims=True) + EPS)
+    xh = (x - m) * r
+    dy = dy.astype(np.float64)
+    h = dy if w is None else dy * w
+    y = xh * (1 if w is None else w) + (0 if b is None else b)
+    dx = r * (h - h.mean(1, keepdims=True) - xh * (h * xh).mean(1, keepdims=True))
+    G = np.zeros((R, D))
+    keep = ids != PAD
+    np.add.at(G, ids[keep], SCALE * dx[keep])
+    unique = np.unique(ids[keep])
+    dense = [*([] if w is None else [(dy * xh).sum(0)]), *([] if b is None else [dy.sum(0)]), other.astype(np.float64)]
+    dense = np.concatenate(dense)
+    norm = np.sqrt((dense ** 2).sum() + (G ** 2).sum())
+    c = min(1.0, max_norm / norm)
+    return y, dense * c, unique, G[unique] * c, norm
+
+
+def _near(got, ref, name):
+    got = got.double().cpu().numpy()
+    assert got.shape == ref.shape, name
+    assert np.abs(got - ref).max() <= 1e-5 * np.abs(ref).max(), (name, np.abs(got - ref).max(), np.abs(ref).max())
+
+
+def _block(other, **kw):
+    return EmbeddingBlock(N, D, R, [other], dtype=torch.float32, scale=SCALE, padding_id=PAD, eps=EPS, **kw)
+
+
+@pytest.mark.parametrize("has_weight,has_bias", [(True, True), (True, False), (False, True), (False, False)])
+def test_a_layer_norm_without_parameters(has_weight, has_bias):
+    """A parameter that is not there has no part in the norm and no place in the contribution."""
+    ids, dy, table, w, b, other = _inputs(1)
+    w, b = w if has_weight else None, b if has_bias else None
+    block = _block(_dev(other), weight=has_weight, bias=has_bias)
+    wd, bd = _dev(w) if has_weight else None, _dev(b) if has_bias else None
+    y = block.forward(_dev(ids), _dev(table), wd, bd)
+    block.backward(_dev(ids), _dev(dy), wd)
+    block.clip()
+    flat, unique, rows = block.contribution()
+    ry, rflat, runique, rrows, rnorm = _exact(ids, dy, table, w, b, other)
+    assert np.array_equal(unique.cpu().numpy(), runique) and block.P == rflat.size
+    assert abs(float(block.norm) - rnorm) <= 1e-5 * rnorm
+    _near(y, ry, "y")
+    _near(flat, rflat, "flat")
+    _near(rows, rrows, "rows")
+
+
+def test_parameters_have_to_be_the_blocks():
+    ids, dy, table, w, b, other = (_dev(t) for t in _inputs(1))
+    for has_weight, has_bias in [(True, True), (True, False), (False, True), (False, False)]:
+        block = _block(other, weight=has_weight, bias=has_bias)
+        for gw, gb in [(w, b), (w, None), (None, b), (None, None)]:
+            if ((gw is not None), (gb is not None)) == (has_weight, has_bias):
+                continue
+            with pytest.raises(gba.GBAError):
+                block.forward(ids, table, gw, gb)
+        with pytest.raises(gba.GBAError):
+            block.backward(ids, dy, None if has_weight else w)
