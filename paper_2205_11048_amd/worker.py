@@ -13,15 +13,26 @@ dense gradients, the distinct IDs and one float32 row each.
 The class owns the block's outputs and scratch (allocated once, reused every
 step); the rows, the parameters and the model's other gradients are the
 caller's tensors.  All calls are enqueued on one stream; the number of distinct
-IDs stays on the GPU until ``contribution`` reads it for the message's length.
+IDs stays on the GPU until ``contribution`` reads it for the message's length,
+and with it the error word: a step that went wrong has nothing to push.
 """
 from __future__ import annotations
 
 import torch
 
-from . import (GBAError, gba_clip_grads, gba_embedding_grad_rows, gba_embedding_grad_workspace_size, gba_embedding_lookup,
+from . import (DERR_NONFINITE, GBAError, gba_clip_grads, gba_embedding_grad_rows, gba_embedding_grad_workspace_size, gba_embedding_lookup,
                gba_grad_norm_workspace_size, gba_layer_norm, gba_layer_norm_grad, gba_layer_norm_grad_workspace_size,
                gba_pull_rows, gba_pull_workspace_size, gba_tensor_list)
+
+
+class StepError(GBAError):
+    """A step without a contribution.  ``bits``: the error word, DERR_ID_RANGE (an
+    ID outside the table) or DERR_NONFINITE (a norm that is infinite or not a
+    number, with which no gradient was written)."""
+
+    def __init__(self, bits: int):
+        super().__init__(f"the step has no contribution to push: error word {bits}")
+        self.bits = bits
 
 
 class EmbeddingBlock:
@@ -95,6 +106,17 @@ class EmbeddingBlock:
         gba_clip_grads(self.list, self.max_norm, self.norm, self.workspace, self.coef, self.err, stream=stream)
 
     def contribution(self):
-        """(flat [P], IDs [U], rows [U, D]) to push; reads U, and so waits for the stream."""
-        U = int(self.num_unique.item())
+        """(flat [P], IDs [U], rows [U, D]) to push; reads U, and so waits for the stream.
+        Raises StepError where the step's IDs or norm were bad, and clears ``err``
+        then: what the buffers hold is not this step's, and the next step begins
+        without it."""
+        U, bits = int(self.num_unique.item()), int(self.err.item())
+        if bits:
+            self.err.zero_()
+            torch.cuda.current_stream(self.err.device).synchronize()   # before a step on any stream
+            # (left by an earlier step whose contribution was not asked for: this one's norm is finite)
+            if float(self.coef.item()) != 0.0:
+                bits &= ~DERR_NONFINITE
+        if bits:
+            raise StepError(bits)
         return self.flat, self.unique_ids[:U], self.rows[:U]

@@ -1,5 +1,5 @@
 """A worker's embedding block where a step is not the plain one: a layer norm
-that lacks a parameter, against float64.
+that lacks a parameter, a step whose norm or IDs are bad; against float64.
 
 Tolerances.  The activations are float32, so what the block computes is a few
 hundred float32 roundings (u = 2^-24): sums over rows of 64 elements, over 300
@@ -10,7 +10,7 @@ import pytest
 import torch
 
 import paper_2205_11048_amd as gba
-from paper_2205_11048_amd.worker import EmbeddingBlock
+from paper_2205_11048_amd.worker import EmbeddingBlock, StepError
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -92,3 +92,71 @@ def test_parameters_have_to_be_the_blocks():
                 block.forward(ids, table, gw, gb)
         with pytest.raises(gba.GBAError):
             block.backward(ids, dy, None if has_weight else w)
+
+
+def _step(block, ids, dy, table, w, b, stream=None):
+    block.forward(ids, table, w, b, stream=stream)
+    block.backward(ids, dy, w, stream=stream)
+    block.clip(stream=stream)
+
+
+def _check(block, inputs, max_norm=1.0):
+    flat, unique, rows = block.contribution()
+    _, rflat, runique, rrows, rnorm = _exact(*inputs, max_norm=max_norm)
+    assert np.array_equal(unique.cpu().numpy(), runique)
+    assert abs(float(block.norm) - rnorm) <= 1e-5 * rnorm
+    _near(flat, rflat, "flat")
+    _near(rows, rrows, "rows")
+
+
+@pytest.mark.parametrize("first", [True, False])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_step_that_is_not_finite_has_no_contribution(bad, first):
+    """A gradient that is not finite after a good step, or in the first one; the steps after it are as if it had not been."""
+    one, two, three = _inputs(1), _inputs(2), _inputs(3)
+    other = _dev(one[-1])
+    block = _block(other)
+    if not first:
+        _step(block, *(_dev(t) for t in one[:5]))
+        _check(block, one)
+    other.copy_(_dev(two[-1]))
+    dy = _dev(two[1])
+    dy[300, 5] = bad
+    _step(block, _dev(two[0]), dy, *(_dev(t) for t in two[2:5]))
+    with pytest.raises(StepError) as e:
+        block.contribution()
+    assert e.value.bits == gba.DERR_NONFINITE
+    other.copy_(_dev(three[-1]))
+    _step(block, *(_dev(t) for t in three[:5]))
+    _check(block, three)
+    assert int(block.err.item()) == 0
+
+
+def test_a_bad_step_that_was_not_asked_for():
+    """The caller looks at the norm itself and goes on."""
+    one, two = _inputs(4), _inputs(5)
+    other = _dev(one[-1])
+    block = _block(other)
+    dy = _dev(one[1])
+    dy[3, 4] = float("nan")
+    _step(block, _dev(one[0]), dy, *(_dev(t) for t in one[2:5]))
+    other.copy_(_dev(two[-1]))
+    _step(block, *(_dev(t) for t in two[:5]))
+    _check(block, two)
+    assert int(block.err.item()) == 0
+
+
+@pytest.mark.parametrize("bad", [R, -1, 1 << 40])
+def test_an_id_outside_the_table_has_no_contribution(bad):
+    one, two = _inputs(6), _inputs(7)
+    other = _dev(one[-1])
+    block = _block(other)
+    ids = _dev(one[0])
+    ids[11] = bad
+    _step(block, ids, *(_dev(t) for t in one[1:5]))
+    with pytest.raises(StepError) as e:
+        block.contribution()
+    assert e.value.bits & gba.DERR_ID_RANGE
+    other.copy_(_dev(two[-1]))
+    _step(block, *(_dev(t) for t in two[:5]))
+    _check(block, two)
