@@ -12,8 +12,9 @@ dense gradients, the distinct IDs and one float32 row each.
 
 The class owns the block's outputs and scratch (allocated once, reused every
 step); the rows, the parameters and the model's other gradients are the
-caller's tensors.  All calls are enqueued on one stream; the number of distinct
-IDs stays on the GPU until ``contribution`` reads it for the message's length,
+caller's tensors.  All calls of a step are enqueued on one stream, the current one
+or ``stream`` (which the caller orders behind what makes the tensors on another);
+the number of distinct IDs stays on the GPU until ``contribution`` reads it for the message's length,
 and with it the error word: a step that went wrong has nothing to push.
 """
 from __future__ import annotations
@@ -76,6 +77,7 @@ class EmbeddingBlock:
         size = max(gba_pull_workspace_size(n, R), gba_layer_norm_grad_workspace_size(n, D),
                    gba_embedding_grad_workspace_size(n, D, R), gba_grad_norm_workspace_size(self.list))
         self.workspace = new(size, kind=torch.uint8)
+        self._stream = None   # of the last step
 
     def _parameter(self, name, given, has):
         # else its gradient would be missing from the norm, or be that of a parameter which is not there
@@ -103,13 +105,16 @@ class EmbeddingBlock:
     def clip(self, stream=None):
         """Every gradient scaled by min(1, max_norm / norm): the dense ones into
         ``flat``, the rows in place."""
+        self._stream = torch.cuda.current_stream(self.err.device) if stream is None else stream
         gba_clip_grads(self.list, self.max_norm, self.norm, self.workspace, self.coef, self.err, stream=stream)
 
-    def contribution(self):
-        """(flat [P], IDs [U], rows [U, D]) to push; reads U, and so waits for the stream.
-        Raises StepError where the step's IDs or norm were bad, and clears ``err``
+    def contribution(self, stream=None):
+        """(flat [P], IDs [U], rows [U, D]) to push; reads U, and so waits for the stream
+        of the last ``clip``, or for ``stream`` (a graph replayed on another than it was
+        recorded on).  Raises StepError where the step's IDs or norm were bad, and clears ``err``
         then: what the buffers hold is not this step's, and the next step begins
         without it."""
+        self._wait(self._stream if stream is None else stream)
         U, bits = int(self.num_unique.item()), int(self.err.item())
         if bits:
             self.err.zero_()
@@ -120,3 +125,10 @@ class EmbeddingBlock:
         if bits:
             raise StepError(bits)
         return self.flat, self.unique_ids[:U], self.rows[:U]
+
+    def _wait(self, stream):
+        if stream is None:
+            raise GBAError("contribution: no step has been clipped")
+        if not hasattr(stream, "synchronize"):
+            stream = torch.cuda.ExternalStream(int(stream), device=self.err.device)
+        stream.synchronize()

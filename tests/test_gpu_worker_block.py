@@ -1,5 +1,6 @@
 """A worker's embedding block where a step is not the plain one: a layer norm
-that lacks a parameter, a step whose norm or IDs are bad; against float64.
+that lacks a parameter, a step whose norm or IDs are bad, a step on
+another stream; against float64.
 
 Tolerances.  The activations are float32, so what the block computes is a few
 hundred float32 roundings (u = 2^-24): sums over rows of 64 elements, over 300
@@ -160,3 +161,52 @@ def test_an_id_outside_the_table_has_no_contribution(bad):
     other.copy_(_dev(two[-1]))
     _step(block, *(_dev(t) for t in two[:5]))
     _check(block, two)
+
+
+@pytest.mark.parametrize("how", ["argument", "handle", "current"])
+def test_a_step_on_another_stream(how):
+    """The contribution is the step's that was clipped, wherever it ran: the side stream has work before it."""
+    one = _inputs(8)
+    tensors = [_dev(t) for t in one]
+    block = _block(tensors[-1])
+    block.num_unique.fill_(3)
+    busy = torch.ones((4096, 4096), device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            busy = busy @ busy * 1e-4
+        if how == "current":
+            _step(block, *tensors[:5])
+    if how != "current":
+        _step(block, *tensors[:5], stream=side if how == "argument" else side.cuda_stream)
+    _check(block, one)
+
+
+def test_a_replay_on_another_stream():
+    """A recorded step replayed on a stream that the block has not seen, which the caller names."""
+    one, two = _inputs(9), _inputs(10)
+    tensors = [_dev(t) for t in one]
+    block = _block(tensors[-1])
+    _step(block, *tensors[:5])
+    _check(block, one)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        _step(block, *tensors[:5])
+    for inputs in (two, one, two):
+        for t, x in zip(tensors, inputs):
+            t.copy_(_dev(x))
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            graph.replay()
+        flat, unique, rows = block.contribution(stream=side)
+        _, rflat, runique, rrows, _ = _exact(*inputs)
+        assert np.array_equal(unique.cpu().numpy(), runique)
+        _near(flat, rflat, "flat")
+        _near(rows, rrows, "rows")
+
+
+def test_no_contribution_before_a_step():
+    with pytest.raises(gba.GBAError):
+        _block(torch.zeros(5, device=DEV)).contribution()
