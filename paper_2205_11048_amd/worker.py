@@ -84,8 +84,16 @@ class EmbeddingBlock:
         if (given is not None) != has:
             raise GBAError(f"{name}: the block was made {'with' if has else 'without'} one ({name}={has})")
 
+    def _batch(self, ids):
+        # fewer would leave tokens of an earlier batch behind them
+        if ids.numel() != self.n:
+            raise GBAError(f"ids: expected {self.n}, got {ids.numel()}")
+
     def forward(self, ids, table, weight=None, bias=None, stream=None):
         """The batch's activations, [n, D]: layer_norm(scale * table[ids])."""
+        self._batch(ids)
+        if table.dim() != 2 or table.shape[1] != self.D:   # (the pulled rows lie one after the other)
+            raise GBAError(f"table: expected rows of {self.D}, got {list(table.shape)}")
         self._parameter("weight", weight, self.weight)
         self._parameter("bias", bias, self.bias)
         gba_pull_rows(ids, table, self.pulled_ids, self.inverse, self.pulled, self.num_pulled, self.workspace, self.err,
@@ -96,6 +104,7 @@ class EmbeddingBlock:
 
     def backward(self, ids, dy, weight=None, stream=None):
         """From the activations' gradient: dweight, dbias, and the rows' gradient by ID."""
+        self._batch(ids)
         self._parameter("weight", weight, self.weight)
         gba_layer_norm_grad(dy, self.x, self.mean, self.rstd, weight, self.dx, self.dweight, self.dbias, self.workspace,
                             stream=stream)

@@ -210,3 +210,14 @@ def test_a_replay_on_another_stream():
 def test_no_contribution_before_a_step():
     with pytest.raises(gba.GBAError):
         _block(torch.zeros(5, device=DEV)).contribution()
+
+
+def test_a_batch_or_a_table_of_another_size():
+    """Fewer tokens than the block's would be followed by an earlier batch's, narrower rows read as the block's."""
+    ids, dy, table, w, b, other = (_dev(t) for t in _inputs(11))
+    block = _block(other)
+    for bad in [lambda: block.forward(ids[:-2], table, w, b), lambda: block.forward(ids.repeat(2), table, w, b),
+                lambda: block.forward(ids, table[:, :32].contiguous(), w, b), lambda: block.forward(ids, table[0], w, b),
+                lambda: block.backward(ids[:-2], dy, w), lambda: block.backward(ids.repeat(2), dy.repeat(2, 1), w)]:
+        with pytest.raises(gba.GBAError):
+            bad()
