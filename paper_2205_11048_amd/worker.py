@@ -65,13 +65,15 @@ class EmbeddingBlock:
         # backward
         self.dx = new(n, D, kind=dtype)
         self.dweight, self.dbias = new(D) if weight else None, new(D) if bias else None
-        self.unique_ids, self.num_unique, self.rows = new(n, kind=torch.int64), new(1, kind=torch.int64), new(n, D)
+        self.unique_ids, self.num_unique = new(n, kind=torch.int64), new(1, kind=torch.int64)
+        self.row_grads = new(n, D)
         # the contribution
         self.grads = [*[g for g in (self.dweight, self.dbias) if g is not None], *dense_grads]
         self.P = sum(g.numel() for g in self.grads)
-        self.flat, self.norm, self.coef = new(self.P), new(1), new(1)
+        self.flat, self.rows, self.norm, self.coef = new(self.P), new(n, D), new(1), new(1)
         places = list(self.flat.split([g.numel() for g in self.grads]))
-        self.list = gba_tensor_list([*self.grads, self.rows], [*places, self.rows],
+        # (the rows not in place: clipped twice, a step would be scaled twice)
+        self.list = gba_tensor_list([*self.grads, self.row_grads], [*places, self.rows],
                                     [*[None] * len(self.grads), self.num_unique])
         # one scratch for all calls: they follow each other on the stream
         size = max(gba_pull_workspace_size(n, R), gba_layer_norm_grad_workspace_size(n, D),
@@ -108,12 +110,12 @@ class EmbeddingBlock:
         self._parameter("weight", weight, self.weight)
         gba_layer_norm_grad(dy, self.x, self.mean, self.rstd, weight, self.dx, self.dweight, self.dbias, self.workspace,
                             stream=stream)
-        gba_embedding_grad_rows(ids, self.dx, self.R, self.unique_ids, self.rows, self.num_unique, self.workspace,
+        gba_embedding_grad_rows(ids, self.dx, self.R, self.unique_ids, self.row_grads, self.num_unique, self.workspace,
                                 self.scale, self.padding_id, self.err, stream=stream)
 
     def clip(self, stream=None):
         """Every gradient scaled by min(1, max_norm / norm): the dense ones into
-        ``flat``, the rows in place."""
+        ``flat``, the rows (``row_grads``) into ``rows``."""
         self._stream = torch.cuda.current_stream(self.err.device) if stream is None else stream
         gba_clip_grads(self.list, self.max_norm, self.norm, self.workspace, self.coef, self.err, stream=stream)
 

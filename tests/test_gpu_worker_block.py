@@ -1,6 +1,6 @@
 """A worker's embedding block where a step is not the plain one: a layer norm
 that lacks a parameter, a step whose norm or IDs are bad, a step on
-another stream; against float64.
+another stream, a step clipped twice; against float64.
 
 Tolerances.  The activations are float32, so what the block computes is a few
 hundred float32 roundings (u = 2^-24): sums over rows of 64 elements, over 300
@@ -221,3 +221,19 @@ def test_a_batch_or_a_table_of_another_size():
                 lambda: block.backward(ids[:-2], dy, w), lambda: block.backward(ids.repeat(2), dy.repeat(2, 1), w)]:
         with pytest.raises(gba.GBAError):
             bad()
+
+
+def test_clipping_again():
+    """The gradients are what they were: a second clip, or one to another norm, is the only one."""
+    one = _inputs(12)
+    tensors = [_dev(t) for t in one]
+    block = _block(tensors[-1])
+    _step(block, *tensors[:5])
+    block.clip()
+    _check(block, one)
+    block.max_norm = 3.0
+    block.clip()
+    _check(block, one, max_norm=3.0)
+    block.max_norm = 1e9
+    block.clip()
+    _check(block, one, max_norm=1e9)
