@@ -21,7 +21,7 @@ from __future__ import annotations
 
 import torch
 
-from . import (DERR_NONFINITE, GBAError, gba_clip_grads, gba_embedding_grad_rows, gba_embedding_grad_workspace_size, gba_embedding_lookup,
+from . import (DERR_NONFINITE, MAX_D, GBAError, gba_clip_grads, gba_embedding_grad_rows, gba_embedding_grad_workspace_size, gba_embedding_lookup,
                gba_grad_norm_workspace_size, gba_layer_norm, gba_layer_norm_grad, gba_layer_norm_grad_workspace_size,
                gba_pull_rows, gba_pull_workspace_size, gba_tensor_list)
 
@@ -43,11 +43,14 @@ class EmbeddingBlock:
     clipped with the block's own and follow them in the contribution:
     [dweight, dbias, *dense_grads].  ``weight``, ``bias``: whether the layer norm has
     them; one that it lacks has no gradient, no part in the norm and no place in
-    the contribution."""
+    the contribution.  ``D`` is a width that can be pulled and pushed: a multiple of 4
+    up to MAX_D."""
 
     def __init__(self, n: int, D: int, R: int, dense_grads=(), dtype=torch.bfloat16, scale: float = 1.0,
                  padding_id: int = -1, eps: float = 1e-5, max_norm: float = 1.0, device="cuda", weight: bool = True,
                  bias: bool = True):
+        if D % 4 or not 4 <= D <= MAX_D:
+            raise GBAError(f"D: rows that are pulled and pushed have a multiple of 4 up to {MAX_D} elements, not {D}")
         self.n, self.D, self.R = n, D, R
         self.weight, self.bias = bool(weight), bool(bias)
         self.scale, self.padding_id, self.eps, self.max_norm = scale, padding_id, eps, max_norm
