@@ -149,14 +149,11 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-# The current stream's handle as a number: 0.3 us, where making the stream
-# object first takes 2.7, a third of a small call's time on the host.
-_raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
-
-
 def _stream(stream):
     if stream is None:
-        return _raw_stream(_device())
+        # The current stream's handle as a number: 0.3 us, where making the stream object first takes 2.7, a third of
+        # a small call's time on the host.  (Looked up here: a torch without a GPU back end lacks the names.)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
