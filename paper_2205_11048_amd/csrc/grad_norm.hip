@@ -126,7 +126,7 @@ struct ChunkData {
   }
   // (past the caches, which then keep what is still to be read: 200 M f32 elements 421 us, 432 through them)
   template <typename O>
-  __device__ __forceinline__ void store(void* to, int count, float coef) const {
+  __device__ __forceinline__ void store(void* to, int count, float first, float second) const {
     O* out = static_cast<O*>(to);
     const int whole = count / V;
 #pragma unroll
@@ -134,12 +134,12 @@ struct ChunkData {
       const int u = k * kNormBlock + threadIdx.x;
       typename VecOf<O, V>::type y;
 #pragma unroll
-      for (int e = 0; e < V; ++e) y[e] = (O)((float)x[k][e] * coef);
+      for (int e = 0; e < V; ++e) y[e] = (O)((float)x[k][e] * first * second);
       typename VecOf<O, V>::type* p = reinterpret_cast<typename VecOf<O, V>::type*>(out + u * V);
       if (u < whole) __builtin_nontemporal_store(y, p);
     }
     const int left = whole * V + threadIdx.x;
-    if (left < count) out[left] = (O)((float)rest * coef);
+    if (left < count) out[left] = (O)((float)rest * first * second);
   }
 };
 
@@ -184,7 +184,10 @@ grad_norm_kernel(const double* __restrict__ partial, int blocks, float* __restri
 }
 
 // What the coefficient is waited for: the first chunk of a block is on its way
-// when the block adds up the partial sums.
+// when the block adds up the partial sums.  The elements are multiplied by
+// `first`, rounded to 24 bits, and then by `second`, a power of two: 1, or
+// 2^-126 where the coefficient is below float's normal range and would have
+// fewer bits there (elements of 1e38 whose norm is 1e40 are still gradients).
 struct Coefficient {
   const double* partial;
   int blocks;
@@ -193,14 +196,18 @@ struct Coefficient {
   float* coef_out;
   int32_t* err;
   double* s_wave;
-  float value;
+  float value, first, second;
   bool known, finite;
   __device__ __forceinline__ void get() {
     if (known) return;
     known = true;
     const double n = sqrt(total_squares(partial, blocks, s_wave));
     finite = isfinite(n);
-    value = !finite ? 0.0f : n > max_norm ? (float)(max_norm / n) : 1.0f;
+    const double c = !finite ? 0.0 : n > max_norm ? max_norm / n : 1.0;
+    const bool small = c < 0x1p-126;
+    value = (float)c;
+    first = small ? (float)(c * 0x1p126) : value;
+    second = small ? 0x1p-126f : 1.0f;
     if (blockIdx.x == 0 && threadIdx.x == 0) {
       *norm = (float)n;
       if (coef_out) *coef_out = value;
@@ -218,7 +225,7 @@ __device__ __forceinline__ void clip_chunk(const TensorChunk& c, int count, Coef
   d.load(c.grad, count);
   f.get();
   if (f.finite && !(f.value == 1.0f && c.types >> 16))   // (in place with nothing to scale)
-    d.template store<O>(c.out, count, f.value);
+    d.template store<O>(c.out, count, f.first, f.second);
 }
 template <typename T>
 __device__ __forceinline__ void clip_chunk(const TensorChunk& c, int count, Coefficient& f) {
@@ -234,7 +241,7 @@ __global__ void __launch_bounds__(kNormBlock)
 clip_kernel(const TensorChunk* __restrict__ list, int64_t chunks, const double* __restrict__ partial, int blocks,
             double max_norm, float* __restrict__ norm, float* __restrict__ coef_out, int32_t* err) {
   __shared__ double s_wave[kNormWaves];
-  Coefficient f{partial, blocks, max_norm, norm, coef_out, err, s_wave, 1.0f, false, true};
+  Coefficient f{partial, blocks, max_norm, norm, coef_out, err, s_wave, 1.0f, 1.0f, 1.0f, false, true};
   const int64_t rounds = (chunks + gridDim.x - 1) / gridDim.x;
   for (int64_t r = rounds - 1; r >= 0; --r) {
     const int64_t i = r * gridDim.x + blockIdx.x;
