@@ -23,7 +23,7 @@ import torch
 
 from . import (DERR_NONFINITE, MAX_D, GBAError, gba_clip_grads, gba_embedding_grad_rows, gba_embedding_grad_workspace_size, gba_embedding_lookup,
                gba_grad_norm_workspace_size, gba_layer_norm, gba_layer_norm_grad, gba_layer_norm_grad_workspace_size,
-               gba_pull_rows, gba_pull_workspace_size, gba_tensor_list)
+               gba_pull_rows, gba_pull_workspace_size, gba_tensor_list, _stream)
 
 
 class StepError(GBAError):
@@ -59,7 +59,9 @@ class EmbeddingBlock:
         def new(*shape, kind=torch.float32):
             return torch.empty(shape, dtype=kind, device=dev)
 
-        self.err = torch.zeros(1, dtype=torch.int32, device=dev)
+        # the number of distinct rows and the error word, read together
+        self._words = torch.zeros(2, dtype=torch.int64, device=dev)
+        self.num_unique, self.err = self._words[:1], self._words[1:].view(torch.int32)[:1]
         # forward
         self.pulled_ids, self.inverse = new(n, kind=torch.int64), new(n, kind=torch.int32)
         self.pulled, self.num_pulled = new(n, D), new(1, kind=torch.int64)
@@ -68,8 +70,7 @@ class EmbeddingBlock:
         # backward
         self.dx = new(n, D, kind=dtype)
         self.dweight, self.dbias = new(D) if weight else None, new(D) if bias else None
-        self.unique_ids, self.num_unique = new(n, kind=torch.int64), new(1, kind=torch.int64)
-        self.row_grads = new(n, D)
+        self.unique_ids, self.row_grads = new(n, kind=torch.int64), new(n, D)
         # the contribution
         self.grads = [*[g for g in (self.dweight, self.dbias) if g is not None], *dense_grads]
         self.P = sum(g.numel() for g in self.grads)
@@ -119,7 +120,7 @@ class EmbeddingBlock:
     def clip(self, stream=None):
         """Every gradient scaled by min(1, max_norm / norm): the dense ones into
         ``flat``, the rows (``row_grads``) into ``rows``."""
-        self._stream = torch.cuda.current_stream(self.err.device) if stream is None else stream
+        self._stream = _stream(None) if stream is None else stream   # (the current one's handle)
         gba_clip_grads(self.list, self.max_norm, self.norm, self.workspace, self.coef, self.err, stream=stream)
 
     def contribution(self, stream=None):
@@ -127,9 +128,10 @@ class EmbeddingBlock:
         of the last ``clip``, or for ``stream`` (a graph replayed on another than it was
         recorded on).  Raises StepError where the step's IDs or norm were bad, and clears ``err``
         then: what the buffers hold is not this step's, and the next step begins
-        without it."""
+        without it.  (An ID outside the table in an earlier step, whose
+        contribution was not asked for, is reported here too.)"""
         self._wait(self._stream if stream is None else stream)
-        U, bits = int(self.num_unique.item()), int(self.err.item())
+        U, bits = self._words.tolist()
         if bits:
             self.err.zero_()
             torch.cuda.current_stream(self.err.device).synchronize()   # before a step on any stream
@@ -144,5 +146,7 @@ class EmbeddingBlock:
         if stream is None:
             raise GBAError("contribution: no step has been clipped")
         if not hasattr(stream, "synchronize"):
+            if int(stream) == _stream(None):
+                return   # what is read next waits for the current stream
             stream = torch.cuda.ExternalStream(int(stream), device=self.err.device)
         stream.synchronize()

@@ -17,7 +17,8 @@ class _Stream:
 
 def _block(monkeypatch):
     block = object.__new__(worker.EmbeddingBlock)
-    block.num_unique, block.err = torch.tensor([9]), torch.zeros(1, dtype=torch.int32)
+    block._words = torch.tensor([9, 0])
+    block.num_unique, block.err = block._words[:1], block._words[1:].view(torch.int32)[:1]
     block.flat, block.unique_ids, block.rows = torch.zeros(4), torch.arange(10), torch.zeros((10, 2))
     block.list = block.norm = block.workspace = block.coef = None
     block.max_norm, block._stream = 1.0, None
