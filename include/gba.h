@@ -551,7 +551,8 @@ gba_status gba_layer_norm_grad(const void* dy, int64_t dy_stride, const void* x,
  *          itself, or its part of the flat dense contribution of a push).
  *
  * The tensors are described once, in a list that the caller copies to the
- * device and keeps for as long as the buffers stay where they are.
+ * device and keeps for as long as the buffers stay where they are (a list is of
+ * addresses: where a buffer has moved, it still names the old one).
  * gba_tensor (host):
  *   grad, grad_type  n adjacent elements.
  *   out, out_type    where they go; NULL: only their norm is wanted (clipping
@@ -566,7 +567,8 @@ gba_status gba_layer_norm_grad(const void* dy, int64_t dy_stride, const void* x,
  * gba_tensor_list_fill: writes the list to host memory.
  *
  * gba_grad_norm: norm alone (one float, device).
- * gba_clip_grads: norm and coef (one float each, device; coef may be NULL),
+ * gba_clip_grads: norm and coef (one float each, device; coef may be NULL; the
+ *   tensors are scaled by it with 24 bits also where it is below float's normal range),
  *   and the clipped tensors.  max_norm > 0 (infinity: never clip).  Where the
  *   norm is not finite, GBA_DERR_NONFINITE is set, coef is 0 and nothing is
  *   written to any tensor: the caller skips the step.

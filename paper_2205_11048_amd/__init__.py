@@ -695,7 +695,13 @@ def gba_tensor_list(grads, outs=None, rows=None) -> TensorList:
     where they are from step to step).  ``outs``: where each goes when clipped (its
     own type; default: in place; None entries: nowhere).  ``rows``: for a matrix
     whose first rows alone count, their number as one int64 on the GPU (None
-    entries: all count)."""
+    entries: all count).
+
+    The list is of addresses: it is made once for tensors that stay where they
+    are, and again when one is replaced (a ``.grad`` that the next backward pass
+    allocates anew: copy into kept tensors, or zero them in place).  It keeps its
+    tensors alive, and a replaced one is not looked at any more.  Making it takes
+    host time and a copy that waits for the current stream: 24 tensors 58 us, 300 540."""
     grads = list(grads)
     outs = grads if outs is None else list(outs)
     rows = [None] * len(grads) if rows is None else list(rows)

@@ -57,7 +57,9 @@ struct Columns {
 // what reads it next then finds more of its other inputs there, and the call
 // itself takes 64 us instead of 81.  A small one is better left in them:
 // followed by a layer norm, 8192 x 4096 bf16 take 57 us and 61 past the
-// caches, 16,384 x 4096 115 and 111.
+// caches, 16,384 x 4096 115 and 111.  Narrow rows through a pull's inverse map,
+// 256,000 of 32 f32 from 72,000: 10.8 us and 7.5 into bf16, all of it the kernel's
+// (a floor of 6.2 and 3.9); 26,624 of 64 into bf16 5.9, the kernel 3.1.
 constexpr int64_t kPastCaches = int64_t(96) << 20;   // bytes
 template <typename T, typename O, bool PAST>
 __global__ void __launch_bounds__(kEmbBlock)
@@ -238,6 +240,12 @@ clear_table_kernel(EmbeddingGradArgs a) {
 // and 4 waves: 16,384 tokens and 1638 MB 299 302 277 268, 410 MB 100 97 89 115,
 // 205 MB 68 69 71 113; 8192 and 819 MB 158 144 136 135, 205 MB 59 50 48 63, 82 MB
 // 41 34 43 61; 6000 and 205 MB 56 46 44 45, 82 MB 38 30 32 46.
+// The comparisons go by the square of the tokens and pass the clear within a
+// doubling of 16,384: the radix sort and this, 1638 MB, 16,384 tokens 282 and 268,
+// 20,000 293 and 280, 24,576 306 and 299, 32,768 325 and 329, 49,152 363 and 475;
+// 410 MB 111 and 105, 20,000 118.6 and 117.9, 24,576 129 and 148.  (A table of
+// several GB is cleared faster by a launch of its own: 6554 MB, 16,384 tokens 1005
+// and 1079.)
 constexpr int64_t kRankMost = 6144, kRankMostWide = 8192, kRankMostClearing = 16384;
 constexpr int64_t kRankWideRows = int64_t(1) << 18;   // IDs of more than two 9-bit digits
 // (A table to clear makes it pay to 8192 for any IDs: into 30,000 x 32, 6000
@@ -321,8 +329,11 @@ rank_kernel(const int64_t* __restrict__ ids, int n, int64_t R, uint32_t* __restr
 // Bound by the gradient rows' bytes where rows are wide (16,384 x 4096 bf16 into
 // a cleared f32 table 37 us, 131 MB read and 60 written at 5.2 TB/s), by the
 // latency of a group's batches of random rows where they are narrow (256,000 x
-// 32 14 us, 28 MB).  Positions, not IDs, are what is shared out, so a token that
-// is a tenth of the batch costs no more than any other.
+// 32 14 us, 28 MB).  Positions, not IDs, are what is shared out, so this launch
+// takes no longer for a token that is half of the batch (the join does, below).
+// Added to a table instead of cleared into one: 16,384 x 4096 bf16 with 4956
+// distinct IDs 71 us, 49 of them here (a floor of 43, the rows read and written),
+// 256,000 x 32 with 58,000 46, 15 of them here.
 //
 // ONE: one block per column slice for at most kOneMost tokens, which it sorts
 // itself.
@@ -584,7 +595,11 @@ embedding_grad_kernel(EmbeddingGradArgs a, GradScratch g) {
 }
 
 // The IDs that cross blocks: by the block in which each begins.  A launch that
-// does little (3 to 5 us): most blocks compare two keys and end.
+// does little (3 to 5 us): most blocks compare two keys and end.  Bound by the
+// one block of a very frequent ID's column slice, whose lane groups read its
+// pieces in turn: 234,375 x 512 bf16 5 us, 44 with an ID that is a fifth of the
+// tokens, 86 with one that is half (whole calls 195, 217, 237, as there are fewer
+// rows to write then; 256,000 x 32 51, 53, 53).
 template <int V, int LPR, bool ROWS>
 __global__ void __launch_bounds__(kEmbBlock)
 embedding_grad_join_kernel(EmbeddingGradArgs a, GradScratch g) {

@@ -8,9 +8,9 @@
 // leads to its data and tensors of any sizes give even work.
 //
 // Bound by bytes, of which the second pass reads again what the 256 MB cache no
-// longer holds: 200 M f32 elements 121 us for the sum (6.6 TB/s) and 287 for the
+// longer holds: 200 M f32 elements 120 us for the sum (6.6 TB/s) and 285 for the
 // scaling (5.6 TB/s); small lists by the two launches (65,536 elements 3.0 and
-// 4.9 us).
+// 5.0 us).
 #include <algorithm>
 #include <cmath>
 #include <limits>
