@@ -261,7 +261,7 @@ def _buffers(case, st):
     st["dgate"] = new(*st["gate"].shape, dtype=st["gate"].dtype) if st["gate"] is not None else None
     for name in ("post_weight", "post_bias", "pre_weight", "pre_bias"):
         st["d" + name] = new(D) if st[name] is not None else None
-    st["workspace"] = new(gba.gba_residual_norm_grad_workspace_size(n, D, case["span"]), dtype=torch.uint8)
+    st["workspace"] = new(gba.gba_residual_norm_grad_workspace_size(n, D), dtype=torch.uint8)
 
 
 # ------------------------------------------------------------------ the calls
