@@ -239,6 +239,8 @@ def _buffers(case, st):
         kw = dict(m_exps=list(st["m_exp"].split(exps)), v_exps=list(st["v_exp"].split(exps))) if case["moments"] == 8 else {}
         st["list"] = gba.gba_adamw_list(parts("param"), st["grads"], parts("m"), parts("v"),
                                         copies=parts("copy") if case["copy"] else None, **kw)
+        if case["moments"] == 8:
+            st["m_values"], st["v_values"] = new(sum(rooms)), new(sum(rooms))
         return
     n, D, kind = case["n"], case["D"], TYPES[case["type"]]
     if op in ("scan_fwd", "scan_bwd"):
@@ -273,7 +275,11 @@ def _run_own(st):
         st["t"] += 1
         gba.gba_adamw(st["list"], LR, BETA1, BETA2, ADAM_EPS, DECAY, st["t"], seed=SEED, coef=st["coef"],
                       err=st["err"])
-        return _adamw_out(st)
+        if case["moments"] == 32:
+            return _adamw_out(st)
+        gba.gba_moments_read(st["m"], st["m_exp"], gba.MOMENT_M, st["m_values"])
+        gba.gba_moments_read(st["v"], st["v_exp"], gba.MOMENT_V, st["v_values"])
+        return {"param": st["param"], "m": st["m_values"], "v": st["v_values"], "copy": st["copy"]}
     if op == "scan_fwd":
         gba.gba_recurrence(st["x"], st["a"], st["out"], offsets=st["offsets"], length=case["L"], h0=st["h0"],
                            h_last=st["last"], workspace=st["workspace"], err=st["err"])
