@@ -446,13 +446,14 @@ def _scan_grad(st):
     keep, first, last, rows = _places(case, st["offsets"])
     x, a, d = st["x"][:rows].float(), st["a"][:rows].float(), st["dh"][:rows].float()
     f, i = torch.sigmoid(a), torch.sigmoid(-a)
-    if st["dlast"] is not None:
-        d[last] += st["dlast"][keep]
     # g[t] = d[t] + f[t + 1] g[t + 1], from the end
     F = torch.zeros_like(f)
     F[:-1] = f[1:]
     F[last] = 0.0
-    g = _affine_scan(F.flip(0), d.flip(0), _steps(case)).flip(0)
+    d = d.flip(0)
+    if st["dlast"] is not None:
+        d[rows - 1 - last] += st["dlast"][keep]
+    g = _affine_scan(F.flip(0), d, _steps(case)).flip(0)
     before = torch.zeros_like(x)
     before[1:] = st["h"][:rows - 1].float()
     before[first] = st["h0"][keep] if st["h0"] is not None else 0.0
