@@ -53,10 +53,10 @@ typedef enum gba_status {
 enum {
   GBA_DERR_ID_RANGE = 1,      /* an embedding ID outside [0, R)                    */
   GBA_DERR_FUTURE_TOKEN = 2,  /* a token newer than the step being applied         */
-  GBA_DERR_OFFSETS = 4,       /* contribution offsets not 0 .. N and non-decreasing */
+  GBA_DERR_OFFSETS = 4,       /* offsets not from 0 to at most N, or decreasing     */
   GBA_DERR_ROW_RANGE = 8,     /* a row index passed to a sparse apply outside [0, R) */
   GBA_DERR_TABLE_FULL = 16,   /* the ID index or the row pool has no room left      */
-  GBA_DERR_NONFINITE = 32     /* a gradient norm that is infinite or not a number   */
+  GBA_DERR_NONFINITE = 32     /* a gradient norm (gba_adamw: an element) that is infinite or not a number */
 };
 
 /* Element types of the worker's operators (32-bit float, bfloat16, half). */
@@ -599,6 +599,209 @@ gba_status gba_grad_norm(const void* list, int64_t chunks, float* norm, void* wo
 
 gba_status gba_clip_grads(const void* list, int64_t chunks, double max_norm, float* norm, float* coef,
                           void* workspace, size_t workspace_bytes, int32_t* err, hipStream_t stream);
+
+/*
+ * A block's output joined to the residual stream, and the stream normalised
+ * for the next block, row by row:
+ *   u = post(z),  h = alpha * x + act(gate) * u,  y = pre(h).
+ * post and pre are each nothing, a layer norm or an RMS norm over the D columns,
+ *   layer: (v - mean) * rstd * weight + bias,  rstd = 1 / sqrt(sum (v - mean)^2 / D + eps);
+ *   RMS:   the same with 0 in the mean's place and no bias;
+ * and what pre normalises is h as it is stored, rounded to its type.  act is 1
+ * (no gate), the gate, or its sigmoid.  Row i takes the gate's row
+ * i / gate_span: gate_span = 1 is a gate for every row, n (or more) one for all
+ * rows, the length of equal sequences one for each of them.
+ *
+ * gba_residual_norm: h, y and the statistics.
+ *   x, h          [n][D] of stream_type, which is `type`, or GBA_F32 beside 16 bits.
+ *                 h may be x itself (the same stride).
+ *   z, y          [n][D] of `type`; y only with pre.
+ *   gate          [ceil(n / gate_span)][D] of gate_type; NULL with GBA_GATE_NONE.
+ *   post_weight, post_bias, pre_weight, pre_bias   [D] of weight_type; each may be
+ *                 NULL (1 and 0); only where there is such a norm, a bias with a layer norm.
+ *   post_mean, post_rstd, pre_mean, pre_rstd       [n] float out, of the norms that
+ *                 there are (no means of an RMS norm); each may be NULL.
+ *
+ * gba_residual_norm_grad: with dy the gradient of y and dh what reaches h
+ * from elsewhere (NULL: nothing),
+ *   e = dh + pre'(dy),  dx = alpha * e,  dz = post'(act(gate) * e),
+ *   dgate = act'(gate) * (sum of e * u over the rows that share the gate's row),
+ * and the parameters' gradients, summed over rows in 32 bits in a fixed order.
+ *   z, h, gate, the weights, post_bias and the statistics as the forward call had
+ *   and left them; x, y and pre_bias are not read, h only with pre.
+ *   dy            [n][D] of `type`, with pre.
+ *   dh, dx        [n][D] of stream_type; dx may be NULL, and may be dh itself.
+ *   dz            [n][D] of `type`; may be NULL, and may be dy itself.
+ *   dgate         like gate; may be NULL.
+ *   dpost_weight, dpost_bias, dpre_weight, dpre_bias   [D] of grad_type; each may
+ *                 be NULL, also where the weight is not.  With n == 0 they are 0.
+ *   workspace     gba_residual_norm_grad_workspace_size bytes, 16-byte aligned.
+ * Limits: 0 <= n < 2^31, 1 <= D <= 2^20, gate_span >= 1, eps >= 0, alpha finite.
+ */
+typedef enum gba_row_norm { GBA_ROW_NORM_NONE = 0, GBA_ROW_NORM_LAYER = 1, GBA_ROW_NORM_RMS = 2 } gba_row_norm;
+typedef enum gba_gate { GBA_GATE_NONE = 0, GBA_GATE_LINEAR = 1, GBA_GATE_SIGMOID = 2 } gba_gate;
+
+typedef struct gba_residual_norm_args {
+  int64_t n;
+  int32_t D;
+  int32_t stream_type, type, weight_type, gate_type, grad_type;   /* gba_dtype */
+  int32_t post, pre;                                              /* gba_row_norm */
+  int32_t gate_kind;                                              /* gba_gate */
+  int32_t unused;                                                 /* 0 */
+  int64_t gate_span;
+  double alpha, eps;
+  /* in */
+  const void* x;
+  const void* z;
+  const void* gate;
+  const void* post_weight;
+  const void* post_bias;
+  const void* pre_weight;
+  const void* pre_bias;
+  /* out of the forward call, in of the gradient */
+  void* h;
+  void* y;
+  float* post_mean;
+  float* post_rstd;
+  float* pre_mean;
+  float* pre_rstd;
+  /* the gradient's */
+  const void* dy;
+  const void* dh;
+  void* dx;
+  void* dz;
+  void* dgate;
+  void* dpost_weight;
+  void* dpost_bias;
+  void* dpre_weight;
+  void* dpre_bias;
+  /* row strides */
+  int64_t x_stride, z_stride, gate_stride, h_stride, y_stride;
+  int64_t dy_stride, dh_stride, dx_stride, dz_stride, dgate_stride;
+} gba_residual_norm_args;
+
+gba_status gba_residual_norm(const gba_residual_norm_args* args /* host */, hipStream_t stream);
+
+gba_status gba_residual_norm_grad_workspace_size(int64_t n, int32_t D, size_t* bytes /* host out */);
+
+gba_status gba_residual_norm_grad(const gba_residual_norm_args* args /* host */, void* workspace,
+                                  size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * A gated linear recurrence over the positions of B sequences, column by column:
+ *   f = sigmoid(a[t]),  h[t] = f * h[t-1] + (1 - f) * x[t],
+ * where h[-1] of sequence b is h0[b].
+ *   x, a, h   [n][D] of `type`, positions of a sequence one after another.
+ *   offsets   [B + 1] int64 on the device: sequence b holds positions
+ *             [offsets[b], offsets[b+1]), any number of them; offsets[0] = 0 and
+ *             offsets[B] <= n, and rows behind it are neither read nor written.
+ *             NULL: B sequences of n / B positions each (one position each: a
+ *             step of serving, for which h0 and h_last may be one array).
+ *   h0        [B][D] float, or NULL (0).
+ *   h_last    [B][D] float out, each sequence's last state before it is rounded
+ *             to `type` (h0 of an empty one); may be NULL, and may be h0 itself.
+ * The state is held in 32 bits from position to position.
+ *
+ * gba_recurrence_grad: with dh the gradient of h and dh_last that of h_last,
+ *   g[t] = dh[t] + f[t+1] * g[t+1]   (the last: dh[t] + dh_last),
+ *   dx[t] = (1 - f) * g[t],  da[t] = g[t] * (h[t-1] - x[t]) * f * (1 - f),
+ *   dh0 = f[0] * g[0]   (of an empty sequence: dh_last).
+ *   dh, dx, da   [n][D] of `type`; h as the forward call left it.  dx may be dh.
+ *   dh_last      [B][D] float, or NULL (0).
+ *   dh0          [B][D] float out; may be NULL, and may be dh_last itself.
+ * No other arrays overlap.
+ * workspace  gba_recurrence_workspace_size bytes, 16-byte aligned.
+ * err        GBA_DERR_OFFSETS (outputs then undefined); may be NULL.
+ * Limits: 0 <= n < 2^31, 1 <= B < 2^31 (with offsets NULL n is a multiple of B),
+ * 1 <= D <= 2^20.
+ */
+gba_status gba_recurrence_workspace_size(int64_t n, int64_t B, int32_t D, size_t* bytes /* host out */);
+
+gba_status gba_recurrence(const void* x, int64_t x_stride, const void* a, int64_t a_stride, gba_dtype type, int64_t n,
+                          int64_t B, int32_t D, const int64_t* offsets, const float* h0, void* h, int64_t h_stride,
+                          float* h_last, void* workspace, size_t workspace_bytes, int32_t* err, hipStream_t stream);
+
+gba_status gba_recurrence_grad(const void* dh, int64_t dh_stride, const void* x, int64_t x_stride, const void* a,
+                               int64_t a_stride, const void* h, int64_t h_stride, gba_dtype type, int64_t n, int64_t B,
+                               int32_t D, const int64_t* offsets, const float* h0, const float* dh_last, void* dx,
+                               int64_t dx_stride, void* da, int64_t da_stride, float* dh0, void* workspace,
+                               size_t workspace_bytes, int32_t* err, hipStream_t stream);
+
+/*
+ * One AdamW step (Loshchilov and Hutter 2019) over many tensors:
+ *   g = coef * grad,  m' = b1 m + (1 - b1) g,  v' = b2 v + (1 - b2) g^2,
+ *   param' = (1 - lr * weight_decay * decay) * param
+ *            - lr * (m' / (1 - b1^t)) / (sqrt(v' / (1 - b2^t)) + eps),
+ * in 32 bits as gba_apply_adam's.  The tensors are described once, in a list
+ * that the caller copies to the device, as gba_tensor_list_* does.
+ *
+ * gba_adamw_tensor (host):
+ *   param         n adjacent floats, updated in place.
+ *   grad          n adjacent elements of grad_type.
+ *   m, v          the moments, updated in place; zeros before the first step.
+ *   moment_bits   32: n floats each.  8: n bytes each, with
+ *   m_exp, v_exp  ceil(n / GBA_MOMENT_BLOCK) bytes each.  Each GBA_MOMENT_BLOCK
+ *                 consecutive elements share an exponent byte E and hold a code c each:
+ *                 m: a sign bit, 4 exponent bits, 3 mantissa bits;
+ *                 v, of which the root is held: 4 exponent bits, 4 mantissa bits.
+ *                 With p mantissa bits, k = c >> p and i = c mod 2^p a code stands for
+ *                 2^(E - 127) * 2^(max(k, 1) - 15) * ((k > 0) + i / 2^p).  E is the least
+ *                 that holds the block's largest value (0 where all are 0).  What lies
+ *                 between two codes is rounded up with the probability of its
+ *                 fraction, by a hash of seed, t, the tensor's place in the list and
+ *                 the element's place in the tensor: the same call gives the same bits.
+ *   copy          n elements of copy_type that get the updated parameters as well; may be NULL.
+ *   decay         what this tensor takes of the weight decay (0 for none, 1 for all of it).
+ * gba_adamw_list_size, gba_adamw_list_fill: as gba_tensor_list_*.
+ *
+ * gba_adamw:
+ *   t         the step's number, from 1.
+ *   t_device  one int64 on the device that is taken in its place when the kernels
+ *             run (below 1 counts as 1), for a step in a graph, whose caller
+ *             advances it there; may be NULL.
+ *   coef      one float on the device that every gradient is multiplied by, as
+ *             gba_clip_grads leaves it; may be NULL (1).  Where it is 0 (a norm
+ *             that was not finite) nothing is written.
+ *   err       GBA_DERR_NONFINITE where an element's m' or v' is infinite or not a
+ *             number; the element's parameter stays as it is, and its moments too (in 8
+ *             bits up to their block's new exponent).
+ * list       the device copy, 16-byte aligned.
+ *
+ * gba_moments_read: the values that n elements' moments in 8 bits stand for, m
+ * or the root of v, as floats (to look at them, to store them, to go on in 32 bits).
+ * Limits: 0 <= T <= 2^20 tensors, 0 <= n <= 2^40 elements each, b1 and b2 in [0, 1), eps >= 2^-126, t >= 1.
+ */
+#define GBA_MOMENT_BLOCK 256
+enum { GBA_MOMENT_M = 0, GBA_MOMENT_V = 1 };
+
+typedef struct gba_adamw_tensor {
+  float* param;
+  const void* grad;
+  void* m;
+  void* v;
+  uint8_t* m_exp;
+  uint8_t* v_exp;
+  void* copy;
+  int64_t n;
+  double decay;
+  int32_t grad_type;     /* gba_dtype */
+  int32_t copy_type;
+  int32_t moment_bits;   /* 32 or 8 */
+  int32_t unused;        /* 0 */
+} gba_adamw_tensor;
+
+gba_status gba_adamw_list_size(const gba_adamw_tensor* tensors /* host */, int32_t T, size_t* bytes /* host out */,
+                               int64_t* chunks /* host out */);
+
+gba_status gba_adamw_list_fill(const gba_adamw_tensor* tensors /* host */, int32_t T, void* list /* host out */,
+                               size_t list_bytes);
+
+gba_status gba_adamw(const void* list, int64_t chunks, double lr, double beta1, double beta2, double eps,
+                     double weight_decay, int64_t t, const int64_t* t_device, uint32_t seed, const float* coef,
+                     int32_t* err, hipStream_t stream);
+
+gba_status gba_moments_read(const uint8_t* codes, const uint8_t* exps, int64_t n, int32_t which /* GBA_MOMENT_* */,
+                            float* out, hipStream_t stream);
 
 #ifdef __cplusplus
 }

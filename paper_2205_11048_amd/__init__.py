@@ -28,6 +28,10 @@ __all__ = [
     "gba_embedding_grad_dense", "gba_layer_norm", "gba_layer_norm_grad_workspace_size", "gba_layer_norm_grad",
     "TensorList", "gba_tensor_list", "gba_grad_norm_workspace_size", "gba_grad_norm", "gba_clip_grads",
     "DERR_NONFINITE",
+    "gba_residual_norm", "gba_residual_norm_grad_workspace_size", "gba_residual_norm_grad", "ROW_NORM_NONE",
+    "ROW_NORM_LAYER", "ROW_NORM_RMS", "GATE_NONE", "GATE_LINEAR", "GATE_SIGMOID", "gba_recurrence_workspace_size",
+    "gba_recurrence", "gba_recurrence_grad", "AdamwList", "gba_adamw_list", "gba_adamw", "gba_moments_read",
+    "MOMENT_BLOCK", "MOMENT_M", "MOMENT_V",
     "pointer_table", "DECAY_TOKEN", "DECAY_ID_TAG", "NORM_PER_ID_COUNT", "NORM_BY_K",
     "DERR_ID_RANGE", "DERR_FUTURE_TOKEN", "DERR_OFFSETS", "DERR_ROW_RANGE", "MAX_K", "MAX_D",
     "LIB_PATH",
@@ -44,6 +48,10 @@ DERR_ID_RANGE, DERR_FUTURE_TOKEN, DERR_OFFSETS, DERR_ROW_RANGE, DERR_TABLE_FULL 
 DERR_NONFINITE = 32
 EMPTY_ID = -1
 SORT_AUTO, SORT_PLAIN, SORT_HOT = -1, 0, 1
+ROW_NORM_NONE, ROW_NORM_LAYER, ROW_NORM_RMS = 0, 1, 2     # gba_row_norm
+GATE_NONE, GATE_LINEAR, GATE_SIGMOID = 0, 1, 2            # gba_gate
+MOMENT_BLOCK = 256                                        # GBA_MOMENT_BLOCK
+MOMENT_M, MOMENT_V = 0, 1
 MAX_K, MAX_D = 4096, 256
 NOALLOC_SCRATCH_BYTES = 64 << 20     # GBA_NOALLOC_SCRATCH_BYTES
 ERR_SCRATCH_LIMIT = 6
@@ -53,6 +61,7 @@ _I32 = ctypes.c_int32
 _I64 = ctypes.c_int64
 _F64 = ctypes.c_double
 _F32 = ctypes.c_float
+_U32 = ctypes.c_uint32
 _SIZE = ctypes.c_size_t
 
 _SIGNATURES = {
@@ -116,6 +125,17 @@ _SIGNATURES = {
     "gba_grad_norm_workspace_size": ([_I64, ctypes.POINTER(_SIZE)], _I32),
     "gba_grad_norm": ([_P, _I64, _P, _P, _SIZE, _P, _P], _I32),
     "gba_clip_grads": ([_P, _I64, _F64, _P, _P, _P, _SIZE, _P, _P], _I32),
+    "gba_residual_norm": ([_P, _P], _I32),
+    "gba_residual_norm_grad_workspace_size": ([_I64, _I32, ctypes.POINTER(_SIZE)], _I32),
+    "gba_residual_norm_grad": ([_P, _P, _SIZE, _P], _I32),
+    "gba_recurrence_workspace_size": ([_I64, _I64, _I32, ctypes.POINTER(_SIZE)], _I32),
+    "gba_recurrence": ([_P, _I64, _P, _I64, _I32, _I64, _I64, _I32, _P, _P, _P, _I64, _P, _P, _SIZE, _P, _P], _I32),
+    "gba_recurrence_grad": ([_P, _I64, _P, _I64, _P, _I64, _P, _I64, _I32, _I64, _I64, _I32, _P, _P, _P, _P, _I64, _P,
+                             _I64, _P, _P, _SIZE, _P, _P], _I32),
+    "gba_adamw_list_size": ([_P, _I32, ctypes.POINTER(_SIZE), ctypes.POINTER(_I64)], _I32),
+    "gba_adamw_list_fill": ([_P, _I32, _P, _SIZE], _I32),
+    "gba_moments_read": ([_P, _P, _I64, _I32, _P, _P], _I32),
+    "gba_adamw": ([_P, _I64, _F64, _F64, _F64, _F64, _F64, _I64, _P, _U32, _P, _P, _P], _I32),
 }
 
 _LIB = None
@@ -754,6 +774,266 @@ def gba_clip_grads(tensors: TensorList, max_norm, norm, workspace, coef=None, er
     _need(err, torch.int32, "err", 1)
     _check(lib().gba_clip_grads(_ptr(tensors.entries), tensors.chunks, float(max_norm), _ptr(norm), _ptr(coef),
                                 _ptr(workspace), workspace.numel(), _ptr(err), _stream(stream)))
+
+
+class _ResidualNorm(ctypes.Structure):   # gba_residual_norm_args
+    _fields_ = ([("n", _I64)] + [(k, _I32) for k in ("D", "stream_type", "type", "weight_type", "gate_type", "grad_type",
+                                                     "post", "pre", "gate_kind", "unused")]
+                + [("gate_span", _I64), ("alpha", _F64), ("eps", _F64)]
+                + [(k, _P) for k in ("x", "z", "gate", "post_weight", "post_bias", "pre_weight", "pre_bias", "h", "y",
+                                     "post_mean", "post_rstd", "pre_mean", "pre_rstd", "dy", "dh", "dx", "dz", "dgate",
+                                     "dpost_weight", "dpost_bias", "dpre_weight", "dpre_bias")]
+                + [(k + "_stride", _I64) for k in ("x", "z", "gate", "h", "y", "dy", "dh", "dx", "dz", "dgate")])
+
+
+def _vectors(D, **given):
+    """Checks vectors that are there to be of one type, and returns it."""
+    kind = None
+    for name, t in given.items():
+        if t is None:
+            continue
+        k = _vector(t, name, D)
+        if kind is not None and k != kind:
+            raise GBAError(f"{name}: expected the type of the other ones of {', '.join(given)}")
+        kind = k
+    return kind or 0
+
+
+def _like(t, name, kind, n, D):
+    """The row stride of a matrix that may be None, of this type and size."""
+    if t is None:
+        return D
+    k, step = _matrix(t, name, n, D)
+    if k != kind:
+        raise GBAError(f"{name}: expected {list(_DTYPES)[kind]}")
+    return step
+
+
+def _gate_matrix(gate, gate_kind, gate_span, n, D):
+    if gate is None:
+        if gate_kind != GATE_NONE:
+            raise GBAError("gate: missing")
+        return 0, D
+    if gate_kind == GATE_NONE:
+        raise GBAError("gate: given with GATE_NONE")
+    if gate_span < 1:
+        raise GBAError(f"gate_span: expected 1 or more, got {gate_span}")
+    return _matrix(gate, "gate", -(-n // gate_span), D)
+
+
+def _statistics(n, post_mean, post_rstd, pre_mean, pre_rstd):
+    _need(post_mean, torch.float32, "post_mean", n)
+    _need(post_rstd, torch.float32, "post_rstd", n)
+    _need(pre_mean, torch.float32, "pre_mean", n)
+    _need(pre_rstd, torch.float32, "pre_rstd", n)
+
+
+def gba_residual_norm(x, z, h, y=None, gate=None, gate_kind=None, gate_span=1, alpha=1.0, eps=1e-5,
+                      post=ROW_NORM_RMS, pre=ROW_NORM_RMS, post_weight=None, post_bias=None, pre_weight=None,
+                      pre_bias=None, post_mean=None, post_rstd=None, pre_mean=None, pre_rstd=None, stream=None):
+    """h = alpha * x + act(gate) * post(z) and y = pre(h), over the rows of ``z``.
+    ``post`` and ``pre``: ROW_NORM_NONE, ROW_NORM_LAYER or ROW_NORM_RMS (``y`` only with ``pre``).
+    ``gate``: a row for every ``gate_span`` rows of z; ``gate_kind``: GATE_LINEAR
+    (default where there is one) or GATE_SIGMOID.  ``x`` and ``h`` (which may be
+    ``x``) have the type of ``z``, or float32 beside 16 bits.  The weights and
+    biases (one type) and the statistics (float32) may be None."""
+    kind, z_step = _matrix(z, "z")
+    n, D = z.shape
+    stream_kind, x_step = _matrix(x, "x", n, D)
+    h_step = _like(h, "h", stream_kind, n, D)
+    y_step = _like(y, "y", kind, n, D)
+    if gate_kind is None:
+        gate_kind = GATE_LINEAR if gate is not None else GATE_NONE
+    g_kind, g_step = _gate_matrix(gate, gate_kind, gate_span, n, D)
+    w_kind = _vectors(D, post_weight=post_weight, post_bias=post_bias, pre_weight=pre_weight, pre_bias=pre_bias)
+    _statistics(n, post_mean, post_rstd, pre_mean, pre_rstd)
+    args = _ResidualNorm(n, D, stream_kind, kind, w_kind, g_kind, 0, post, pre, gate_kind, 0, gate_span, alpha, eps,
+                         _ptr(x), _ptr(z), _ptr(gate), _ptr(post_weight), _ptr(post_bias), _ptr(pre_weight),
+                         _ptr(pre_bias), _ptr(h), _ptr(y), _ptr(post_mean), _ptr(post_rstd), _ptr(pre_mean),
+                         _ptr(pre_rstd), None, None, None, None, None, None, None, None, None, x_step, z_step, g_step,
+                         h_step, y_step, 0, 0, 0, 0, 0)
+    _check(lib().gba_residual_norm(ctypes.addressof(args), _stream(stream)))
+
+
+def gba_residual_norm_grad_workspace_size(n, D) -> int:
+    b = _SIZE(0)
+    _check(lib().gba_residual_norm_grad_workspace_size(int(n), int(D), ctypes.byref(b)))
+    return int(b.value)
+
+
+def gba_residual_norm_grad(dy, dh, z, h, dx, dz, workspace, gate=None, gate_kind=None, gate_span=1, alpha=1.0, eps=1e-5,
+                           post=ROW_NORM_RMS, pre=ROW_NORM_RMS, post_weight=None, post_bias=None, pre_weight=None,
+                           post_mean=None, post_rstd=None, pre_mean=None, pre_rstd=None, dgate=None,
+                           dpost_weight=None, dpost_bias=None, dpre_weight=None, dpre_bias=None, stream=None):
+    """Gradients of gba_residual_norm from ``dy`` (with ``pre``) and ``dh``, what
+    reaches h from elsewhere (None: nothing).  ``dx`` (which may be ``dh``), ``dz``
+    (which may be ``dy``), ``dgate`` (the type of ``gate``) and the parameters'
+    gradients (one type) may be None."""
+    kind, z_step = _matrix(z, "z")
+    n, D = z.shape
+    stream_kind = next((_DTYPES.get(t.dtype) for t in (dh, dx, h) if t is not None), kind)
+    steps = [_like(t, name, k, n, D) for t, name, k in ((h, "h", stream_kind), (dy, "dy", kind), (dh, "dh", stream_kind),
+                                                        (dx, "dx", stream_kind), (dz, "dz", kind))]
+    if gate_kind is None:
+        gate_kind = GATE_LINEAR if gate is not None else GATE_NONE
+    g_kind, g_step = _gate_matrix(gate, gate_kind, gate_span, n, D)
+    dg_step = _like(dgate, "dgate", g_kind, -(-n // gate_span), D)
+    w_kind = _vectors(D, post_weight=post_weight, post_bias=post_bias, pre_weight=pre_weight)
+    dw_kind = _vectors(D, dpost_weight=dpost_weight, dpost_bias=dpost_bias, dpre_weight=dpre_weight,
+                       dpre_bias=dpre_bias)
+    _statistics(n, post_mean, post_rstd, pre_mean, pre_rstd)
+    _need(workspace, torch.uint8, "workspace")
+    args = _ResidualNorm(n, D, stream_kind, kind, w_kind, g_kind, dw_kind, post, pre, gate_kind, 0, gate_span, alpha, eps,
+                         None, _ptr(z), _ptr(gate), _ptr(post_weight), _ptr(post_bias), _ptr(pre_weight), None,
+                         _ptr(h), None, _ptr(post_mean), _ptr(post_rstd), _ptr(pre_mean), _ptr(pre_rstd), _ptr(dy),
+                         _ptr(dh), _ptr(dx), _ptr(dz), _ptr(dgate), _ptr(dpost_weight), _ptr(dpost_bias),
+                         _ptr(dpre_weight), _ptr(dpre_bias), 0, z_step, g_step, steps[0], 0, steps[1], steps[2],
+                         steps[3], steps[4], dg_step)
+    _check(lib().gba_residual_norm_grad(ctypes.addressof(args), _ptr(workspace), workspace.numel(), _stream(stream)))
+
+
+def gba_recurrence_workspace_size(n, B, D) -> int:
+    b = _SIZE(0)
+    _check(lib().gba_recurrence_workspace_size(int(n), int(B), int(D), ctypes.byref(b)))
+    return int(b.value)
+
+
+def _sequences(n, D, offsets, length, states):
+    """The number of sequences: of ``length`` positions each, or by ``offsets``; checks the [B, D] states."""
+    if offsets is not None:
+        _need(offsets, torch.int64, "offsets")
+        B = offsets.numel() - 1
+        if B < 1 or length:
+            raise GBAError("offsets: expected one more than there are sequences (at least one), and no length")
+    else:
+        if length < 1 or n % length:
+            raise GBAError(f"length: {n} positions are not sequences of {length}")
+        B = n // length
+    for name, t in states:
+        if t is not None:
+            _need(t, torch.float32, name)
+            if t.shape != (B, D):
+                raise GBAError(f"{name}: expected [{B}, {D}], got {list(t.shape)}")
+    return B
+
+
+def gba_recurrence(x, a, h, offsets=None, length=0, h0=None, h_last=None, workspace=None, err=None, stream=None):
+    """h[t] = f * h[t-1] + (1 - f) * x[t] with f = sigmoid(a[t]) over the rows of
+    ``x``, the positions of sequences one after another: of ``length`` each, or
+    (``length`` 0) sequence b those of [offsets[b], offsets[b+1]).  ``h0`` and
+    ``h_last`` (float32 [B, D], which may be one tensor) may be None."""
+    kind, x_step = _matrix(x, "x")
+    n, D = x.shape
+    a_step, h_step = _like(a, "a", kind, n, D), _like(h, "h", kind, n, D)
+    B = _sequences(n, D, offsets, length, (("h0", h0), ("h_last", h_last)))
+    _need(workspace, torch.uint8, "workspace")
+    _need(err, torch.int32, "err", 1)
+    if n == 0 and offsets is None:
+        return
+    if workspace is None:
+        raise GBAError("workspace: missing")
+    _check(lib().gba_recurrence(_ptr(x), x_step, _ptr(a), a_step, kind, n, B, D, _ptr(offsets), _ptr(h0), _ptr(h), h_step,
+                                _ptr(h_last), _ptr(workspace), workspace.numel(), _ptr(err), _stream(stream)))
+
+
+def gba_recurrence_grad(dh, x, a, h, dx, da, offsets=None, length=0, h0=None, dh_last=None, dh0=None, workspace=None,
+                        err=None, stream=None):
+    """Gradients of gba_recurrence from ``dh`` and ``dh_last`` (None: 0); ``h`` as
+    the forward call left it; ``dx`` may be ``dh``, ``dh0`` (may be None) ``dh_last``."""
+    kind, x_step = _matrix(x, "x")
+    n, D = x.shape
+    steps = [_like(t, name, kind, n, D) for t, name in ((dh, "dh"), (a, "a"), (h, "h"), (dx, "dx"), (da, "da"))]
+    B = _sequences(n, D, offsets, length, (("h0", h0), ("dh_last", dh_last), ("dh0", dh0)))
+    _need(workspace, torch.uint8, "workspace")
+    _need(err, torch.int32, "err", 1)
+    if n == 0 and offsets is None:
+        return
+    if workspace is None:
+        raise GBAError("workspace: missing")
+    _check(lib().gba_recurrence_grad(_ptr(dh), steps[0], _ptr(x), x_step, _ptr(a), steps[1], _ptr(h), steps[2], kind, n, B,
+                                     D, _ptr(offsets), _ptr(h0), _ptr(dh_last), _ptr(dx), steps[3], _ptr(da), steps[4],
+                                     _ptr(dh0), _ptr(workspace), workspace.numel(), _ptr(err), _stream(stream)))
+
+
+class _AdamwTensor(ctypes.Structure):   # gba_adamw_tensor
+    _fields_ = [("param", _P), ("grad", _P), ("m", _P), ("v", _P), ("m_exp", _P), ("v_exp", _P), ("copy", _P), ("n", _I64),
+                ("decay", _F64), ("grad_type", _I32), ("copy_type", _I32), ("moment_bits", _I32), ("unused", _I32)]
+
+
+class AdamwList:
+    """Tensors described for gba_adamw: the device list, its number of chunks,
+    and the tensors, which it keeps alive."""
+
+    def __init__(self, entries, chunks, tensors):
+        self.entries, self.chunks, self.tensors = entries, chunks, tensors
+
+
+def gba_adamw_list(params, grads, m, v, m_exps=None, v_exps=None, copies=None, decays=None) -> AdamwList:
+    """Describes ``params`` (contiguous float32) with their gradients (contiguous
+    float32, bfloat16 or float16) and moments: float32 tensors of the same
+    sizes, or uint8 ones with an exponent (uint8) for every MOMENT_BLOCK elements in
+    ``m_exps`` and ``v_exps``; all of them zeros before the first step.
+    ``copies``: tensors (or None) that get the updated parameters in their own
+    type.  ``decays``: each one's part of the weight decay (default 1).  As with
+    gba_tensor_list, the list is of addresses: it is made again when a tensor is replaced."""
+    params, grads, m, v = list(params), list(grads), list(m), list(v)
+    T = len(params)
+    m_exps, v_exps, copies = ([None] * T if t is None else list(t) for t in (m_exps, v_exps, copies))
+    decays = [1.0] * T if decays is None else list(decays)
+    if not T == len(grads) == len(m) == len(v) == len(m_exps) == len(v_exps) == len(copies) == len(decays):
+        raise GBAError("params, grads, moments, exponents, copies and decays differ in length")
+    host = (_AdamwTensor * T)()
+    for i, (p, g, mi, vi, me, ve, c) in enumerate(zip(params, grads, m, v, m_exps, v_exps, copies)):
+        n = p.numel()
+        _need(p, torch.float32, f"params[{i}]")
+        for t, name in ((g, "grads"), (c, "copies")):
+            if t is not None and (t.dtype not in _DTYPES or not t.is_cuda or not t.is_contiguous() or t.numel() != n):
+                raise GBAError(f"{name}[{i}]: expected a contiguous float32, bfloat16 or float16 tensor of {n} elements "
+                               "on the GPU")
+        eight = mi.dtype == torch.uint8
+        for t, name in ((mi, "m"), (vi, "v")):
+            _need(t, torch.uint8 if eight else torch.float32, f"{name}[{i}]")
+            if t.numel() != n:
+                raise GBAError(f"{name}[{i}]: expected {n} elements, got {t.numel()}")
+        for t, name in ((me, "m_exps"), (ve, "v_exps")):
+            if (t is not None) != eight:
+                raise GBAError(f"{name}[{i}]: expected with moments in 8 bits, and only with them")
+            _need(t, torch.uint8, f"{name}[{i}]", -(-n // MOMENT_BLOCK))
+        if n == 0:
+            continue
+        host[i] = _AdamwTensor(_ptr(p), _ptr(g), _ptr(mi), _ptr(vi), _ptr(me), _ptr(ve), _ptr(c), n, float(decays[i]),
+                               _DTYPES[g.dtype], 0 if c is None else _DTYPES[c.dtype], 8 if eight else 32, 0)
+    for i in range(T):
+        host[i].moment_bits = host[i].moment_bits or 32   # (an empty tensor)
+    size, chunks = _SIZE(0), _I64(0)
+    _check(lib().gba_adamw_list_size(host, T, ctypes.byref(size), ctypes.byref(chunks)))
+    image = torch.empty(size.value, dtype=torch.uint8)
+    _check(lib().gba_adamw_list_fill(host, T, _ptr(image), size.value))
+    device = params[0].device if params else torch.device("cuda")
+    return AdamwList(image.to(device), int(chunks.value), (params, grads, m, v, m_exps, v_exps, copies))
+
+
+def gba_adamw(tensors: AdamwList, lr, beta1, beta2, eps, weight_decay, t, t_device=None, seed=0, coef=None, err=None,
+              stream=None):
+    """One AdamW step over the list's tensors.  ``t``: the step's number from 1,
+    or ``t_device`` (one int64 on the GPU) in its place; ``coef``: one float32 on
+    the GPU that scales every gradient (0: nothing is written); ``seed``: of the rounding of
+    moments in 8 bits."""
+    _need(t_device, torch.int64, "t_device", 1)
+    _need(coef, torch.float32, "coef", 1)
+    _need(err, torch.int32, "err", 1)
+    _check(lib().gba_adamw(_ptr(tensors.entries), tensors.chunks, lr, beta1, beta2, eps, weight_decay, t, _ptr(t_device),
+                           seed & 0xFFFFFFFF, _ptr(coef), _ptr(err), _stream(stream)))
+
+
+def gba_moments_read(codes, exps, which, out, stream=None):
+    """The values that moments in 8 bits stand for: of m (MOMENT_M), or of the
+    root of v (MOMENT_V), as float32."""
+    n = codes.numel()
+    _need(codes, torch.uint8, "codes")
+    _need(exps, torch.uint8, "exps", -(-n // MOMENT_BLOCK))
+    _need(out, torch.float32, "out", n)
+    _check(lib().gba_moments_read(_ptr(codes), _ptr(exps), n, which, _ptr(out), _stream(stream)))
 
 
 # ------------------------------------------------- measurement kernels

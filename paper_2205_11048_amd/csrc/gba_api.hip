@@ -742,4 +742,224 @@ gba_status gba_clip_grads(const void* list, int64_t chunks, double max_norm, flo
   return from_hip(launch_clip_grads(list, chunks, max_norm, norm, coef, workspace, err, stream));
 }
 
+// ------------------------------------ norms with gate and residual
+static gba_status residual_norm_check(const gba_residual_norm_args* a, bool grad) {
+  if (!a) return GBA_ERR_NULL;
+  const int32_t D = a->D;
+  if (a->n < 0 || a->n > INT32_MAX || !columns_ok(D) || a->gate_span < 1 || !(a->eps >= 0.0) ||
+      !std::isfinite(a->eps) || !std::isfinite(a->alpha))
+    return GBA_ERR_INVALID_ARG;
+  if (!dtype_ok(a->type) || !dtype_ok(a->stream_type) || !dtype_ok(a->weight_type) || !dtype_ok(a->gate_type) ||
+      !dtype_ok(a->grad_type) || (a->stream_type != a->type && a->stream_type != GBA_F32))
+    return GBA_ERR_INVALID_ARG;
+  if (a->post < GBA_ROW_NORM_NONE || a->post > GBA_ROW_NORM_RMS || a->pre < GBA_ROW_NORM_NONE ||
+      a->pre > GBA_ROW_NORM_RMS || a->gate_kind < GBA_GATE_NONE || a->gate_kind > GBA_GATE_SIGMOID)
+    return GBA_ERR_INVALID_ARG;
+  const bool post = a->post != GBA_ROW_NORM_NONE, pre = a->pre != GBA_ROW_NORM_NONE;
+  // a parameter, a gate or a gradient of one that the call would not use
+  if ((!post && (a->post_weight || a->dpost_weight)) || (!pre && (a->pre_weight || a->dpre_weight)) ||
+      (a->post != GBA_ROW_NORM_LAYER && (a->post_bias || a->dpost_bias || a->post_mean)) ||
+      (a->pre != GBA_ROW_NORM_LAYER && (a->pre_bias || a->dpre_bias || a->pre_mean)) ||
+      (!post && a->post_rstd) || (!pre && (a->pre_rstd || a->y || a->dy)) ||
+      (a->gate_kind == GBA_GATE_NONE && (a->gate || a->dgate)))
+    return GBA_ERR_INVALID_ARG;
+  const void* params[] = {a->post_weight, a->post_bias, a->pre_weight, a->pre_bias};
+  for (const void* p : params)
+    if (!element_aligned(p, a->weight_type)) return GBA_ERR_INVALID_ARG;
+  const void* stats[] = {a->post_mean, a->post_rstd, a->pre_mean, a->pre_rstd};
+  for (const void* p : stats)
+    if (!element_aligned(p, GBA_F32)) return GBA_ERR_INVALID_ARG;
+  struct Rows {
+    const void* p;
+    int64_t stride;
+    int32_t type;
+  } rows[] = {{a->z, a->z_stride, a->type},          {a->h, a->h_stride, a->stream_type},
+              {a->gate, a->gate_stride, a->gate_type}, {grad ? nullptr : a->x, a->x_stride, a->stream_type},
+              {grad ? nullptr : a->y, a->y_stride, a->type}, {grad ? a->dy : nullptr, a->dy_stride, a->type},
+              {grad ? a->dh : nullptr, a->dh_stride, a->stream_type}, {grad ? a->dx : nullptr, a->dx_stride, a->stream_type},
+              {grad ? a->dz : nullptr, a->dz_stride, a->type}, {grad ? a->dgate : nullptr, a->dgate_stride, a->gate_type}};
+  for (const Rows& r : rows)
+    if (r.p && (!stride_ok(r.stride, D) || !element_aligned(r.p, r.type))) return GBA_ERR_INVALID_ARG;
+  if (a->n > 0 && a->gate_kind != GBA_GATE_NONE && !a->gate) return GBA_ERR_NULL;
+  return GBA_OK;
+}
+
+gba_status gba_residual_norm(const gba_residual_norm_args* a, hipStream_t stream) {
+  const gba_status st = residual_norm_check(a, false);
+  if (st != GBA_OK) return st;
+  if (a->n == 0) return GBA_OK;
+  if (!a->x || !a->z || !a->h || (a->pre != GBA_ROW_NORM_NONE && !a->y)) return GBA_ERR_NULL;
+  if (a->h == a->x && a->h_stride != a->x_stride) return GBA_ERR_INVALID_ARG;
+  return from_hip(launch_residual_norm(*a, stream));
+}
+
+gba_status gba_residual_norm_grad_workspace_size(int64_t n, int32_t D, size_t* bytes) {
+  if (!bytes) return GBA_ERR_NULL;
+  if (n < 0 || n > INT32_MAX || !columns_ok(D)) return GBA_ERR_INVALID_ARG;
+  *bytes = align_up(residual_norm_grad_workspace_bytes(n, D));
+  return GBA_OK;
+}
+
+gba_status gba_residual_norm_grad(const gba_residual_norm_args* a, void* workspace, size_t workspace_bytes,
+                                  hipStream_t stream) {
+  const gba_status st = residual_norm_check(a, true);
+  if (st != GBA_OK) return st;
+  if (!element_aligned(a->dpost_weight, a->grad_type) || !element_aligned(a->dpost_bias, a->grad_type) ||
+      !element_aligned(a->dpre_weight, a->grad_type) || !element_aligned(a->dpre_bias, a->grad_type))
+    return GBA_ERR_INVALID_ARG;
+  if (!workspace) return GBA_ERR_NULL;
+  if (!aligned16(workspace)) return GBA_ERR_INVALID_ARG;
+  if (a->n > 0) {
+    if (!a->z || (a->pre != GBA_ROW_NORM_NONE && (!a->h || !a->dy || !a->pre_rstd)) ||
+        (a->pre == GBA_ROW_NORM_LAYER && !a->pre_mean) || (a->post != GBA_ROW_NORM_NONE && !a->post_rstd) ||
+        (a->post == GBA_ROW_NORM_LAYER && !a->post_mean))
+      return GBA_ERR_NULL;
+    if ((a->dx && a->dx == a->dh && a->dx_stride != a->dh_stride) ||
+        (a->dz && a->dz == a->dy && a->dz_stride != a->dy_stride))
+      return GBA_ERR_INVALID_ARG;
+  }
+  if (workspace_bytes < align_up(residual_norm_grad_workspace_bytes(a->n, a->D))) return GBA_ERR_WORKSPACE;
+  return from_hip(launch_residual_norm_grad(*a, workspace, stream));
+}
+
+// ------------------------------------ gated linear recurrence
+static bool recurrence_sizes_ok(int64_t n, int64_t B, int32_t D) {
+  return n >= 0 && n <= INT32_MAX && B >= 1 && B <= INT32_MAX && columns_ok(D);
+}
+static bool recurrence_rows_ok(const void* p, int64_t stride, int32_t type, int32_t D) {
+  return stride_ok(stride, D) && element_aligned(p, type);
+}
+static bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
+
+gba_status gba_recurrence_workspace_size(int64_t n, int64_t B, int32_t D, size_t* bytes) {
+  if (!bytes) return GBA_ERR_NULL;
+  if (!recurrence_sizes_ok(n, B, D)) return GBA_ERR_INVALID_ARG;
+  *bytes = align_up(recurrence_workspace_bytes(n, B, D));
+  return GBA_OK;
+}
+
+gba_status gba_recurrence(const void* x, int64_t x_stride, const void* a, int64_t a_stride, gba_dtype type, int64_t n,
+                          int64_t B, int32_t D, const int64_t* offsets, const float* h0, void* h, int64_t h_stride,
+                          float* h_last, void* workspace, size_t workspace_bytes, int32_t* err, hipStream_t stream) {
+  if (!recurrence_sizes_ok(n, B, D) || !dtype_ok(type) || (!offsets && n % B != 0)) return GBA_ERR_INVALID_ARG;
+  if (!workspace || (n > 0 && (!x || !a || !h))) return GBA_ERR_NULL;
+  if (!recurrence_rows_ok(x, x_stride, type, D) || !recurrence_rows_ok(a, a_stride, type, D) ||
+      !recurrence_rows_ok(h, h_stride, type, D) || !element_aligned(h0, GBA_F32) || !element_aligned(h_last, GBA_F32) ||
+      !aligned8(offsets) || !aligned16(workspace))
+    return GBA_ERR_INVALID_ARG;
+  if (workspace_bytes < align_up(recurrence_workspace_bytes(n, B, D))) return GBA_ERR_WORKSPACE;
+  RecurrenceArgs r{};
+  r.x = x;
+  r.a = a;
+  r.h = h;
+  r.h0 = h0;
+  r.h_last = h_last;
+  r.offsets = offsets;
+  r.n = n;
+  r.B = B;
+  r.x_stride = x_stride;
+  r.a_stride = a_stride;
+  r.h_stride = h_stride;
+  r.D = D;
+  r.type = (int32_t)type;
+  return from_hip(launch_recurrence(r, workspace, err, stream));
+}
+
+gba_status gba_recurrence_grad(const void* dh, int64_t dh_stride, const void* x, int64_t x_stride, const void* a,
+                               int64_t a_stride, const void* h, int64_t h_stride, gba_dtype type, int64_t n, int64_t B,
+                               int32_t D, const int64_t* offsets, const float* h0, const float* dh_last, void* dx,
+                               int64_t dx_stride, void* da, int64_t da_stride, float* dh0, void* workspace,
+                               size_t workspace_bytes, int32_t* err, hipStream_t stream) {
+  if (!recurrence_sizes_ok(n, B, D) || !dtype_ok(type) || (!offsets && n % B != 0)) return GBA_ERR_INVALID_ARG;
+  if (!workspace || (n > 0 && (!dh || !x || !a || !h || !dx || !da))) return GBA_ERR_NULL;
+  if (!recurrence_rows_ok(dh, dh_stride, type, D) || !recurrence_rows_ok(x, x_stride, type, D) ||
+      !recurrence_rows_ok(a, a_stride, type, D) || !recurrence_rows_ok(h, h_stride, type, D) ||
+      !recurrence_rows_ok(dx, dx_stride, type, D) || !recurrence_rows_ok(da, da_stride, type, D) ||
+      !element_aligned(h0, GBA_F32) || !element_aligned(dh_last, GBA_F32) || !element_aligned(dh0, GBA_F32) ||
+      !aligned8(offsets) || !aligned16(workspace) || (n > 0 && dx == dh && dx_stride != dh_stride))
+    return GBA_ERR_INVALID_ARG;
+  if (workspace_bytes < align_up(recurrence_workspace_bytes(n, B, D))) return GBA_ERR_WORKSPACE;
+  RecurrenceArgs r{};
+  r.x = x;
+  r.a = a;
+  r.h = const_cast<void*>(h);
+  r.h0 = h0;
+  r.offsets = offsets;
+  r.dh = dh;
+  r.dx = dx;
+  r.da = da;
+  r.dh_last = dh_last;
+  r.dh0 = dh0;
+  r.n = n;
+  r.B = B;
+  r.x_stride = x_stride;
+  r.a_stride = a_stride;
+  r.h_stride = h_stride;
+  r.dh_stride = dh_stride;
+  r.dx_stride = dx_stride;
+  r.da_stride = da_stride;
+  r.D = D;
+  r.type = (int32_t)type;
+  return from_hip(launch_recurrence_grad(r, workspace, err, stream));
+}
+
+// ------------------------------------ AdamW over many tensors
+static gba_status adamw_tensors_check(const gba_adamw_tensor* t, int32_t T) {
+  if (T < 0 || T > (1 << 20)) return GBA_ERR_INVALID_ARG;
+  if (T > 0 && !t) return GBA_ERR_NULL;
+  for (int32_t i = 0; i < T; ++i) {
+    if (t[i].n < 0 || t[i].n > (int64_t(1) << 40) || !dtype_ok(t[i].grad_type) || !dtype_ok(t[i].copy_type) ||
+        (t[i].moment_bits != 32 && t[i].moment_bits != 8) || !std::isfinite(t[i].decay))
+      return GBA_ERR_INVALID_ARG;
+    if (t[i].n > 0 && (!t[i].param || !t[i].grad || !t[i].m || !t[i].v ||
+                       (t[i].moment_bits == 8 && (!t[i].m_exp || !t[i].v_exp))))
+      return GBA_ERR_NULL;
+    if (!element_aligned(t[i].param, GBA_F32) || !element_aligned(t[i].grad, t[i].grad_type) ||
+        !element_aligned(t[i].copy, t[i].copy_type) ||
+        (t[i].moment_bits == 32 && (!element_aligned(t[i].m, GBA_F32) || !element_aligned(t[i].v, GBA_F32))))
+      return GBA_ERR_INVALID_ARG;
+  }
+  return GBA_OK;
+}
+
+gba_status gba_adamw_list_size(const gba_adamw_tensor* tensors, int32_t T, size_t* bytes, int64_t* chunks) {
+  if (!bytes || !chunks) return GBA_ERR_NULL;
+  const gba_status st = adamw_tensors_check(tensors, T);
+  if (st != GBA_OK) return st;
+  *chunks = adamw_chunks(tensors, T);
+  *bytes = adamw_list_bytes(*chunks);
+  return GBA_OK;
+}
+
+gba_status gba_adamw_list_fill(const gba_adamw_tensor* tensors, int32_t T, void* list, size_t list_bytes) {
+  const gba_status st = adamw_tensors_check(tensors, T);
+  if (st != GBA_OK) return st;
+  const size_t need = adamw_list_bytes(adamw_chunks(tensors, T));
+  if (list_bytes < need) return GBA_ERR_WORKSPACE;
+  if (need == 0) return GBA_OK;
+  if (!list) return GBA_ERR_NULL;
+  fill_adamw_list(tensors, T, list);
+  return GBA_OK;
+}
+
+gba_status gba_adamw(const void* list, int64_t chunks, double lr, double beta1, double beta2, double eps,
+                     double weight_decay, int64_t t, const int64_t* t_device, uint32_t seed, const float* coef,
+                     int32_t* err, hipStream_t stream) {
+  if (!chunks_ok(chunks) || !adam_args_ok(beta1, beta2, t) || !((float)eps >= 0x1p-126f) || !std::isfinite(eps) ||
+      !std::isfinite(lr) || !std::isfinite(weight_decay))
+    return GBA_ERR_INVALID_ARG;
+  if (chunks > 0 && !list) return GBA_ERR_NULL;
+  if (!aligned16(list) || !aligned8(t_device) || !element_aligned(coef, GBA_F32)) return GBA_ERR_INVALID_ARG;
+  const AdamwParams hp{lr, beta1, beta2, eps, weight_decay};
+  return from_hip(launch_adamw(list, chunks, hp, t, t_device, seed, coef, err, stream));
+}
+
+gba_status gba_moments_read(const uint8_t* codes, const uint8_t* exps, int64_t n, int32_t which, float* out,
+                            hipStream_t stream) {
+  if (n < 0 || n > (int64_t(1) << 40) || (which != GBA_MOMENT_M && which != GBA_MOMENT_V)) return GBA_ERR_INVALID_ARG;
+  if (n > 0 && (!codes || !exps || !out)) return GBA_ERR_NULL;
+  if (!element_aligned(out, GBA_F32)) return GBA_ERR_INVALID_ARG;
+  return from_hip(launch_moments_read(codes, exps, n, which, out, stream));
+}
+
 }  // extern "C"

@@ -264,4 +264,44 @@ hipError_t launch_grad_norm(const void* list, int64_t chunks, float* norm, void*
 hipError_t launch_clip_grads(const void* list, int64_t chunks, double max_norm, float* norm, float* coef, void* ws,
                              int32_t* err, hipStream_t stream);
 
+// ---- norms with gate and residual
+hipError_t launch_residual_norm(const gba_residual_norm_args& a, hipStream_t stream);
+// (the most of any n up to this one)
+size_t residual_norm_grad_workspace_bytes(int64_t n, int32_t D);
+hipError_t launch_residual_norm_grad(const gba_residual_norm_args& a, void* ws, hipStream_t stream);
+
+// ---- gated linear recurrence
+struct RecurrenceArgs {
+  const void* x;
+  const void* a;
+  void* h;               // out, or as the forward call left it
+  const float* h0;       // [B][D], may be null
+  float* h_last;         // [B][D], may be null
+  const int64_t* offsets;   // [B + 1], null: equal lengths
+  // the gradient's
+  const void* dh;
+  void* dx;
+  void* da;
+  const float* dh_last;  // may be null
+  float* dh0;            // may be null
+  int64_t n, B, x_stride, a_stride, h_stride, dh_stride, dx_stride, da_stride;
+  int32_t D, type;
+};
+// (the most of any n up to this one)
+size_t recurrence_workspace_bytes(int64_t n, int64_t B, int32_t D);
+hipError_t launch_recurrence(const RecurrenceArgs& r, void* ws, int32_t* err, hipStream_t stream);
+hipError_t launch_recurrence_grad(const RecurrenceArgs& r, void* ws, int32_t* err, hipStream_t stream);
+
+// ---- AdamW over many tensors
+struct AdamwParams {
+  double lr, beta1, beta2, eps, weight_decay;
+};
+int64_t adamw_chunks(const gba_adamw_tensor* t, int32_t T);
+size_t adamw_list_bytes(int64_t chunks);
+void fill_adamw_list(const gba_adamw_tensor* t, int32_t T, void* list);
+hipError_t launch_adamw(const void* list, int64_t chunks, const AdamwParams& hp, int64_t t, const int64_t* t_device,
+                        uint32_t seed, const float* coef, int32_t* err, hipStream_t stream);
+hipError_t launch_moments_read(const uint8_t* codes, const uint8_t* exps, int64_t n, int which, float* out,
+                               hipStream_t stream);
+
 }  // namespace gba

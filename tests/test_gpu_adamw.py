@@ -1,0 +1,288 @@
+"""The AdamW step over many tensors against float64, and its moments in 8 bits
+against the header's formula, code by code.
+
+Tolerances: u is float32's unit roundoff.  m' passes through the gradient's
+product with coef, two constants, two products and a sum: 5 u of the magnitudes.
+v' has the gradient twice: 8 u of itself.  The update's further factors (the
+root of v' 4 u and 2 u of its own, the constants, the sum with eps, the reciprocal 2 u,
+two products) leave 16 u of it beside m's; the decay's factor and the difference 4 u of p."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2205_11048_amd as gba
+from block_reference import BF16, F16, F32, U32, close, decode, encode, random_words, rounded
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+HP = dict(lr=3e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.05)
+
+
+def _dev(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).to(DEV)
+
+
+class Case:
+    def __init__(self, sizes, gtypes, eight, copies=None, decays=None, shift=0, seed=0, fresh=False):
+        rng = np.random.default_rng(len(sizes) * 7 + sum(sizes) + seed)
+        T = len(sizes)
+        self.sizes, self.eight, self.decays = sizes, eight, decays or [1.0] * T
+        f = np.float32
+        self.p0 = [rng.normal(size=n).astype(f) for n in sizes]
+        scale = [np.exp(3 * rng.normal(size=n)) * 10.0 ** rng.integers(-6, 3) for n in sizes]
+        g = [torch.from_numpy(s * rng.normal(size=n)).to(t) for s, n, t in zip(scale, sizes, gtypes)]
+        self.g0 = [t.double().numpy() for t in g]
+        m = [np.zeros(n, f) if fresh else (s * rng.normal(size=n)).astype(f) for s, n in zip(scale, sizes)]
+        v = [np.zeros(n, f) if fresh else ((s * rng.normal(size=n)) ** 2).astype(f) for s, n in zip(scale, sizes)]
+        def place(x):   # `shift` elements into a longer tensor, whose ends are looked at afterwards
+            x = torch.as_tensor(x)
+            wide = torch.full((len(x) + 2 * shift + 1,), 77, dtype=x.dtype, device=DEV)
+            self.wide.append((wide, shift, len(x)))
+            wide[shift:shift + len(x)] = x.to(DEV)
+            return wide[shift:shift + len(x)]
+
+        self.wide = []
+        self.p, self.g = [place(x) for x in self.p0], [place(x) for x in g]
+        kw = {}
+        if eight:
+            half = [np.full(n, 32768) for n in sizes]
+            cm, cv = [encode(x, 3, h) for x, h in zip(m, half)], [encode(np.sqrt(x), 4, h) for x, h in zip(v, half)]
+            self.m, self.v = [place(c) for c, _ in cm], [place(c) for c, _ in cv]
+            self.me, self.ve = [place(e) for _, e in cm], [place(e) for _, e in cv]
+            self.m0 = [decode(*c, 3).astype(f) for c in cm]
+            self.v0 = [(r * r).astype(f) for r in (decode(*c, 4).astype(f) for c in cv)]
+            kw = dict(m_exps=self.me, v_exps=self.ve)
+        else:
+            self.m, self.v, self.m0, self.v0 = [place(x) for x in m], [place(x) for x in v], m, v
+        self.copies = [None if t is None else torch.zeros(n, dtype=t, device=DEV) for n, t in zip(sizes, copies or [None] * T)]
+        self.list = gba.gba_adamw_list(self.p, self.g, self.m, self.v, copies=self.copies, decays=self.decays, **kw)
+        self.err = torch.zeros(1, dtype=torch.int32, device=DEV)
+
+    def step(self, t=7, **kw):
+        gba.gba_adamw(self.list, **{**HP, **kw}, t=t, err=self.err) if "seed" in kw else \
+            gba.gba_adamw(self.list, **{**HP, **kw}, t=t, seed=12345, err=self.err)
+
+    def untouched(self):
+        for wide, shift, n in self.wide:
+            assert (wide[:shift] == 77).all() and (wide[shift + n:] == 77).all()
+
+
+def check(c, t=7, coef=1.0, tensor_coef=False, seed=12345):
+    c.step(t=t, coef=torch.tensor([coef], device=DEV) if tensor_coef else None, seed=seed)
+    b1, b2, lr = HP["beta1"], HP["beta2"], HP["lr"]
+    cf = np.float64(np.float32(coef))
+    infinite = False
+    for i, n in enumerate(c.sizes):
+        # (a half that has become infinite leaves its element as it is)
+        fine = np.isfinite(c.g0[i])
+        infinite |= not fine.all()
+        g, m0, v0 = np.where(fine, c.g0[i], 0.0) * cf, c.m0[i].astype(np.float64), c.v0[i].astype(np.float64)
+        m, v = np.where(fine, b1 * m0 + (1 - b1) * g, m0), np.where(fine, b2 * v0 + (1 - b2) * g * g, v0)
+        size = b1 * np.abs(m0) + (1 - b1) * np.abs(g)
+        if not c.eight:
+            close(c.m[i], m, 5 * U32 * size + 1e-44, f"m[{i}]")
+            close(c.v[i], v, 8 * U32 * v + 1e-44, f"v[{i}]")
+        factor = lr / (1 - b1 ** t) / (np.sqrt(v / (1 - b2 ** t)) + HP["eps"])
+        p0 = c.p0[i].astype(np.float64)
+        p = np.where(fine, p0 * (1 - lr * HP["weight_decay"] * c.decays[i]) - factor * m, p0)
+        bound = factor * (5 * U32 * size + 16 * U32 * np.abs(m)) + 4 * U32 * np.abs(p0) + 1e-44
+        close(c.p[i], p, rounded(bound, p, F32), f"param[{i}]")
+        if c.copies[i] is not None:
+            assert torch.equal(c.copies[i], c.p[i].to(c.copies[i].dtype))
+        if c.eight:
+            # the same operations in float32, each rounded, then the header's formula
+            f = np.float32
+            x = np.where(fine, c.g0[i], 0.0).astype(f) * f(coef)
+            mn = np.where(fine, f(b1) * c.m0[i] + f(1 - b1) * x, c.m0[i])
+            vn = np.where(fine, f(b2) * c.v0[i] + f(1 - b2) * (x * x), c.v0[i])
+            wm, wv = random_words(n, seed, t, i)
+            for got, exps, value, mantissa, words in ((c.m[i], c.me[i], mn, 3, wm), (c.v[i], c.ve[i], np.sqrt(vn), 4, wv)):
+                code, exp = encode(value, mantissa, words)
+                assert np.array_equal(exps.cpu().numpy(), exp)
+                assert np.array_equal(got.cpu().numpy(), code)
+    assert int(c.err) == (gba.DERR_NONFINITE if infinite else 0)
+    c.untouched()
+
+
+SIZES = [[1], [2, 3], [255], [256], [257, 1], [1000, 0, 17], [4095], [4096], [4097], [70_001], [5] * 40, [12_288, 3, 100_000]]
+
+
+@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("sizes", SIZES)
+@pytest.mark.parametrize("eight", [False, True])
+def test_sizes(sizes, eight, shift):
+    kinds = [F32, BF16, F16]
+    check(Case(sizes, [kinds[i % 3] for i in range(len(sizes))], eight, shift=shift))
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_coefficient_copies_and_decay(eight):
+    c = Case([300, 5000, 77, 1], [BF16, F32, F16, F32], eight, copies=[BF16, F16, None, F32], decays=[0.0, 1.0, 0.5, 0.0])
+    check(c, t=1, coef=0.3125, tensor_coef=True)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("t", [1, 2, 1000, 1 << 40])
+def test_steps_from_nothing(t, eight):
+    check(Case([3000], [F32], eight, fresh=True), t=t, seed=0xFFFFFFFF)
+
+
+def test_chunks_beyond_one_round_of_blocks():
+    n = 2048 * 4096 + 5000
+    p, g = torch.ones(n, device=DEV), torch.full((n,), 0.5, dtype=BF16, device=DEV)
+    m, v = torch.zeros(n, device=DEV), torch.zeros(n, device=DEV)
+    gba.gba_adamw(gba.gba_adamw_list([p], [g], [m], [v]), **HP, t=1)
+    first = torch.ones(1000, device=DEV)
+    gba.gba_adamw(gba.gba_adamw_list([first], [g[:1000]], [m[:1000].zero_()], [v[:1000].zero_()]), **HP, t=1)
+    assert (p == first[0]).all() and (m == m[0]).all() and (v == v[0]).all()
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_a_coefficient_of_nothing_writes_nothing(eight):
+    c = Case([700, 3], [F32, BF16], eight)
+    before = [w.clone() for w, _, _ in c.wide]
+    c.step(coef=torch.zeros(1, device=DEV))
+    assert all(torch.equal(a, w) for a, (w, _, _) in zip(before, c.wide)) and int(c.err) == 0
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("value", [float("inf"), float("nan"), 3e38])
+def test_what_is_not_finite_is_left_out(eight, value):
+    """(3e38 squared is not.)  The other elements go on, those of the same block too."""
+    c, plain = Case([600], [F32], eight), Case([600], [F32], eight)
+    plain.g[0][5] = 0.0
+    c.g[0][5] = value
+    c.step()
+    plain.step()
+    assert int(c.err) == gba.DERR_NONFINITE and int(plain.err) == 0
+    keep = torch.ones(600, dtype=torch.bool, device=DEV)
+    keep[5] = False
+    assert torch.equal(c.p[0][keep], plain.p[0][keep]) and float(c.p[0][5]) == c.p0[0][5]
+    if not eight:
+        assert torch.equal(c.m[0][keep], plain.m[0][keep]) and torch.equal(c.v[0][keep], plain.v[0][keep])
+        assert float(c.m[0][5]) == c.m0[0][5] and float(c.v[0][5]) == c.v0[0][5]
+    else:
+        assert torch.equal(c.m[0][256:], plain.m[0][256:]) and torch.equal(c.v[0][256:], plain.v[0][256:])
+        got = decode(c.m[0].cpu().numpy(), c.me[0].cpu().numpy(), 3)[5]
+        assert abs(got - c.m0[0][5]) <= 0.125 * abs(c.m0[0][5]) + 2.0 ** -16 * np.abs(c.m0[0][:256]).max()
+
+
+def test_rounding_is_right_on_average():
+    """A mean of 2^20 roundings of one value: each is off by less than the distance of two codes, d, with a variance
+    of no more than d^2 / 4, and the 16 bits of a random number leave 2^-17 d of bias."""
+    n = 1 << 20
+    for value in (0.3, 1.0 / 3.0, 0.9 * 2.0 ** -3, 2.0 ** -13 * 0.7):
+        g = torch.full((n,), value, device=DEV)
+        g[::256] = 1.9   # the largest of every block: above 1.875, the most at an exponent of 0 with 3 mantissa bits
+        p, m, v = torch.zeros(n, device=DEV), torch.zeros(n, dtype=torch.uint8, device=DEV), torch.zeros(n, dtype=torch.uint8, device=DEV)
+        me, ve = torch.zeros(n // 256, dtype=torch.uint8, device=DEV), torch.zeros(n // 256, dtype=torch.uint8, device=DEV)
+        gba.gba_adamw(gba.gba_adamw_list([p], [g], [m], [v], [me], [ve]), 0.0, 0.0, 0.0, 1e-8, 0.0, 1, seed=5)
+        for code, exp, mantissa in ((m, me, 3), (v, ve, 4)):
+            got = decode(code.cpu().numpy(), exp.cpu().numpy(), mantissa)
+            keep = np.arange(n) % 256 != 0
+            got = got[keep]
+            near = np.unique(got)
+            assert len(near) <= 2
+            # (codes of the least exponent are 2^(E - 127) 2^(1 - 15) 2^-mantissa apart)
+            assert int(exp[0]) == 127 + (mantissa == 3)
+            d = max(2.0 ** (np.floor(np.log2(value)) - mantissa), 2.0 ** (int(exp[0]) - 127 - 14 - mantissa))
+            assert np.abs(near - value).max() < d
+            assert abs(got.mean() - value) <= 6 * d / 2 / np.sqrt(keep.sum()) + 2.0 ** -17 * d + 4 * U32 * value
+
+
+def test_another_seed_step_or_place_rounds_otherwise():
+    def codes(seed, t, tensors=1):
+        n = 4096
+        g = torch.linspace(0.1, 1.0, n, device=DEV)
+        p, m, v, me, ve = ([torch.zeros(k, dtype=dt, device=DEV) for _ in range(tensors)]
+                           for k, dt in ((n, F32), (n, torch.uint8), (n, torch.uint8), (16, torch.uint8), (16, torch.uint8)))
+        gba.gba_adamw(gba.gba_adamw_list(p, [g] * tensors, m, v, me, ve), 0.0, 0.9, 0.9, 1e-8, 0.0, t, seed=seed)
+        return m
+    base = codes(1, 1)[0]
+    assert torch.equal(base, codes(1, 1)[0])
+    two = codes(1, 1, 2)
+    for other in (codes(2, 1)[0], codes(1, 2)[0], two[1]):
+        assert 0.2 < float((other != base).float().mean()) < 0.6
+    assert torch.equal(two[0], base)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_in_a_graph_with_the_step_on_the_device(eight):
+    def make():
+        return Case([3000, 41], [BF16, F32], eight, copies=[BF16, None])
+    c, eager = make(), make()
+    t, coef = torch.zeros(1, dtype=torch.int64, device=DEV), torch.tensor([0.5], device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        t.add_(1)
+        gba.gba_adamw(c.list, **HP, t=99, t_device=t, seed=3, coef=coef, err=c.err)
+    other = torch.cuda.Stream()
+    for k in range(1, 5):
+        graph.replay()
+        torch.cuda.synchronize()
+        gba.gba_adamw(eager.list, **HP, t=k, seed=3, coef=coef, err=eager.err, stream=other)
+        other.synchronize()
+        for a, b in zip((*c.p, *c.m, *c.v, c.copies[0]), (*eager.p, *eager.m, *eager.v, eager.copies[0])):
+            assert torch.equal(a, b), k
+    t.fill_(-5)   # counts as 1
+    gba.gba_adamw(c.list, **HP, t=99, t_device=t, seed=3)
+    assert torch.isfinite(c.p[0]).all()
+
+
+def test_it_finds_a_minimum_with_both_kinds_of_moments():
+    """The gradients of a quadratic: runs, and every parameter moves towards its target."""
+    for eight in (False, True):
+        torch.manual_seed(1)
+        n = 1000
+        target, p = torch.randn(n, device=DEV), torch.zeros(n, device=DEV)
+        start = p.clone()
+        g = torch.zeros(n, device=DEV)
+        dt = torch.uint8 if eight else F32
+        m, v = torch.zeros(n, dtype=dt, device=DEV), torch.zeros(n, dtype=dt, device=DEV)
+        e = dict(m_exps=[torch.zeros(4, dtype=torch.uint8, device=DEV)], v_exps=[torch.zeros(4, dtype=torch.uint8, device=DEV)]) if eight else {}
+        lst = gba.gba_adamw_list([p], [g], [m], [v], **e)
+        for t in range(1, 11):
+            g.copy_(p - target)
+            gba.gba_adamw(lst, 1e-3, 0.9, 0.999, 1e-8, 0.0, t)
+        far = (target.abs() > 0.05)
+        assert (((p - start) * target)[far] > 0).all()
+
+
+@pytest.mark.parametrize("n", [1, 4, 255, 256, 1001, 5 * (1 << 20) + 3])
+def test_what_moments_stand_for(n):
+    rng = np.random.default_rng(n)
+    code, exp = rng.integers(0, 256, n).astype(np.uint8), rng.integers(0, 255, -(-n // 256)).astype(np.uint8)
+    for which, mantissa in ((gba.MOMENT_M, 3), (gba.MOMENT_V, 4)):
+        out = torch.full((n + 1,), 7.0, device=DEV)
+        gba.gba_moments_read(_dev(code), _dev(exp), which, out)
+        assert np.array_equal(out[:n].cpu().numpy(), decode(code, exp, mantissa).astype(np.float32)) and float(out[n]) == 7.0
+
+
+def test_nothing_to_do():
+    lst = gba.gba_adamw_list([], [], [], [])
+    gba.gba_adamw(lst, **HP, t=1)
+    e = torch.empty(0, device=DEV)
+    b = torch.empty(0, dtype=torch.uint8, device=DEV)
+    gba.gba_moments_read(b, b, gba.MOMENT_M, e)
+    gba.gba_adamw(gba.gba_adamw_list([e], [e], [e], [e]), **HP, t=1)
+
+
+def test_refusals():
+    p, b = torch.zeros(300, device=DEV), torch.zeros(300, dtype=torch.uint8, device=DEV)
+    lst = gba.gba_adamw_list([p], [p], [p], [p])
+    L, step = gba.gba_adamw_list, gba.gba_adamw
+    for bad in [lambda: L([p], [p], [p], []), lambda: L([p.half()], [p], [p], [p]), lambda: L([p], [p[:299]], [p], [p]),
+                lambda: L([p], [p.double()], [p], [p]), lambda: L([p], [p], [p[:299]], [p]), lambda: L([p], [p], [b], [b]),
+                lambda: L([p], [p], [b], [b], [b[:1]], [b]), lambda: L([p], [p], [b], [p], [b], [b]),
+                lambda: L([p], [p], [p], [p], [b], [b]), lambda: L([p], [p], [p], [p], copies=[p[:5]]),
+                lambda: L([p[::2]], [p[::2]], [p[::2]], [p[::2]]), lambda: L([p.cpu()], [p], [p], [p]),
+                lambda: L([p], [p], [p], [p], decays=[float("nan")]),
+                lambda: gba.gba_moments_read(b, b[:1], gba.MOMENT_M, p), lambda: gba.gba_moments_read(b, b, 2, p),
+                lambda: gba.gba_moments_read(b, b, gba.MOMENT_V, p[:299]),
+                lambda: step(lst, **{**HP, "beta1": 1.0}, t=1), lambda: step(lst, **{**HP, "beta2": -0.1}, t=1),
+                lambda: step(lst, **{**HP, "eps": 0.0}, t=1), lambda: step(lst, **{**HP, "lr": float("inf")}, t=1),
+                lambda: step(lst, **HP, t=0), lambda: step(lst, **HP, t=1, coef=torch.ones(1)),
+                lambda: step(lst, **HP, t=1, t_device=torch.ones(1, dtype=torch.int32, device=DEV))]:
+        with pytest.raises(gba.GBAError):
+            bad()
