@@ -13,8 +13,9 @@
 // takes the initial state instead of what comes before it, so the map of
 // positions that hold a first step forgets the state (a flag, not F = 0: an
 // infinity of one sequence stays there).  A block goes from tile to tile with
-// the state.  The gradient is the same from the end to the front, its first
-// steps the sequences' last ones.
+// the state, and loads the next tile before it joins the maps of this one.
+// The gradient is the same from the end to the front, its first steps the
+// sequences' last ones.
 //
 // Blocks take whole sequences where there are enough of them.  Of few long
 // ones each is cut into parts of equal length, the maps of all parts are made
@@ -27,33 +28,34 @@
 
 namespace gba {
 
-constexpr int kScanV = 4;                 // columns of a lane
-constexpr int64_t kScanMaxParts = 512;    // most parts of the positions, times the groups of columns
-constexpr int kScanMapBlock = 256;
+constexpr int kScanBlock = 256;
+constexpr int kScanWaves = kScanBlock / kWave;
+constexpr int kScanV = 4;                  // columns of a lane
+constexpr int kScanLanes = 32;             // most lanes over the columns of a block
+constexpr int kScanWidest = kScanLanes * kScanV;
+constexpr int kScanSimd = 2;               // waves of a SIMD that the registers are for
+constexpr int64_t kScanBlocks = 256 * kScanSimd;   // ... and so the blocks of a round, a wave of each on every SIMD
+constexpr int64_t kScanSplitBelow = 192;   // blocks
 
 __host__ __device__ static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 static inline size_t align_up(size_t x) { return (x + 255) & ~size_t(255); }
 
 // ---------------------------------------------------------------- the gate
-// The smaller of f and 1 - f, held with all its bits: t = 1 - f, or -f.
-// (which of the two the sign bit says: either may be 0)
-__device__ __forceinline__ float gate_of(float a) {
-  // e^-|a| as a power of two; what its rounded exponent leaves out is put back as a factor near 1
+// f = sigmoid(a) and i = 1 - f, each within a few u of itself, or (not FINE:
+// 16-bit types, whose values carry 2^-9 or 2^-12 anyway) |a| u more.
+template <bool FINE>
+__device__ __forceinline__ void gate_of(float a, float& f, float& i) {
   const float y = -1.44269504f * fabsf(a);
-  const float rest = __builtin_fmaf(-1.44269504f, fabsf(a), -y) - 1.92596299e-8f * fabsf(a);
   float e = __builtin_amdgcn_exp2f(y);
-  e = y > -126.0f ? __builtin_fmaf(e, 0.693147181f * rest, e) : e;   // (rest is not a number where a is infinite)
-  return __builtin_copysignf(e * __builtin_amdgcn_rcpf(1.0f + e), a);
+  if constexpr (FINE) {   // what y's rounding leaves out is put back as a factor near 1
+    const float rest = __builtin_fmaf(-1.92596299e-8f, fabsf(a), __builtin_fmaf(-1.44269504f, fabsf(a), -y));
+    e = y > -126.0f ? __builtin_fmaf(e, 0.693147181f * rest, e) : e;   // (rest is not a number where a is infinite)
+  }
+  const float big = __builtin_amdgcn_rcpf(1.0f + e), small = e * big;
+  const bool holds = a >= 0.0f;
+  f = holds ? big : small;
+  i = holds ? small : big;
 }
-__device__ __forceinline__ bool gate_holds(float t) { return __float_as_int(t) >= 0; }
-__device__ __forceinline__ float gate_f(float t) { return gate_holds(t) ? 1.0f - t : -t; }
-__device__ __forceinline__ float gate_i(float t) { return gate_holds(t) ? t : 1.0f + t; }
-// f h + (1 - f) x, one rounding beside that of the difference
-__device__ __forceinline__ float gate_step(float t, float h, float x) {
-  return __builtin_fmaf(t, x - h, gate_holds(t) ? h : x);
-}
-// f g
-__device__ __forceinline__ float gate_back(float t, float g) { return __builtin_fmaf(-t, g, gate_holds(t) ? g : 0.0f); }
 
 // ------------------------------------------------------ which sequence
 // Packed sequences: the sequence of every position (-1 behind the last), and
@@ -66,10 +68,10 @@ struct ScanMapArgs {
   int64_t n, B, D;
   int32_t* err;
 };
-__global__ void __launch_bounds__(kScanMapBlock)
+__global__ void __launch_bounds__(kScanBlock)
 scan_map_kernel(ScanMapArgs a) {
-  const int64_t stride = (int64_t)gridDim.x * kScanMapBlock;
-  const int64_t first = (int64_t)blockIdx.x * kScanMapBlock + threadIdx.x;
+  const int64_t stride = (int64_t)gridDim.x * kScanBlock;
+  const int64_t first = (int64_t)blockIdx.x * kScanBlock + threadIdx.x;
   for (int64_t p = first; p < a.n; p += stride) {
     int64_t lo = 0, hi = a.B;   // the last b with offsets[b] <= p, of lo .. hi - 1
     while (hi - lo > 1) {
@@ -96,8 +98,9 @@ struct ScanArgs {
   const int32_t* seq;      // packed: the sequence of each position; null: equal lengths
   int32_t length;          // ... of this many positions
   int32_t groups;          // of columns
-  int32_t parts;           // of the sequences, or of the positions
-  int32_t part_len;        // positions of a part; 0: parts are whole sequences
+  int32_t parts;           // of the positions
+  int32_t part_len;        // positions of a part
+  bool split;              // parts are cut through sequences
   float* part_F;           // [parts][D] the parts' maps
   float* part_S;
   int32_t* part_forget;    // [parts][groups]
@@ -105,12 +108,13 @@ struct ScanArgs {
 };
 
 // One map over V columns.
+template <int V>
 struct Affine {
-  float F[kScanV], S[kScanV];
+  float F[V], S[V];
   bool forget;             // the state before it does not matter
   __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int e = 0; e < kScanV; ++e) {
+    for (int e = 0; e < V; ++e) {
       F[e] = 1.0f;
       S[e] = 0.0f;
     }
@@ -119,50 +123,74 @@ struct Affine {
   // this after `before`
   __device__ __forceinline__ void after(const Affine& before) {
 #pragma unroll
-    for (int e = 0; e < kScanV; ++e) {
+    for (int e = 0; e < V; ++e) {
       S[e] = forget ? S[e] : __builtin_fmaf(F[e], before.S[e], S[e]);
       F[e] *= before.F[e];
     }
     forget |= before.forget;
   }
-  __device__ __forceinline__ void apply(float (&h)[kScanV]) const {
+  __device__ __forceinline__ void apply(float (&h)[V]) const {
 #pragma unroll
-    for (int e = 0; e < kScanV; ++e) h[e] = forget ? S[e] : __builtin_fmaf(F[e], h[e], S[e]);
+    for (int e = 0; e < V; ++e) h[e] = forget ? S[e] : __builtin_fmaf(F[e], h[e], S[e]);
   }
 };
 
-// How a tile lies over a block: LPC lanes over the columns of a group, SLOTS
-// groups of lanes over the positions, T positions each.
-template <int BLOCK, int LPC, int T>
+// Positions of a lane.
+template <bool GRAD>
+constexpr int kScanT = GRAD ? 4 : 8;
+
+// How a tile lies over a block: LPC lanes with V columns each over the columns
+// of a group, SLOTS groups of lanes over the positions, T positions each.
+template <int LPC, int V, int T>
 struct ScanShape {
-  static constexpr int WAVES = BLOCK / kWave;
   static constexpr int PER = kWave / LPC;       // slots of a wave
-  static constexpr int SLOTS = BLOCK / LPC;
+  static constexpr int SLOTS = kScanBlock / LPC;
   static constexpr int TILE = SLOTS * T;
-  static constexpr int COLUMNS = LPC * kScanV;
+  static constexpr int COLUMNS = LPC * V;
 };
 
-template <int BLOCK, int LPC, int T>
+// A lane's columns.  The last lane's are moved back to end at the row's end:
+// its first `shift` columns are other lanes' (all V past the end), which it
+// computes as they do and does not store.
+template <int V>
+struct ScanColumns {
+  int at, shift;
+  __device__ __forceinline__ ScanColumns(int c, int D) {
+    at = c + V > D ? D - V : c;
+    shift = c - at < V ? c - at : V;
+  }
+  // p: the lane's first column
+  template <typename X>
+  __device__ __forceinline__ void store(X* __restrict__ p, const float (&o)[V]) const {
+    if (shift == 0) {
+      store_vec<X, V, true>(p, o);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (e >= shift) p[e] = (X)o[e];
+    }
+  }
+};
+
+template <int LPC, int V>
 struct ScanShared {
-  typedef ScanShape<BLOCK, LPC, T> Sh;
-  float F[2][Sh::WAVES][Sh::COLUMNS], S[2][Sh::WAVES][Sh::COLUMNS];
-  int forget[2][Sh::WAVES];
+  float F[2][kScanWaves][LPC * V], S[2][kScanWaves][LPC * V];
+  int forget[2][kScanWaves];
 };
 
 // Joins the slots' maps: leaves in `in` the state that this slot's positions
 // are entered with and in `carry` (before: the tile's first) the state after the
-// tile.  `waves`: how many of them hold positions.
-template <int BLOCK, int LPC, int T, bool MAP>
-__device__ __forceinline__ void scan_join(Affine& m, Affine& carry, float (&in)[kScanV], int waves, int& buffer,
-                                          ScanShared<BLOCK, LPC, T>& s) {
-  typedef ScanShape<BLOCK, LPC, T> Sh;
+// tile.
+template <int LPC, int V, bool MAP>
+__device__ __forceinline__ void scan_join(Affine<V>& m, Affine<V>& carry, float (&in)[V], int& buffer,
+                                          ScanShared<LPC, V>& s) {
   const int lane = lane_id(), w = threadIdx.x / kWave, cl = lane % LPC;
   // inclusive over the slots of the wave
 #pragma unroll
   for (int off = LPC; off < kWave; off <<= 1) {
-    Affine b;
+    Affine<V> b;
 #pragma unroll
-    for (int e = 0; e < kScanV; ++e) {
+    for (int e = 0; e < V; ++e) {
       b.F[e] = __shfl_up(m.F[e], off, kWave);
       b.S[e] = __shfl_up(m.S[e], off, kWave);
     }
@@ -171,23 +199,34 @@ __device__ __forceinline__ void scan_join(Affine& m, Affine& carry, float (&in)[
   }
   if (lane >= kWave - LPC) {
 #pragma unroll
-    for (int e = 0; e < kScanV; ++e) {
-      s.F[buffer][w][cl * kScanV + e] = m.F[e];
-      s.S[buffer][w][cl * kScanV + e] = m.S[e];
+    for (int e = 0; e < V; ++e) {
+      s.F[buffer][w][cl * V + e] = m.F[e];
+      s.S[buffer][w][cl * V + e] = m.S[e];
     }
-    if (cl == 0) s.forget[buffer][w] = m.forget;   // (the first lane has columns, the last may have none)
+    if (cl == 0) s.forget[buffer][w] = m.forget;
+  }
+  // exclusive: what the slots before this one do
+  Affine<V> x;
+  if constexpr (!MAP) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      x.F[e] = __shfl_up(m.F[e], LPC, kWave);
+      x.S[e] = __shfl_up(m.S[e], LPC, kWave);
+    }
+    x.forget = __shfl_up((int)m.forget, LPC, kWave) != 0;
   }
   __syncthreads();
-  for (int k = 0; k < waves; ++k) {
+#pragma unroll
+  for (int k = 0; k < kScanWaves; ++k) {
     if (k == w) {
 #pragma unroll
-      for (int e = 0; e < kScanV; ++e) in[e] = carry.S[e];
+      for (int e = 0; e < V; ++e) in[e] = carry.S[e];
     }
-    Affine b;
+    Affine<V> b;
 #pragma unroll
-    for (int e = 0; e < kScanV; ++e) {
-      b.F[e] = s.F[buffer][k][cl * kScanV + e];
-      b.S[e] = s.S[buffer][k][cl * kScanV + e];
+    for (int e = 0; e < V; ++e) {
+      b.F[e] = s.F[buffer][k][cl * V + e];
+      b.S[e] = s.S[buffer][k][cl * V + e];
     }
     b.forget = s.forget[buffer][k] != 0;
     if constexpr (MAP) {
@@ -198,186 +237,257 @@ __device__ __forceinline__ void scan_join(Affine& m, Affine& carry, float (&in)[
     }
   }
   buffer ^= 1;
-  if constexpr (Sh::PER > 1 && !MAP) {
-    // exclusive: what the slots before this one do
-    Affine b;
-#pragma unroll
-    for (int e = 0; e < kScanV; ++e) {
-      b.F[e] = __shfl_up(m.F[e], LPC, kWave);
-      b.S[e] = __shfl_up(m.S[e], LPC, kWave);
-    }
-    b.forget = __shfl_up((int)m.forget, LPC, kWave) != 0;
-    if (lane >= LPC) b.apply(in);
-  }
+  if constexpr (!MAP)
+    if (lane >= LPC) x.apply(in);
 }
 
 // The state that part `part` of the positions is entered with (in carry.S):
-// the maps of the `before` parts in front of it (front to back, or with BACK
-// back to front), each wave a share of them.
-template <int BLOCK, int LPC, int T, bool BACK>
-__device__ __forceinline__ void enter_part(const ScanArgs& a, int part, int group, int c0, int count, Affine& carry,
-                                           int& buffer, ScanShared<BLOCK, LPC, T>& s) {
-  typedef ScanShape<BLOCK, LPC, T> Sh;
+// the maps of the parts in front of it (front to back, or with BACK back to
+// front), each slot a share of them.
+template <int LPC, int V, bool BACK>
+__device__ __forceinline__ void enter_part(const ScanArgs& a, int part, int group, int col, Affine<V>& carry, int& buffer,
+                                           ScanShared<LPC, V>& s) {
+  constexpr int SLOTS = kScanBlock / LPC;
   const int before = BACK ? a.parts - 1 - part : part;
-  const int w = threadIdx.x / kWave;
-  const int lo = (int)((int64_t)before * w / Sh::WAVES), hi = (int)((int64_t)before * (w + 1) / Sh::WAVES);
-  Affine m;
+  const int slot = threadIdx.x / LPC;
+  const int lo = (int)((int64_t)before * slot / SLOTS), hi = (int)((int64_t)before * (slot + 1) / SLOTS);
+  Affine<V> m;
   m.clear();
-  // (the lanes of a wave's first slot alone; the others hand on the identity)
-  if (lane_id() < LPC) {
 #pragma unroll 4
-    for (int k = lo; k < hi; ++k) {
-      const int j = BACK ? a.parts - 1 - k : k;
-      Affine b;
-      b.clear();
-      if (count > 0) {
-        load_part<float, kScanV>(a.part_F + (int64_t)j * a.r.D + c0, count, b.F);
-        load_part<float, kScanV>(a.part_S + (int64_t)j * a.r.D + c0, count, b.S);
-      }
-      b.forget = a.part_forget[(int64_t)j * a.groups + group] != 0;
-      b.after(m);
-      m = b;
-    }
+  for (int k = lo; k < hi; ++k) {
+    const int j = BACK ? a.parts - 1 - k : k;
+    Affine<V> b;
+    load_vec<float, V>(a.part_F + (int64_t)j * a.r.D + col, b.F);
+    load_vec<float, V>(a.part_S + (int64_t)j * a.r.D + col, b.S);
+    b.forget = a.part_forget[(int64_t)j * a.groups + group] != 0;
+    b.after(m);
+    m = b;
   }
-  float unused[kScanV];
-  scan_join<BLOCK, LPC, T, false>(m, carry, unused, Sh::WAVES, buffer, s);
+  float unused[V];
+  scan_join<LPC, V, false>(m, carry, unused, buffer, s);
+}
+
+// Where the first sequence that begins at position p or behind it begins.
+__device__ __forceinline__ int64_t next_start(const ScanArgs& a, int64_t p) {
+  if (p <= 0 || p >= a.r.n) return p <= 0 ? 0 : a.r.n;
+  const int32_t here = a.seq[p];
+  if (here != a.seq[p - 1]) return p;
+  if (here < 0) return a.r.n;
+  const int64_t end = a.r.offsets[here + 1];
+  return end < a.r.n ? end : a.r.n;   // (behind p, whatever the offsets)
+}
+
+// Where a block is in the order of parts and groups: blocks go to the eight dies
+// in turn, and neighbours, which read the same rows, come to one die.
+__device__ __forceinline__ unsigned block_place() {
+  constexpr unsigned kDies = 8;
+  const unsigned n = gridDim.x, each = n / kDies, more = n % kDies, die = blockIdx.x % kDies;
+  return die * each + (die < more ? die : more) + blockIdx.x / kDies;
 }
 
 // The positions that a block takes.
 __device__ __forceinline__ void part_range(const ScanArgs& a, int part, int64_t& p0, int64_t& p1) {
-  const int64_t n = a.r.n, B = a.r.B;
-  if (a.part_len) {
-    p0 = (int64_t)part * a.part_len;
-    p1 = p0 + a.part_len;
-    int64_t end = n;
-    if (a.seq) {
-      end = a.r.offsets[B];
-      end = end < 0 ? 0 : end > n ? n : end;
-    }
-    if (p1 > end) p1 = end;
-    return;
-  }
-  const int64_t b0 = B * part / a.parts, b1 = B * (part + 1) / a.parts;
+  p0 = (int64_t)part * a.part_len;
+  p1 = p0 + a.part_len;
+  int64_t end = a.r.n;
   if (a.seq) {
-    p0 = a.r.offsets[b0];
-    p1 = a.r.offsets[b1];
-    p0 = p0 < 0 ? 0 : p0;
-    p1 = p1 > n ? n : p1;
-  } else {
-    p0 = b0 * a.length;
-    p1 = b1 * a.length;
+    if (!a.split) {
+      p0 = next_start(a, p0);
+      p1 = next_start(a, p1);
+    }
+    end = a.r.offsets[a.r.B];
+    end = end < 0 ? 0 : end > a.r.n ? a.r.n : end;
   }
+  if (p1 > end) p1 = end;
+  p0 = __builtin_amdgcn_readfirstlane((int)p0);   // (the same in every lane, also to the compiler)
+  p1 = __builtin_amdgcn_readfirstlane((int)p1);
 }
 
-// Which of T positions from q on begin or end a sequence (bits), and the
-// sequence of the first.
+// Which of T positions from q on begin and end a sequence, as bits.
 template <int T>
 struct Bounds {
   uint32_t starts, ends;
-  int32_t seq[T];
-  __device__ __forceinline__ void find(const ScanArgs& a, int64_t q, int count) {
-    starts = ends = 0;
-    if (count <= 0) return;
-    if (!a.seq) {
-      int32_t b = (int32_t)((uint32_t)q / (uint32_t)a.length);
-      int32_t r = (int32_t)q - b * a.length;
+  int32_t seq[T + 2];      // packed: the sequences of the position before, of the T and of the one behind
+  // (positions below 0 and from n on are not looked at by `find`)
+  __device__ __forceinline__ void load(const ScanArgs& a, int64_t q) {
+    if (!a.seq) return;
+    const int64_t last = a.r.n - 1;
+    if (q >= 1 && q + T <= last) {
 #pragma unroll
-      for (int i = 0; i < T; ++i) {
-        seq[i] = b;
-        if (r == 0) starts |= 1u << i;
-        if (r == a.length - 1) ends |= 1u << i;
-        if (++r == a.length) {
-          r = 0;
-          ++b;
-        }
-      }
-      return;
-    }
-    int32_t last = q > 0 ? a.seq[q - 1] : -2;   // (position 0 begins a sequence whatever the offsets)
-    int32_t now = a.seq[q];
+      for (int i = 0; i < T + 2; ++i) seq[i] = a.seq[q - 1 + i];
+    } else {
 #pragma unroll
-    for (int i = 0; i < T; ++i) {
-      if (i < count) {
-        const int32_t next = q + i + 1 < a.r.n ? a.seq[q + i + 1] : -1;
-        seq[i] = now < 0 ? 0 : now;   // (offsets that are not in order alone have such positions)
-        if (now != last) starts |= 1u << i;
-        if (now != next) ends |= 1u << i;
-        last = now;
-        now = next;
+      for (int i = 0; i < T + 2; ++i) {
+        const int64_t p = q - 1 + i;
+        seq[i] = a.seq[p < 0 ? 0 : p > last ? last : p];
+        if (p < 0 || p > last) seq[i] = -2;   // (position 0 begins a sequence whatever the offsets)
       }
     }
   }
+  // of positions q + from .. q + to - 1
+  __device__ __forceinline__ void find(const ScanArgs& a, int64_t q, int from, int to) {
+    starts = ends = 0;
+    if (a.seq) {
+#pragma unroll
+      for (int i = 0; i < T; ++i) {
+        if (seq[i + 1] != seq[i]) starts |= 1u << i;
+        if (seq[i + 1] != seq[i + 2]) ends |= 1u << i;
+      }
+    } else {
+      const int32_t p = (int32_t)(q < 0 ? 0 : q);   // (only those below 0 are wrong, and masked)
+      int32_t r = p - (int32_t)((uint32_t)p / (uint32_t)a.length) * a.length - (int32_t)(p - q);
+#pragma unroll
+      for (int i = 0; i < T; ++i) {
+        if (r == 0) starts |= 1u << i;
+        if (r == a.length - 1) ends |= 1u << i;
+        r = r == a.length - 1 ? 0 : r + 1;
+      }
+    }
+    const uint32_t mask = (to <= 0 ? 0u : (1u << to) - 1) & ~((1u << from) - 1);
+    starts &= mask;
+    ends &= mask;
+  }
+  static __device__ __forceinline__ int64_t sequence(const ScanArgs& a, int64_t p) {
+    if (!a.seq) return (uint32_t)p / (uint32_t)a.length;
+    const int32_t b = a.seq[p];
+    return b < 0 ? 0 : b;   // (offsets that are not in order alone have such positions)
+  }
 };
 
-template <typename X, int BLOCK, int LPC, int T, bool MAP>
-__global__ void __launch_bounds__(BLOCK)
+// A lane's place in a matrix, in bytes from a tile's first row: `slot` and
+// column.  The rows of a tile are then at a uniform address each, to which this
+// is added (the compiler would otherwise hold a pointer per row and matrix in
+// registers, twice as many as the tile itself takes).
+template <typename X>
+__device__ __forceinline__ uint64_t lane_place(int64_t stride, int64_t row, int col) {
+  return (uint64_t)(row * stride + col) * sizeof(X);
+}
+__device__ __forceinline__ void keep_place(uint64_t& place) { asm volatile("" : "+v"(place)); }
+
+// A matrix's rows from a uniform one on.
+template <typename X>
+struct RowsFrom {
+  char* first;
+  int64_t step;   // bytes
+  __device__ __forceinline__ RowsFrom(const void* base, int64_t stride, int64_t row)
+      : first(const_cast<char*>(static_cast<const char*>(base)) + row * stride * (int64_t)sizeof(X)),
+        step(stride * (int64_t)sizeof(X)) {}
+  __device__ __forceinline__ X* at(int i, uint64_t place) const {
+    return reinterpret_cast<X*>(first + i * step + place);
+  }
+  template <int V>
+  __device__ __forceinline__ typename VecOf<X, V>::type load(int i, uint64_t place) const {
+    typedef typename VecOf<X, V>::type vec;
+    return __builtin_nontemporal_load(reinterpret_cast<const vec*>(at(i, place)));
+  }
+};
+
+template <typename X, int LPC, int V, int T, bool MAP>
+__global__ void __launch_bounds__(kScanBlock, kScanSimd)
 scan_kernel(ScanArgs a) {
-  typedef ScanShape<BLOCK, LPC, T> Sh;
-  constexpr int V = kScanV;
-  __shared__ ScanShared<BLOCK, LPC, T> s;
-  const int group = (int)blockIdx.x % a.groups, part = (int)blockIdx.x / a.groups;
-  const int slot = threadIdx.x / LPC, c0 = group * Sh::COLUMNS + (int)(threadIdx.x % LPC) * V;
-  const int count = a.r.D - c0;   // columns of this lane, V of them or fewer (none: <= 0)
+  typedef ScanShape<LPC, V, T> Sh;
+  typedef typename VecOf<X, V>::type vec;
+  __shared__ ScanShared<LPC, V> s;
+  const unsigned block = block_place();
+  const int group = (int)(block % (unsigned)a.groups), part = (int)(block / (unsigned)a.groups);
+  const int slot = threadIdx.x / LPC;
+  const ScanColumns<V> col(group * Sh::COLUMNS + (int)(threadIdx.x % LPC) * V, a.r.D);
   const float* first_state = a.state && !MAP ? a.state : a.r.h0;
   int64_t p0, p1;
   part_range(a, part, p0, p1);
   int buffer = 0;
-  Affine carry;
+  Affine<V> carry;
   carry.clear();
-  if constexpr (!MAP)
-    if (a.part_len && part > 0) enter_part<BLOCK, LPC, T, false>(a, part, group, c0, count, carry, buffer, s);
-  for (int64_t p = p0; p < p1; p += Sh::TILE) {
+  vec x[T] = {}, g[T] = {};
+  Bounds<T> at;
+  uint64_t place_x = lane_place<X>(a.r.x_stride, slot * T, col.at), place_a = lane_place<X>(a.r.a_stride, slot * T, col.at);
+  uint64_t place_h = lane_place<X>(a.r.h_stride, slot * T, col.at);
+  auto load = [&](int64_t p) {
+    keep_place(place_x);
+    keep_place(place_a);
     const int64_t q = p + slot * T;
-    const int here = count <= 0 ? 0 : p1 - q < T ? (int)(p1 - q) : T;   // positions of this slot (none: <= 0)
-    float t[T][V], x[T][V];
-#pragma unroll
-    for (int i = 0; i < T; ++i)
-      if (i < here) {
-        load_part<X, V>(static_cast<const X*>(a.r.x) + (q + i) * a.r.x_stride + c0, count, x[i]);
-        load_part<X, V>(static_cast<const X*>(a.r.a) + (q + i) * a.r.a_stride + c0, count, t[i]);
-      }
-    Bounds<T> at;
-    at.find(a, q, here);
-    Affine m;
-    m.clear();
-#pragma unroll
-    for (int i = 0; i < T; ++i) {
-      if (i >= here) continue;
-      const bool first = at.starts >> i & 1;
-      float h0[V] = {};
-      if (first && first_state) {
-        load_part<float, V>(first_state + (int64_t)at.seq[i] * a.r.D + c0, count, h0);
-        if (MAP && a.state) store_part<float, V>(a.state + (int64_t)at.seq[i] * a.r.D + c0, count, h0);
-      }
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        t[i][e] = gate_of(t[i][e]);
-        if (first) x[i][e] = gate_step(t[i][e], h0[e], x[i][e]);   // the state after the step
-        m.S[e] = first ? x[i][e] : gate_step(t[i][e], m.S[e], x[i][e]);
-        m.F[e] *= gate_f(t[i][e]);
-      }
-      m.forget |= first;
-    }
-    float h[V] = {};
-    const int64_t rest = ceil_div(p1 - p, Sh::PER * T);
-    scan_join<BLOCK, LPC, T, MAP>(m, carry, h, rest < Sh::WAVES ? (int)rest : Sh::WAVES, buffer, s);
-    if constexpr (!MAP) {
+    const RowsFrom<X> rows_a(a.r.a, a.r.a_stride, p), rows_x(a.r.x, a.r.x_stride, p);
+    if (p + Sh::TILE <= p1) {
 #pragma unroll
       for (int i = 0; i < T; ++i) {
-        if (i >= here) continue;
-        const bool first = at.starts >> i & 1;
+        g[i] = rows_a.template load<V>(i, place_a);
+        x[i] = rows_x.template load<V>(i, place_x);
+      }
+    } else {
 #pragma unroll
-        for (int e = 0; e < V; ++e) h[e] = first ? x[i][e] : gate_step(t[i][e], h[e], x[i][e]);
-        store_part<X, V>(static_cast<X*>(a.r.h) + (q + i) * a.r.h_stride + c0, count, h);
-        if (a.r.h_last && (at.ends >> i & 1))
-          store_part<float, V>(a.r.h_last + (int64_t)at.seq[i] * a.r.D + c0, count, h);
+      for (int i = 0; i < T; ++i) {
+        if (q + i >= p1) continue;
+        g[i] = rows_a.template load<V>(i, place_a);
+        x[i] = rows_x.template load<V>(i, place_x);
+      }
+    }
+    at.load(a, q);
+  };
+  if (p0 < p1) load(p0);
+  if constexpr (!MAP)
+    if (a.split && part > 0) enter_part<LPC, V, false>(a, part, group, col.at, carry, buffer, s);
+  for (int64_t p = p0; p < p1; p += Sh::TILE) {
+    const int64_t q = p + slot * T;
+    const int here = p1 - q < T ? (int)(p1 - q) : T;   // positions of this slot (none: <= 0)
+    float f[T][V], v[T][V];
+#pragma unroll
+    for (int i = 0; i < T; ++i)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        gate_of<sizeof(X) == 4>((float)g[i][e], f[i][e], v[i][e]);
+        v[i][e] *= (float)x[i][e];
+      }
+    // (what slots past the end compute goes nowhere: the tile is the last, and nobody enters with the last part's map)
+    at.find(a, q, 0, here);
+    const uint32_t starts = at.starts, ends = at.ends;
+    if (starts && first_state) {
+#pragma unroll
+      for (int i = 0; i < T; ++i) {
+        if (!(starts >> i & 1)) continue;
+        const int64_t to = Bounds<T>::sequence(a, q + i) * a.r.D;
+        float h0[V];
+        load_vec<float, V>(first_state + to + col.at, h0);
+        if (MAP && a.state) col.store(a.state + to + col.at, h0);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[i][e] = __builtin_fmaf(f[i][e], h0[e], v[i][e]);   // the state after the step
+      }
+    }
+    if (p + Sh::TILE < p1) load(p + Sh::TILE);
+    Affine<V> m;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      m.F[e] = f[0][e];
+      m.S[e] = v[0][e];
+    }
+#pragma unroll
+    for (int i = 1; i < T; ++i) {
+      const bool first = starts >> i & 1;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        m.S[e] = first ? v[i][e] : __builtin_fmaf(f[i][e], m.S[e], v[i][e]);
+        m.F[e] *= f[i][e];
+      }
+    }
+    m.forget = starts != 0;
+    float h[V];
+    scan_join<LPC, V, MAP>(m, carry, h, buffer, s);
+    if constexpr (!MAP) {
+      keep_place(place_h);
+      const RowsFrom<X> out(a.r.h, a.r.h_stride, p);
+#pragma unroll
+      for (int i = 0; i < T; ++i) {
+        const bool first = starts >> i & 1;
+#pragma unroll
+        for (int e = 0; e < V; ++e) h[e] = first ? v[i][e] : __builtin_fmaf(f[i][e], h[e], v[i][e]);
+        if (i < here) col.store(out.at(i, place_h), h);
+        if (a.r.h_last && (ends >> i & 1)) col.store(a.r.h_last + Bounds<T>::sequence(a, q + i) * a.r.D + col.at, h);
       }
     }
   }
   if constexpr (MAP) {
-    if ((int)threadIdx.x < LPC && count > 0) {
-      store_part<float, V>(a.part_F + (int64_t)part * a.r.D + c0, count, carry.F);
-      store_part<float, V>(a.part_S + (int64_t)part * a.r.D + c0, count, carry.S);
+    if ((int)threadIdx.x < LPC) {
+      store_vec<float, V>(a.part_F + (int64_t)part * a.r.D + col.at, carry.F);
+      store_vec<float, V>(a.part_S + (int64_t)part * a.r.D + col.at, carry.S);
     }
     if (threadIdx.x == 0) a.part_forget[(int64_t)part * a.groups + group] = carry.forget;
   }
@@ -385,132 +495,188 @@ scan_kernel(ScanArgs a) {
 
 // The gradient: positions from the end; slot 0 takes a tile's last ones.  The
 // state that runs through is f_t g_t, what a position hands to the one before it.
-template <typename X, int BLOCK, int LPC, int T, bool MAP>
-__global__ void __launch_bounds__(BLOCK)
+template <typename X, int LPC, int V, int T, bool MAP>
+__global__ void __launch_bounds__(kScanBlock, kScanSimd)
 scan_grad_kernel(ScanArgs a) {
-  typedef ScanShape<BLOCK, LPC, T> Sh;
-  constexpr int V = kScanV;
-  __shared__ ScanShared<BLOCK, LPC, T> s;
-  const int group = (int)blockIdx.x % a.groups, part = (int)blockIdx.x / a.groups;
-  const int slot = threadIdx.x / LPC, c0 = group * Sh::COLUMNS + (int)(threadIdx.x % LPC) * V;
-  const int count = a.r.D - c0;
+  typedef ScanShape<LPC, V, T> Sh;
+  typedef typename VecOf<X, V>::type vec;
+  __shared__ ScanShared<LPC, V> s;
+  const unsigned block = block_place();
+  const int group = (int)(block % (unsigned)a.groups), part = (int)(block / (unsigned)a.groups);
+  const int slot = threadIdx.x / LPC;
+  const ScanColumns<V> col(group * Sh::COLUMNS + (int)(threadIdx.x % LPC) * V, a.r.D);
   const float* last_grad = a.state && !MAP ? a.state : a.r.dh_last;
   int64_t p0, p1;
   part_range(a, part, p0, p1);
   int buffer = 0;
-  Affine carry;
+  Affine<V> carry;
   carry.clear();
-  if constexpr (!MAP)
-    if (a.part_len && part + 1 < a.parts) enter_part<BLOCK, LPC, T, true>(a, part, group, c0, count, carry, buffer, s);
-  for (int64_t p = p1; p > p0; p -= Sh::TILE) {
-    const int64_t q = p - (int64_t)(slot + 1) * T;   // positions q .. q + T - 1, those from p0 on
-    const int skip = q < p0 ? (p0 - q < T ? (int)(p0 - q) : T) : 0;
-    const bool any = count > 0 && skip < T;
-    float t[T][V], d[T][V], x[T][V], hp[T][V];
-    Bounds<T> at;
-    at.starts = at.ends = 0;
-    if (any) {
-      // (positions below p0, and below 0, are not of this slot)
-      const int64_t q0 = q + skip;
-      Bounds<T> b;
-      b.find(a, q0, T - skip);
-      at.starts = b.starts << skip;
-      at.ends = b.ends << skip;
-      // (the sequence of a position, as its place among the ones from q on)
+  vec gate[T] = {}, dh[T] = {}, x[T] = {}, before[T] = {};
+  Bounds<T> at;
+  // (a tile's last slot is its first one in memory)
+  const int back = (Sh::SLOTS - 1 - slot) * T;
+  uint64_t place_a = lane_place<X>(a.r.a_stride, back, col.at), place_d = lane_place<X>(a.r.dh_stride, back, col.at);
+  uint64_t place_x = lane_place<X>(a.r.x_stride, back, col.at), place_h = lane_place<X>(a.r.h_stride, back, col.at);
+  uint64_t place_dx = lane_place<X>(a.r.dx_stride, back, col.at), place_da = lane_place<X>(a.r.da_stride, back, col.at);
+  auto load = [&](int64_t p) {   // positions p - TILE .. p - 1, those from p0 on
+    keep_place(place_a);
+    keep_place(place_d);
+    keep_place(place_x);
+    keep_place(place_h);
+    const int64_t first = p - Sh::TILE, q = first + back;
+    const RowsFrom<X> rows_a(a.r.a, a.r.a_stride, first), rows_d(a.r.dh, a.r.dh_stride, first);
+    const RowsFrom<X> rows_x(a.r.x, a.r.x_stride, first), rows_h(a.r.h, a.r.h_stride, first - 1);
+    if (first >= p0 && first > 0) {
 #pragma unroll
       for (int i = 0; i < T; ++i) {
-        at.seq[i] = 0;
-#pragma unroll
-        for (int j = 0; j <= i; ++j)
-          if (i - j == skip) at.seq[i] = b.seq[j];
-      }
-#pragma unroll
-      for (int i = 0; i < T; ++i) {
-        if (i < skip) continue;
-        const int64_t r = q + i;
-        load_part<X, V>(static_cast<const X*>(a.r.dh) + r * a.r.dh_stride + c0, count, d[i]);
-        load_part<X, V>(static_cast<const X*>(a.r.a) + r * a.r.a_stride + c0, count, t[i]);
+        gate[i] = rows_a.template load<V>(i, place_a);
+        dh[i] = rows_d.template load<V>(i, place_d);
         if constexpr (!MAP) {
-          load_part<X, V>(static_cast<const X*>(a.r.x) + r * a.r.x_stride + c0, count, x[i]);
-          if (!(at.starts >> i & 1)) {
-            load_part<X, V>(static_cast<const X*>(a.r.h) + (r - 1) * a.r.h_stride + c0, count, hp[i]);
-          } else if (a.r.h0) {
-            load_part<float, V>(a.r.h0 + (int64_t)at.seq[i] * a.r.D + c0, count, hp[i]);
-          } else {
+          x[i] = rows_x.template load<V>(i, place_x);
+          before[i] = rows_h.template load<V>(i, place_h);
+        }
+      }
+    } else {
 #pragma unroll
-            for (int e = 0; e < V; ++e) hp[i][e] = 0.0f;
-          }
+      for (int i = 0; i < T; ++i) {
+        if (q + i < p0) continue;
+        gate[i] = rows_a.template load<V>(i, place_a);
+        dh[i] = rows_d.template load<V>(i, place_d);
+        if constexpr (!MAP) {
+          x[i] = rows_x.template load<V>(i, place_x);
+          if (q + i > 0) before[i] = rows_h.template load<V>(i, place_h);
         }
       }
     }
-    Affine m;
-    m.clear();
+    at.load(a, q);
+  };
+  if (p0 < p1) load(p1);
+  if constexpr (!MAP)
+    if (a.split && part + 1 < a.parts) enter_part<LPC, V, true>(a, part, group, col.at, carry, buffer, s);
+  for (int64_t p = p1; p > p0; p -= Sh::TILE) {
+    const int64_t q = p - Sh::TILE + back;
+    const int skip = q < p0 ? (p0 - q < T ? (int)(p0 - q) : T) : 0;
+    float f[T][V], in[T][V], d[T][V], diff[T][V];
 #pragma unroll
-    for (int i = T - 1; i >= 0; --i) {
-      if (!any || i < skip) continue;
-      const bool last = at.ends >> i & 1;
-      if (last && last_grad) {
+    for (int i = 0; i < T; ++i)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        gate_of<sizeof(X) == 4>((float)gate[i][e], f[i][e], in[i][e]);
+        d[i][e] = (float)dh[i][e];
+        if constexpr (!MAP) diff[i][e] = (float)before[i][e] - (float)x[i][e];
+      }
+    if (MAP && p - Sh::TILE < p0) {   // in front of the part (of a map, which is handed on): steps that do nothing
+#pragma unroll
+      for (int i = 0; i < T; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          f[i][e] = i < skip ? 1.0f : f[i][e];
+          d[i][e] = i < skip ? 0.0f : d[i][e];
+        }
+    }
+    at.find(a, q, skip, T);
+    const uint32_t starts = at.starts, ends = at.ends;
+    if (starts && !MAP) {
+#pragma unroll
+      for (int i = 0; i < T; ++i) {
+        if (!(starts >> i & 1)) continue;
+        float h0[V] = {};
+        if (a.r.h0) load_vec<float, V>(a.r.h0 + Bounds<T>::sequence(a, q + i) * a.r.D + col.at, h0);
+#pragma unroll
+        for (int e = 0; e < V; ++e) diff[i][e] = h0[e] - (float)x[i][e];
+      }
+    }
+    if (ends && last_grad) {
+#pragma unroll
+      for (int i = 0; i < T; ++i) {
+        if (!(ends >> i & 1)) continue;
+        const int64_t to = Bounds<T>::sequence(a, q + i) * a.r.D;
         float g[V];
-        load_part<float, V>(last_grad + (int64_t)at.seq[i] * a.r.D + c0, count, g);
-        if (MAP && a.state) store_part<float, V>(a.state + (int64_t)at.seq[i] * a.r.D + c0, count, g);
+        load_vec<float, V>(last_grad + to + col.at, g);
+        if (MAP && a.state) col.store(a.state + to + col.at, g);
 #pragma unroll
         for (int e = 0; e < V; ++e) d[i][e] += g[e];
       }
+    }
+    if (p - Sh::TILE > p0) load(p - Sh::TILE);
+    Affine<V> m;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      m.F[e] = f[T - 1][e];
+      m.S[e] = f[T - 1][e] * d[T - 1][e];
+    }
+#pragma unroll
+    for (int i = T - 2; i >= 0; --i) {
+      const bool last = ends >> i & 1;
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        t[i][e] = gate_of(t[i][e]);
-        m.S[e] = gate_back(t[i][e], last ? d[i][e] : d[i][e] + m.S[e]);
-        m.F[e] *= gate_f(t[i][e]);
+        m.S[e] = f[i][e] * (last ? d[i][e] : d[i][e] + m.S[e]);
+        m.F[e] *= f[i][e];
       }
-      m.forget |= last;
     }
-    float c[V] = {};
-    const int64_t rest = ceil_div(p - p0, Sh::PER * T);
-    scan_join<BLOCK, LPC, T, MAP>(m, carry, c, rest < Sh::WAVES ? (int)rest : Sh::WAVES, buffer, s);
+    m.forget = ends != 0;
+    float c[V];
+    scan_join<LPC, V, MAP>(m, carry, c, buffer, s);
     if constexpr (!MAP) {
+      keep_place(place_dx);
+      keep_place(place_da);
+      const RowsFrom<X> out_x(a.r.dx, a.r.dx_stride, p - Sh::TILE), out_a(a.r.da, a.r.da_stride, p - Sh::TILE);
 #pragma unroll
       for (int i = T - 1; i >= 0; --i) {
-        if (!any || i < skip) continue;
-        const bool last = at.ends >> i & 1;
+        const bool last = ends >> i & 1;
         float dx[V], da[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           const float g = last ? d[i][e] : d[i][e] + c[e];
-          const float small = fabsf(t[i][e]);
-          dx[e] = gate_i(t[i][e]) * g;
-          da[e] = g * (hp[i][e] - x[i][e]) * (small * (1.0f - small));
-          c[e] = gate_back(t[i][e], g);
+          dx[e] = in[i][e] * g;
+          da[e] = dx[e] * (diff[i][e] * f[i][e]);
+          c[e] = f[i][e] * g;
         }
-        store_part<X, V>(static_cast<X*>(a.r.dx) + (q + i) * a.r.dx_stride + c0, count, dx);
-        store_part<X, V>(static_cast<X*>(a.r.da) + (q + i) * a.r.da_stride + c0, count, da);
-        if (a.r.dh0 && (at.starts >> i & 1))
-          store_part<float, V>(a.r.dh0 + (int64_t)at.seq[i] * a.r.D + c0, count, c);
+        if (i >= skip) {
+          col.store(out_x.at(i, place_dx), dx);
+          col.store(out_a.at(i, place_da), da);
+        }
+        if (a.r.dh0 && (starts >> i & 1)) col.store(a.r.dh0 + Bounds<T>::sequence(a, q + i) * a.r.D + col.at, c);
       }
     }
   }
   if constexpr (MAP) {
-    if ((int)threadIdx.x < LPC && count > 0) {
-      store_part<float, V>(a.part_F + (int64_t)part * a.r.D + c0, count, carry.F);
-      store_part<float, V>(a.part_S + (int64_t)part * a.r.D + c0, count, carry.S);
+    if ((int)threadIdx.x < LPC) {
+      store_vec<float, V>(a.part_F + (int64_t)part * a.r.D + col.at, carry.F);
+      store_vec<float, V>(a.part_S + (int64_t)part * a.r.D + col.at, carry.S);
     }
     if (threadIdx.x == 0) a.part_forget[(int64_t)part * a.groups + group] = carry.forget;
   }
 }
 
-// ------------------------------------------------------------- launching
-constexpr int kScanBlock = 512;
-constexpr int kScanGradBlock = 512;
-constexpr int64_t kScanSplitBelow = 128;   // blocks
-
-// Lanes over the columns.
-static int scan_lanes(int32_t D) {
-  const int vecs = (int)std::min<int64_t>(ceil_div(D, kScanV), kWave);
-  int l = 4;
-  while (l < vecs) l *= 2;
-  return l;
+// One position of each of n sequences: a vector of columns a thread, `lanes` of
+// them over a row's columns.
+template <typename X, int V>
+__global__ void __launch_bounds__(kScanBlock)
+scan_step_kernel(RecurrenceArgs r, int lanes, int column_blocks) {
+  const int rows = kScanBlock / lanes;
+  const ScanColumns<V> col((int)((blockIdx.x % (unsigned)column_blocks) * lanes + threadIdx.x % lanes) * V, r.D);
+  if (col.shift == V) return;
+  const int64_t step = (int64_t)(gridDim.x / (unsigned)column_blocks) * rows;
+  for (int64_t b = (int64_t)(blockIdx.x / (unsigned)column_blocks) * rows + threadIdx.x / lanes; b < r.n; b += step) {
+    float x[V], g[V], h[V] = {};
+    load_vec<X, V>(static_cast<const X*>(r.a) + b * r.a_stride + col.at, g);
+    load_vec<X, V>(static_cast<const X*>(r.x) + b * r.x_stride + col.at, x);
+    if (r.h0) load_vec<float, V>(r.h0 + b * r.D + col.at, h);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      float f, i;
+      gate_of<sizeof(X) == 4>(g[e], f, i);
+      h[e] = __builtin_fmaf(f, h[e], i * x[e]);
+    }
+    col.store(static_cast<X*>(r.h) + b * r.h_stride + col.at, h);
+    if (r.h_last) col.store(r.h_last + b * r.D + col.at, h);
+  }
 }
-static int64_t scan_groups(int32_t D) { return ceil_div(D, (int64_t)scan_lanes(D) * kScanV); }
-static int64_t scan_most_parts(int32_t D) { return std::max<int64_t>(1, kScanMaxParts / scan_groups(D)); }
+
+// ------------------------------------------------------------- launching
+// The most parts that sequences are cut into: of blocks of the widest groups of columns.
+static int64_t scan_most_parts(int32_t D) { return std::max<int64_t>(1, kScanBlocks / ceil_div(D, kScanWidest)); }
 
 // The sequence of each position, the parts' maps, and the states of as many
 // sequences as are ever cut into parts.
@@ -525,60 +691,76 @@ static ScanRoom scan_room(int64_t n, int64_t B, int32_t D) {
     at += align_up(bytes);
     return here;
   };
-  const int64_t parts = scan_most_parts(D), groups = scan_groups(D);
+  const int64_t parts = scan_most_parts(D);
   r.seq = take((size_t)n * sizeof(int32_t));
   r.F = take((size_t)parts * D * sizeof(float));
   r.S = take((size_t)parts * D * sizeof(float));
-  r.forget = take((size_t)parts * groups * sizeof(int32_t));
+  r.forget = take((size_t)std::max<int64_t>(kScanBlocks, D) * sizeof(int32_t));   // (parts x groups)
   r.state = take((size_t)std::min(B, kScanSplitBelow) * D * sizeof(float));
   r.bytes = at + 256;
   return r;
 }
 size_t recurrence_workspace_bytes(int64_t n, int64_t B, int32_t D) { return scan_room(n, B, D).bytes; }
 
-template <typename X, int LPC, bool GRAD>
+template <typename X, int LPC, int V, bool GRAD>
 static hipError_t scan_in(ScanArgs a, void* ws, hipStream_t stream) {
-  constexpr int BLOCK = GRAD ? kScanGradBlock : kScanBlock;
-  constexpr int T = !GRAD && sizeof(X) == 2 ? 8 : 4;
-  typedef ScanShape<BLOCK, LPC, T> Sh;
+  constexpr int T = kScanT<GRAD>;
+  typedef ScanShape<LPC, V, T> Sh;
   const RecurrenceArgs& r = a.r;
   const int64_t tiles = ceil_div(r.n, Sh::TILE);
-  a.groups = (int32_t)scan_groups(r.D);
+  a.groups = (int32_t)ceil_div(r.D, Sh::COLUMNS);
   const ScanRoom room = scan_room(r.n, r.B, r.D);
   char* base = static_cast<char*>(ws);
-  a.part_len = 0;
-  a.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({r.B, tiles, 4096 / a.groups + 1}));
-  const int64_t most = scan_most_parts(r.D);
-  const bool split = r.B * a.groups < kScanSplitBelow && most > r.B && tiles > 2 * r.B;
-  if (split) {
-    const int64_t parts = std::min(most, tiles);
+  const int64_t most = std::max<int64_t>(1, kScanBlocks / a.groups);
+  a.split = r.B * a.groups < kScanSplitBelow && most > r.B && tiles > 2 * r.B;
+  const int64_t parts = std::min(most, tiles);
+  if (a.split) {
     a.part_len = (int32_t)(ceil_div(ceil_div(r.n, parts), Sh::TILE) * Sh::TILE);
-    a.parts = (int32_t)ceil_div(r.n, a.part_len);
     a.part_F = reinterpret_cast<float*>(base + room.F);
     a.part_S = reinterpret_cast<float*>(base + room.S);
     a.part_forget = reinterpret_cast<int32_t*>(base + room.forget);
     if (GRAD ? r.dh_last && r.dh0 : r.h0 && r.h_last) a.state = reinterpret_cast<float*>(base + room.state);
+  } else {
+    a.part_len = (int32_t)ceil_div(r.n, parts);
+    if (!a.seq) a.part_len = (int32_t)(ceil_div(a.part_len, a.length) * a.length);   // (no more than n)
   }
+  a.parts = (int32_t)ceil_div(r.n, a.part_len);
   const dim3 grid((unsigned)((int64_t)a.parts * a.groups));
   if constexpr (GRAD) {
-    if (split) hipLaunchKernelGGL((scan_grad_kernel<X, BLOCK, LPC, T, true>), grid, dim3(BLOCK), 0, stream, a);
-    hipLaunchKernelGGL((scan_grad_kernel<X, BLOCK, LPC, T, false>), grid, dim3(BLOCK), 0, stream, a);
+    if (a.split) hipLaunchKernelGGL((scan_grad_kernel<X, LPC, V, T, true>), grid, dim3(kScanBlock), 0, stream, a);
+    hipLaunchKernelGGL((scan_grad_kernel<X, LPC, V, T, false>), grid, dim3(kScanBlock), 0, stream, a);
   } else {
-    if (split) hipLaunchKernelGGL((scan_kernel<X, BLOCK, LPC, T, true>), grid, dim3(BLOCK), 0, stream, a);
-    hipLaunchKernelGGL((scan_kernel<X, BLOCK, LPC, T, false>), grid, dim3(BLOCK), 0, stream, a);
+    if (a.split) hipLaunchKernelGGL((scan_kernel<X, LPC, V, T, true>), grid, dim3(kScanBlock), 0, stream, a);
+    hipLaunchKernelGGL((scan_kernel<X, LPC, V, T, false>), grid, dim3(kScanBlock), 0, stream, a);
   }
+  return hipGetLastError();
+}
+
+template <typename X, int V>
+static hipError_t scan_step(const RecurrenceArgs& r, hipStream_t stream) {
+  const int64_t vecs = ceil_div(r.D, V);
+  int lanes = 1;
+  while (lanes < kScanBlock && lanes < vecs) lanes *= 2;
+  const int64_t columns = ceil_div(vecs, lanes), rows = kScanBlock / lanes;
+  const int64_t blocks = std::min(ceil_div(r.n, rows), std::max<int64_t>(1, (int64_t(1) << 20) / columns));
+  hipLaunchKernelGGL((scan_step_kernel<X, V>), dim3((unsigned)(blocks * columns)), dim3(kScanBlock), 0, stream, r, lanes,
+                     (int)columns);
   return hipGetLastError();
 }
 
 template <typename X, bool GRAD>
 static hipError_t scan_as(const ScanArgs& a, void* ws, hipStream_t stream) {
-  switch (scan_lanes(a.r.D)) {
-    case 4: return scan_in<X, 4, GRAD>(a, ws, stream);
-    case 8: return scan_in<X, 8, GRAD>(a, ws, stream);
-    case 16: return scan_in<X, 16, GRAD>(a, ws, stream);
-    case 32: return scan_in<X, 32, GRAD>(a, ws, stream);
-    default: return scan_in<X, 64, GRAD>(a, ws, stream);
-  }
+  constexpr int V = kScanV;
+  const int32_t D = a.r.D;
+  if (!GRAD && !a.seq && a.length == 1) return D < V ? scan_step<X, 1>(a.r, stream) : scan_step<X, V>(a.r, stream);
+  if (D < V) return scan_in<X, 4, 1, GRAD>(a, ws, stream);
+  if (D <= 4 * V) return scan_in<X, 4, V, GRAD>(a, ws, stream);
+  if (D <= 8 * V) return scan_in<X, 8, V, GRAD>(a, ws, stream);
+  // fewer columns to a block where the sequences are then enough blocks, and are too few for what memory takes at once
+  const int64_t blocks = a.r.B * ceil_div(D, kScanWidest);
+  const bool few = blocks * (int64_t)sizeof(X) < kScanBlocks * 2 && 2 * blocks >= kScanSplitBelow;
+  if (D <= 16 * V || few) return scan_in<X, 16, V, GRAD>(a, ws, stream);
+  return scan_in<X, kScanLanes, V, GRAD>(a, ws, stream);
 }
 
 template <bool GRAD>
@@ -597,8 +779,8 @@ static hipError_t launch_scan(const RecurrenceArgs& r, void* ws, int32_t* err, h
     m.err = err;
     a.seq = m.seq;
     const int64_t work = std::max<int64_t>(r.n, m.to ? r.B * kWave : r.B);
-    const int64_t blocks = std::min<int64_t>(ceil_div(work, kScanMapBlock), 1024);
-    hipLaunchKernelGGL(scan_map_kernel, dim3((unsigned)blocks), dim3(kScanMapBlock), 0, stream, m);
+    const int64_t blocks = std::min<int64_t>(ceil_div(work, kScanBlock), 1024);
+    hipLaunchKernelGGL(scan_map_kernel, dim3((unsigned)blocks), dim3(kScanBlock), 0, stream, m);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   } else if (r.n > 0) {
