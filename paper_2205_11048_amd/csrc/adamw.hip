@@ -29,9 +29,8 @@ constexpr int kAdamBlock = 256;
 constexpr int kAdamV = 4;                            // elements of a thread at a time: a wave takes one 8-bit block
 constexpr int kMomentBlock = kWave * kAdamV;         // elements that share an exponent
 static_assert(kMomentBlock == GBA_MOMENT_BLOCK, "a block of 8-bit moments is what a wave holds at a time");
-constexpr int kAdamVecs = 4;                         // vectors of a thread
-constexpr int kAdamwChunk = kAdamBlock * kAdamV * kAdamVecs;
-constexpr int64_t kAdamMaxBlocks = 2048;
+constexpr int kAdamwChunk = kAdamBlock * kAdamV;
+constexpr int64_t kAdamMaxBlocks = 1 << 17;
 
 struct AdamwChunk {
   float* param;        // the chunk's first element
@@ -155,129 +154,144 @@ __device__ __forceinline__ int block_exponent(uint32_t top) {
   return top == 0 ? 0 : E < 1 ? 1 : E > 254 ? 254 : E;
 }
 
+// The root of x >= 0, within an ulp, or EXACT: rounded to the nearest by one
+// step of Newton's from the reciprocal root (the residue x - s^2 is exact in one
+// fma).  The instructions do not know subnormal numbers: small x are scaled.
+template <bool EXACT>
+__device__ __forceinline__ float root_of(float x) {
+  const bool small = x < 0x1p-96f;
+  x *= small ? 0x1p64f : 1.0f;
+  float s;
+  if constexpr (EXACT) {
+    const float y = __builtin_amdgcn_rsqf(fmaxf(x, 0x1p-126f));   // (0 stays 0)
+    s = x * y;
+    s = __builtin_fmaf(__builtin_fmaf(-s, s, x), 0.5f * y, s);
+  } else {
+    s = __builtin_amdgcn_sqrtf(x);
+  }
+  return s * (small ? 0x1p-32f : 1.0f);
+}
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+constexpr uint32_t kInfinite = 0x7f800000u;   // magnitudes from here on are not finite
+
+template <typename T, int V>
+__device__ __forceinline__ void load_once(const T* __restrict__ p, int count, float (&o)[V]) {
+  if (count >= V) {
+    typedef typename VecOf<T, V>::type vec;
+    const vec v = __builtin_nontemporal_load(reinterpret_cast<const vec*>(p));
+#pragma unroll
+    for (int e = 0; e < V; ++e) o[e] = (float)v[e];
+  } else {
+    load_part<T, V>(p, count, o);
+  }
+}
+
 template <typename G, bool EIGHT>
 __device__ __forceinline__ void adamw_chunk(const AdamwChunk& c, const AdamwStep& s, float coef, uint32_t key,
                                             int32_t* err) {
-  constexpr int V = kAdamV, N = kAdamVecs;
+  constexpr int V = kAdamV;
   typedef uint8_t bytes __attribute__((ext_vector_type(V), aligned(1)));
-  float p[N][V], g[N][V], m[N][V], v[N][V];
-  int at[N], left[N];
-#pragma unroll
-  for (int k = 0; k < N; ++k) {
-    at[k] = (k * kAdamBlock + (int)threadIdx.x) * V;
-    left[k] = c.count - at[k];
-#pragma unroll
-    for (int e = 0; e < V; ++e) p[k][e] = g[k][e] = m[k][e] = v[k][e] = 0.0f;
-    if (left[k] <= 0) continue;
-    load_part<float, V>(c.param + at[k], left[k], p[k]);
-    load_part<G, V>(static_cast<const G*>(c.grad) + at[k], left[k], g[k]);
+  const int at = (int)threadIdx.x * V, left = c.count - at, block = at / kMomentBlock;
+  float p[V] = {}, g[V] = {}, m[V] = {}, v[V] = {};
+  bytes cm{}, cv{};
+  int Em = 0, Ev = 0;
+  if (left > 0) {
+    load_once<float, V>(c.param + at, left, p);
+    load_once<G, V>(static_cast<const G*>(c.grad) + at, left, g);
     if constexpr (!EIGHT) {
-      load_part<float, V>(static_cast<const float*>(c.m) + at[k], left[k], m[k]);
-      load_part<float, V>(static_cast<const float*>(c.v) + at[k], left[k], v[k]);
-    }
-  }
-  if constexpr (EIGHT) {
-    bytes cm[N], cv[N];
-    int Em[N], Ev[N];
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-      cm[k] = cv[k] = bytes{};
-      Em[k] = Ev[k] = 0;
-      if (left[k] <= 0) continue;
-      const uint8_t* a = static_cast<const uint8_t*>(c.m) + at[k];
-      const uint8_t* b = static_cast<const uint8_t*>(c.v) + at[k];
-      if (left[k] >= V) {
-        cm[k] = *reinterpret_cast<const bytes*>(a);
-        cv[k] = *reinterpret_cast<const bytes*>(b);
+      load_once<float, V>(static_cast<const float*>(c.m) + at, left, m);
+      load_once<float, V>(static_cast<const float*>(c.v) + at, left, v);
+    } else {
+      const uint8_t* a = static_cast<const uint8_t*>(c.m) + at;
+      const uint8_t* b = static_cast<const uint8_t*>(c.v) + at;
+      if (left >= V) {
+        cm = *reinterpret_cast<const bytes*>(a);
+        cv = *reinterpret_cast<const bytes*>(b);
       } else {
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          cm[k][e] = e < left[k] ? a[e] : 0;
-          cv[k][e] = e < left[k] ? b[e] : 0;
+          cm[e] = e < left ? a[e] : 0;
+          cv[e] = e < left ? b[e] : 0;
         }
       }
-      Em[k] = c.m_exp[at[k] / kMomentBlock];
-      Ev[k] = c.v_exp[at[k] / kMomentBlock];
+      Em = c.m_exp[block];
+      Ev = c.v_exp[block];
     }
-#pragma unroll
-    for (int k = 0; k < N; ++k)
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float x = decode<3>(cm[k][e] & 127u, Em[k]);
-        m[k][e] = cm[k][e] & 128u ? -x : x;
-        const float r = decode<4>(cv[k][e], Ev[k]);
-        v[k][e] = r * r;
-      }
   }
   const float keep = 1.0f - s.lr_wd * c.decay;
-  bool bad = false;
+  float mn[V], vn[V], root[V], pn[V];
+  uint32_t top_m = 0, top_v = 0;
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    float root[V];
+  for (int e = 0; e < V; ++e) {
+    if constexpr (EIGHT) {
+      const float y = decode<3>(cm[e] & 127u, Em);
+      m[e] = cm[e] & 128u ? -y : y;
+      const float r = decode<4>(cv[e], Ev);
+      v[e] = r * r;
+    }
+    const float x = g[e] * coef;
+    mn[e] = s.b1 * m[e] + s.omb1 * x;
+    vn[e] = s.b2 * v[e] + s.omb2 * (x * x);
+    // (8 bits: the rounded root, which the code is of; else within an ulp)
+    root[e] = root_of<EIGHT>(vn[e]);
+    const float step = (s.lr_m * mn[e]) * __builtin_amdgcn_rcpf(root[e] * s.r_scale + s.eps);
+    pn[e] = p[e] * keep - step;
+    top_m = max(top_m, magnitude(mn[e]));
+    top_v = max(top_v, magnitude(vn[e]));
+  }
+  if (max(top_m, top_v) >= kInfinite) {   // what is not finite stays as it was
+    raise_error(err, GBA_DERR_NONFINITE);
+    top_m = 0;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      const float x = g[k][e] * coef;
-      const float mn = s.b1 * m[k][e] + s.omb1 * x;
-      const float vn = s.b2 * v[k][e] + s.omb2 * (x * x);
-      const bool fine = isfinite(mn) && isfinite(vn);
-      bad |= !fine;
-      if (fine) {
-        m[k][e] = mn;
-        v[k][e] = vn;
-      }
-      // (8 bits: the rounded root, which the code is of; else within an ulp)
-      root[e] = EIGHT ? sqrtf(v[k][e]) : __builtin_amdgcn_sqrtf(v[k][e]);
-      const float step = (s.lr_m * mn) * __builtin_amdgcn_rcpf(root[e] * s.r_scale + s.eps);
-      if (fine) p[k][e] = p[k][e] * keep - step;
+      const bool fine = max(magnitude(mn[e]), magnitude(vn[e])) < kInfinite;
+      mn[e] = fine ? mn[e] : m[e];
+      vn[e] = fine ? vn[e] : v[e];
+      pn[e] = fine ? pn[e] : p[e];
+      root[e] = root_of<EIGHT>(vn[e]);
+      top_m = max(top_m, magnitude(mn[e]));
     }
-    if constexpr (EIGHT) {
-      uint32_t top_m = 0, top_r = 0;
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const uint32_t bm = __float_as_uint(m[k][e]) & 0x7fffffffu, br = __float_as_uint(root[e]);
-        top_m = bm > top_m ? bm : top_m;
-        top_r = br > top_r ? br : top_r;
-      }
-      const int Em = block_exponent<3>(wave_max(top_m)), Ev = block_exponent<4>(wave_max(top_r));
-      if (left[k] <= 0) continue;
-      const uint32_t here = mix_bits(key + c.block + (uint32_t)(at[k] / kMomentBlock));
-      bytes cm, cv;
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const uint32_t random = mix_bits(here + (uint32_t)(at[k] % kMomentBlock + e));
-        cm[e] = (uint8_t)(encode<3>(fabsf(m[k][e]), Em, random & 0xffffu) | (m[k][e] < 0.0f ? 128u : 0u));
-        cv[e] = (uint8_t)encode<4>(root[e], Ev, random >> 16);
-      }
-      uint8_t* a = static_cast<uint8_t*>(c.m) + at[k];
-      uint8_t* b = static_cast<uint8_t*>(c.v) + at[k];
-      if (left[k] >= V) {
-        *reinterpret_cast<bytes*>(a) = cm;
-        *reinterpret_cast<bytes*>(b) = cv;
-      } else {
-#pragma unroll
-        for (int e = 0; e < V; ++e)
-          if (e < left[k]) {
-            a[e] = cm[e];
-            b[e] = cv[e];
-          }
-      }
-      if (lane_id() == 0) {
-        c.m_exp[at[k] / kMomentBlock] = (uint8_t)Em;
-        c.v_exp[at[k] / kMomentBlock] = (uint8_t)Ev;
-      }
-    }
-    if (left[k] <= 0) continue;
-    store_part<float, V>(c.param + at[k], left[k], p[k]);
-    if constexpr (!EIGHT) {
-      store_part<float, V>(static_cast<float*>(c.m) + at[k], left[k], m[k]);
-      store_part<float, V>(static_cast<float*>(c.v) + at[k], left[k], v[k]);
-    }
-    if (c.copy) store_part<V>(c.copy, c.types >> 8, at[k], left[k], p[k]);
   }
-  if (bad) raise_error(err, GBA_DERR_NONFINITE);
+  if constexpr (EIGHT) {
+    const float top_r = fmaxf(fmaxf(root[0], root[1]), fmaxf(root[2], root[3]));
+    Em = block_exponent<3>(wave_max(top_m));
+    Ev = block_exponent<4>(wave_max(__float_as_uint(top_r)));
+  }
+  if (left <= 0) return;
+  if constexpr (EIGHT) {
+    const uint32_t here = mix_bits(key + c.block + (uint32_t)block);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const uint32_t random = mix_bits(here + (uint32_t)(at % kMomentBlock + e));
+      cm[e] = (uint8_t)(encode<3>(fabsf(mn[e]), Em, random & 0xffffu) | (mn[e] < 0.0f ? 128u : 0u));
+      cv[e] = (uint8_t)encode<4>(root[e], Ev, random >> 16);
+    }
+    uint8_t* a = static_cast<uint8_t*>(c.m) + at;
+    uint8_t* b = static_cast<uint8_t*>(c.v) + at;
+    if (left >= V) {
+      *reinterpret_cast<bytes*>(a) = cm;
+      *reinterpret_cast<bytes*>(b) = cv;
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (e < left) {
+          a[e] = cm[e];
+          b[e] = cv[e];
+        }
+    }
+    if (lane_id() == 0) {
+      c.m_exp[block] = (uint8_t)Em;
+      c.v_exp[block] = (uint8_t)Ev;
+    }
+  } else {
+    store_part<float, V, true>(static_cast<float*>(c.m) + at, left, mn);
+    store_part<float, V, true>(static_cast<float*>(c.v) + at, left, vn);
+  }
+  store_part<float, V, true>(c.param + at, left, pn);
+  if (c.copy) store_part<V>(c.copy, c.types >> 8, at, left, pn);
 }
 
-__global__ void __launch_bounds__(kAdamBlock)
+__global__ void __launch_bounds__(kAdamBlock, 8)
 adamw_kernel(const AdamwChunk* __restrict__ list, int64_t chunks, AdamwParams hp, AdamwStep s,
              const int64_t* __restrict__ t_device, int64_t t, uint32_t seed, const float* __restrict__ coef_device,
              int32_t* err) {

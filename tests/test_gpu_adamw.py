@@ -137,6 +137,33 @@ def test_chunks_beyond_one_round_of_blocks():
     assert (p == first[0]).all() and (m == m[0]).all() and (v == v[0]).all()
 
 
+def test_more_chunks_than_blocks():
+    n = (1 << 27) + 5000   # a block goes on to another chunk from 2^27 elements on
+    p, g = torch.ones(n, device=DEV), torch.full((n,), 0.5, dtype=BF16, device=DEV)
+    m, v = torch.zeros(n, device=DEV), torch.zeros(n, device=DEV)
+    gba.gba_adamw(gba.gba_adamw_list([p], [g], [m], [v]), **HP, t=1)
+    assert float(m[0]) == np.float32(0.1) * np.float32(0.5) and float(p[0]) < 1.0
+    assert (p == p[0]).all() and (m == m[0]).all() and (v == v[0]).all()
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_squares_below_the_normal_numbers(eight):
+    """Gradients of 1e-20 to 5e-19: v holds a few bits, its root (and the step) what they say.  v is off by the rounding
+    of the square and of its product, 2^-150 each, a root by half of that part of v."""
+    n, t = 700, 1
+    rng = np.random.default_rng(3)
+    g = (10.0 ** rng.uniform(-20, -18.3, n) * rng.choice([-1.0, 1.0], n)).astype(np.float32)
+    p, kw = torch.zeros(n, device=DEV), {}
+    m, v = (torch.zeros(n, device=DEV, dtype=torch.uint8 if eight else F32) for _ in range(2))
+    if eight:
+        kw = dict(m_exps=[torch.zeros(3, dtype=torch.uint8, device=DEV)], v_exps=[torch.zeros(3, dtype=torch.uint8, device=DEV)])
+    gba.gba_adamw(gba.gba_adamw_list([p], [_dev(g)], [m], [v], **kw), **{**HP, "eps": 1e-30}, t=t)
+    g = g.astype(np.float64)
+    ref = -HP["lr"] * g / (np.abs(g) + 1e-30)
+    exact_v = (1 - HP["beta2"]) * g * g
+    close(p, ref, np.abs(ref) * (32 * U32 + 2.0 ** -149 / exact_v), "param")
+
+
 @pytest.mark.parametrize("eight", [False, True])
 def test_a_coefficient_of_nothing_writes_nothing(eight):
     c = Case([700, 3], [F32, BF16], eight)
