@@ -17,9 +17,12 @@
 // The gradient is the same from the end to the front, its first steps the
 // sequences' last ones.
 //
-// Blocks take whole sequences where there are enough of them.  Of few long
-// ones each is cut into parts of equal length, the maps of all parts are made
-// by a first launch, and each block of the second joins those before its own.
+// Positions are cut into parts, one for a block and group of columns.  Equal
+// lengths: of whole sequences where there are enough of them.  Few long ones, and
+// packed ones of any lengths, are cut where the parts come out equal, and a first
+// launch maps what a part hands on to the next: the positions from its last
+// sequence's beginning on (nothing where that ends with the part).  A block of the
+// second launch joins the maps of those parts that the sequence passes before.
 #include <algorithm>
 
 #include "elements.hpp"
@@ -57,56 +60,102 @@ __device__ __forceinline__ void gate_of(float a, float& f, float& i) {
   i = holds ? small : big;
 }
 
-// ------------------------------------------------------ which sequence
-// Packed sequences: the sequence of every position (-1 behind the last), and
-// what an empty sequence hands on: its state, or its state's gradient.
-struct ScanMapArgs {
-  const int64_t* offsets;   // [B + 1]
-  int32_t* seq;             // [n]
-  const float* from;        // [B][D], may be null (0)
-  float* to;                // [B][D], may be null
-  int64_t n, B, D;
-  int32_t* err;
-};
-__global__ void __launch_bounds__(kScanBlock)
-scan_map_kernel(ScanMapArgs a) {
-  const int64_t stride = (int64_t)gridDim.x * kScanBlock;
-  const int64_t first = (int64_t)blockIdx.x * kScanBlock + threadIdx.x;
-  for (int64_t p = first; p < a.n; p += stride) {
-    int64_t lo = 0, hi = a.B;   // the last b with offsets[b] <= p, of lo .. hi - 1
-    while (hi - lo > 1) {
-      const int64_t mid = (lo + hi) >> 1;
-      if (a.offsets[mid] <= p) lo = mid;
-      else hi = mid;
-    }
-    a.seq[p] = a.offsets[lo] <= p && p < a.offsets[lo + 1] ? (int32_t)lo : -1;
-  }
-  for (int64_t b = first; b < a.B; b += stride)
-    if (a.offsets[b] > a.offsets[b + 1] || (b == 0 && a.offsets[0] != 0) || a.offsets[b + 1] > a.n)
-      raise_error(a.err, GBA_DERR_OFFSETS);
-  if (!a.to) return;
-  const int64_t waves = stride / kWave;
-  for (int64_t b = first / kWave; b < a.B; b += waves) {
-    if (a.offsets[b] < a.offsets[b + 1]) continue;
-    for (int64_t c = lane_id(); c < a.D; c += kWave) a.to[b * a.D + c] = a.from ? a.from[b * a.D + c] : 0.0f;
-  }
-}
-
-// ------------------------------------------------------------ the kernels
+// ------------------------------------------------------------ the positions
 struct ScanArgs {
   RecurrenceArgs r;
-  const int32_t* seq;      // packed: the sequence of each position; null: equal lengths
+  int32_t* seq;            // packed: the sequence of each position (-1 behind the last); null: equal lengths
   int32_t length;          // ... of this many positions
   int32_t groups;          // of columns
   int32_t parts;           // of the positions
   int32_t part_len;        // positions of a part
-  bool split;              // parts are cut through sequences
+  struct ScanPart* part;   // [parts] (null: parts of whole sequences)
   float* part_F;           // [parts][D] the parts' maps
   float* part_S;
-  int32_t* part_forget;    // [parts][groups]
-  float* state;            // [B][D] copy of the states that sequences begin with, where a part writes over them
+  float* state;            // [parts][D] the state (or gradient) that a sequence begins (ends) with in a part and leaves
+                           // it, where its own place is written over by another block; may be null
 };
 
+// What the first launch leaves of a part.
+struct ScanPart {
+  int32_t end;             // where its positions end
+  int32_t from;            // the part in which the sequence begins that it is entered in the middle of (GRAD: ends), or -1
+  int32_t on;              // the sequence that goes on behind it (GRAD: in front of it), or -1
+  int32_t unused;
+};
+
+// Where sequence b begins and ends.
+__device__ __forceinline__ int64_t seq_begin(const ScanArgs& a, int64_t b) {
+  return a.seq ? a.r.offsets[b] : b * a.length;
+}
+__device__ __forceinline__ int64_t seq_end(const ScanArgs& a, int64_t b) {
+  return a.seq ? a.r.offsets[b + 1] : (b + 1) * a.length;
+}
+// For each of two positions the last b of 0 .. B - 1 with offsets[b] <= p, or 0: the wave reads 64 of them at once.
+__device__ __forceinline__ void wave_find(const int64_t* offsets, int64_t B, int64_t p, int64_t q, int64_t& b, int64_t& c) {
+  b = c = 0;
+  for (int64_t width = B; width > 1;) {
+    const int64_t step = (width + kWave - 1) / kWave, i = b + lane_id() * step, j = c + lane_id() * step;
+    const bool in = lane_id() * step < width;
+    const int64_t x = in && i < B ? offsets[i] : INT64_MAX, y = in && j < B ? offsets[j] : INT64_MAX;
+    const uint64_t up_to_p = __ballot(x <= p) | 1u, up_to_q = __ballot(y <= q) | 1u;
+    b += (63 - __clzll(up_to_p)) * step;
+    c += (63 - __clzll(up_to_q)) * step;
+    width = step;
+  }
+}
+
+// Where a block is in the order of parts and groups: blocks go to the eight dies
+// in turn, and neighbours, which read the same rows, come to one die.
+__device__ __forceinline__ unsigned block_place(unsigned n) {
+  constexpr unsigned kDies = 8;
+  const unsigned each = n / kDies, more = n % kDies, die = blockIdx.x % kDies;
+  return die * each + (die < more ? die : more) + blockIdx.x / kDies;
+}
+// Packed sequences: the sequence of each of a part's positions.
+__device__ __forceinline__ void write_sequences(const ScanArgs& a, int part, int group) {
+  const int64_t* offsets = a.r.offsets;
+  const int64_t p0 = (int64_t)part * a.part_len, p1 = p0 + a.part_len < a.r.n ? p0 + a.part_len : a.r.n;
+  int64_t first, last;
+  wave_find(offsets, a.r.B, p0, p1 - 1, first, last);
+  const int64_t to = p0 + (p1 - p0) * (group + 1) / a.groups;   // the groups' blocks share the part
+  for (int64_t p = p0 + (p1 - p0) * group / a.groups + threadIdx.x; p < to; p += kScanBlock) {
+    int64_t lo = first, hi = last + 1;
+    while (hi - lo > 1) {
+      const int64_t mid = (lo + hi) >> 1;
+      if (offsets[mid] <= p) lo = mid;
+      else hi = mid;
+    }
+    a.seq[p] = offsets[lo] <= p && p < offsets[lo + 1] ? (int32_t)lo : -1;
+  }
+}
+// The checks of the offsets, and what an empty sequence hands on: its state, or
+// its state's gradient: block `block` of `blocks`, a wave every (waves)-th
+// sequence, 64 at a time.
+template <bool GRAD>
+__device__ __forceinline__ void check_sequences(const ScanArgs& a, unsigned block, unsigned blocks, int32_t* err) {
+  const int64_t* offsets = a.r.offsets;
+  const int64_t B = a.r.B, D = a.r.D, waves = (int64_t)blocks * kScanWaves;
+  float* to = GRAD ? a.r.dh0 : a.r.h_last;
+  const float* from = GRAD ? a.r.dh_last : a.r.h0;
+  if (to == from) to = nullptr;
+  for (int64_t b0 = (int64_t)block * kScanWaves + threadIdx.x / kWave; b0 < B; b0 += waves * kWave) {
+    const int64_t b = b0 + lane_id() * waves;
+    const int64_t begin = b < B ? offsets[b] : 0, end = b < B ? offsets[b + 1] : 1;
+    if (begin > end || (b == 0 && begin != 0) || (b < B && end > a.r.n)) raise_error(err, GBA_DERR_OFFSETS);
+    if (!to) continue;
+    for (uint64_t empty = __ballot(begin >= end); empty; empty &= empty - 1) {
+      const int64_t row = (b0 + (__ffsll((unsigned long long)empty) - 1) * waves) * D;
+#pragma unroll 4
+      for (int64_t c = lane_id() * 4; c < D; c += kWave * 4) {
+        float v[4] = {};
+        if (from) load_part<float, 4>(from + row + c, (int)(D - c), v);
+        store_part<float, 4>(to + row + c, (int)(D - c), v);
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------ the kernels
 // One map over V columns.
 template <int V>
 struct Affine {
@@ -181,7 +230,8 @@ struct ScanShared {
 // Joins the slots' maps: leaves in `in` the state that this slot's positions
 // are entered with and in `carry` (before: the tile's first) the state after the
 // tile.
-template <int LPC, int V, bool MAP>
+// (JOIN: how many waves' maps are read at a time)
+template <int LPC, int V, bool MAP, int JOIN = kScanWaves>
 __device__ __forceinline__ void scan_join(Affine<V>& m, Affine<V>& carry, float (&in)[V], int& buffer,
                                           ScanShared<LPC, V>& s) {
   const int lane = lane_id(), w = threadIdx.x / kWave, cl = lane % LPC;
@@ -216,7 +266,7 @@ __device__ __forceinline__ void scan_join(Affine<V>& m, Affine<V>& carry, float 
     x.forget = __shfl_up((int)m.forget, LPC, kWave) != 0;
   }
   __syncthreads();
-#pragma unroll
+#pragma unroll JOIN
   for (int k = 0; k < kScanWaves; ++k) {
     if (k == w) {
 #pragma unroll
@@ -241,66 +291,28 @@ __device__ __forceinline__ void scan_join(Affine<V>& m, Affine<V>& carry, float 
     if (lane >= LPC) x.apply(in);
 }
 
-// The state that part `part` of the positions is entered with (in carry.S):
-// the maps of the parts in front of it (front to back, or with BACK back to
-// front), each slot a share of them.
+// The state that a part is entered with (in carry.S): the maps of `count` parts
+// from `first` on (back to front with BACK), each slot a share of them.
 template <int LPC, int V, bool BACK>
-__device__ __forceinline__ void enter_part(const ScanArgs& a, int part, int group, int col, Affine<V>& carry, int& buffer,
+__device__ __forceinline__ void enter_part(const ScanArgs& a, int first, int count, int col, Affine<V>& carry, int& buffer,
                                            ScanShared<LPC, V>& s) {
   constexpr int SLOTS = kScanBlock / LPC;
-  const int before = BACK ? a.parts - 1 - part : part;
   const int slot = threadIdx.x / LPC;
-  const int lo = (int)((int64_t)before * slot / SLOTS), hi = (int)((int64_t)before * (slot + 1) / SLOTS);
+  const int lo = (int)((int64_t)count * slot / SLOTS), hi = (int)((int64_t)count * (slot + 1) / SLOTS);
   Affine<V> m;
   m.clear();
 #pragma unroll 4
   for (int k = lo; k < hi; ++k) {
-    const int j = BACK ? a.parts - 1 - k : k;
+    const int64_t j = BACK ? first - k : first + k;
     Affine<V> b;
-    load_vec<float, V>(a.part_F + (int64_t)j * a.r.D + col, b.F);
-    load_vec<float, V>(a.part_S + (int64_t)j * a.r.D + col, b.S);
-    b.forget = a.part_forget[(int64_t)j * a.groups + group] != 0;
+    load_vec<float, V>(a.part_F + j * a.r.D + col, b.F);
+    load_vec<float, V>(a.part_S + j * a.r.D + col, b.S);
+    b.forget = false;
     b.after(m);
     m = b;
   }
   float unused[V];
   scan_join<LPC, V, false>(m, carry, unused, buffer, s);
-}
-
-// Where the first sequence that begins at position p or behind it begins.
-__device__ __forceinline__ int64_t next_start(const ScanArgs& a, int64_t p) {
-  if (p <= 0 || p >= a.r.n) return p <= 0 ? 0 : a.r.n;
-  const int32_t here = a.seq[p];
-  if (here != a.seq[p - 1]) return p;
-  if (here < 0) return a.r.n;
-  const int64_t end = a.r.offsets[here + 1];
-  return end < a.r.n ? end : a.r.n;   // (behind p, whatever the offsets)
-}
-
-// Where a block is in the order of parts and groups: blocks go to the eight dies
-// in turn, and neighbours, which read the same rows, come to one die.
-__device__ __forceinline__ unsigned block_place() {
-  constexpr unsigned kDies = 8;
-  const unsigned n = gridDim.x, each = n / kDies, more = n % kDies, die = blockIdx.x % kDies;
-  return die * each + (die < more ? die : more) + blockIdx.x / kDies;
-}
-
-// The positions that a block takes.
-__device__ __forceinline__ void part_range(const ScanArgs& a, int part, int64_t& p0, int64_t& p1) {
-  p0 = (int64_t)part * a.part_len;
-  p1 = p0 + a.part_len;
-  int64_t end = a.r.n;
-  if (a.seq) {
-    if (!a.split) {
-      p0 = next_start(a, p0);
-      p1 = next_start(a, p1);
-    }
-    end = a.r.offsets[a.r.B];
-    end = end < 0 ? 0 : end > a.r.n ? a.r.n : end;
-  }
-  if (p1 > end) p1 = end;
-  p0 = __builtin_amdgcn_readfirstlane((int)p0);   // (the same in every lane, also to the compiler)
-  p1 = __builtin_amdgcn_readfirstlane((int)p1);
 }
 
 // Which of T positions from q on begin and end a sequence, as bits.
@@ -382,19 +394,175 @@ struct RowsFrom {
   }
 };
 
-template <typename X, int LPC, int V, int T, bool MAP>
+// The map of what a part hands on.  Forward: of its positions from the last
+// sequence's beginning on; GRAD: back from the first sequence's end.
+template <typename X, int LPC, int V, bool GRAD>
+__device__ __forceinline__ void map_part(const ScanArgs& a, int part, int group, ScanShared<LPC, V>& s) {
+  constexpr int T = kScanT<false>;
+  typedef ScanShape<LPC, V, T> Sh;
+  typedef typename VecOf<X, V>::type vec;
+  const int64_t p0 = (int64_t)part * a.part_len;
+  int64_t p1 = p0 + a.part_len < a.r.n ? p0 + a.part_len : a.r.n;
+  int64_t used = a.r.n, first, last;
+  if (a.seq) {
+    used = a.r.offsets[a.r.B];
+    wave_find(a.r.offsets, a.r.B, p0, p1 - 1, first, last);
+  } else {
+    first = (uint32_t)p0 / (uint32_t)a.length;
+    last = (uint32_t)(p1 - 1) / (uint32_t)a.length;
+  }
+  // (of the first and of the last position: those behind the last sequence are in none)
+  const int64_t begin0 = seq_begin(a, first), end0 = seq_end(a, first), begin1 = seq_begin(a, last), end1 = seq_end(a, last);
+  const bool before = begin0 < p0 && end0 > p0, behind = begin1 < p1 && end1 > p1;
+  if (group == 0 && threadIdx.x == 0) {
+    ScanPart o;
+    o.end = (int32_t)(used < 0 ? 0 : used < p1 ? used : p1);
+    const int64_t there = GRAD ? (end1 < a.r.n ? end1 : a.r.n) - 1 : (begin0 < 0 ? 0 : begin0);
+    o.from = (GRAD ? behind : before) ? (int32_t)((uint32_t)there / (uint32_t)a.part_len) : -1;
+    o.on = (GRAD ? before : behind) ? (int32_t)(GRAD ? first : last) : -1;
+    o.unused = 0;
+    a.part[part] = o;
+  }
+  // the sequence that goes on, and its positions here
+  if (GRAD ? !before : !behind) return;
+  const int64_t b = GRAD ? first : last;
+  const bool forget = GRAD ? end0 <= p1 : begin1 >= p0;   // it begins (ends) here
+  const int64_t q0 = __builtin_amdgcn_readfirstlane((int)(!GRAD && forget ? begin1 : p0));
+  const int64_t q1 = __builtin_amdgcn_readfirstlane((int)(GRAD && forget ? end0 : p1));
+
+  const int slot = threadIdx.x / LPC;
+  const ScanColumns<V> col(group * Sh::COLUMNS + (int)(threadIdx.x % LPC) * V, a.r.D);
+  const int place = GRAD ? (Sh::SLOTS - 1 - slot) * T : slot * T;   // of the slot in a tile
+  const void* const in = GRAD ? a.r.dh : a.r.x;
+  const int64_t in_stride = GRAD ? a.r.dh_stride : a.r.x_stride;
+  uint64_t place_a = lane_place<X>(a.r.a_stride, place, col.at), place_x = lane_place<X>(in_stride, place, col.at);
+  float h0[V] = {};
+  if (forget) {
+    const float* from = GRAD ? a.r.dh_last : a.r.h0;
+    if (from) load_vec<float, V>(from + b * a.r.D + col.at, h0);
+    if (a.state && slot == 0) col.store(a.state + (int64_t)part * a.r.D + col.at, h0);
+  }
+  vec x[T] = {}, g[T] = {};
+  auto load = [&](int64_t t) {   // the tile that begins at t
+    keep_place(place_a);
+    keep_place(place_x);
+    const RowsFrom<X> rows_a(a.r.a, a.r.a_stride, t), rows_x(in, in_stride, t);
+    const int64_t q = t + place;
+    if (t >= q0 && t + Sh::TILE <= q1) {
+#pragma unroll
+      for (int i = 0; i < T; ++i) {
+        g[i] = rows_a.template load<V>(i, place_a);
+        x[i] = rows_x.template load<V>(i, place_x);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < T; ++i) {
+        if (q + i < q0 || q + i >= q1) continue;
+        g[i] = rows_a.template load<V>(i, place_a);
+        x[i] = rows_x.template load<V>(i, place_x);
+      }
+    }
+  };
+  int buffer = 0;
+  Affine<V> carry;
+  carry.clear();
+  const int64_t tiles = (q1 - q0 + Sh::TILE - 1) / Sh::TILE;
+  auto tile = [&](int64_t k) { return GRAD ? q1 - (k + 1) * Sh::TILE : q0 + k * Sh::TILE; };
+  load(tile(0));
+  for (int64_t k = 0; k < tiles; ++k) {
+    const int64_t t = tile(k), q = t + place;
+    float f[T][V], v[T][V];
+#pragma unroll
+    for (int i = 0; i < T; ++i)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        gate_of<sizeof(X) == 4>((float)g[i][e], f[i][e], v[i][e]);
+        v[i][e] = GRAD ? (float)x[i][e] : v[i][e] * (float)x[i][e];
+      }
+    if (k + 1 < tiles) load(tile(k + 1));
+    if (t < q0 || t + Sh::TILE > q1) {   // beyond the positions: steps that do nothing
+#pragma unroll
+      for (int i = 0; i < T; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const bool here = q + i >= q0 && q + i < q1;
+          f[i][e] = here ? f[i][e] : 1.0f;
+          v[i][e] = here ? v[i][e] : 0.0f;
+        }
+    }
+    Affine<V> m;
+    m.forget = false;
+    if constexpr (GRAD) {
+      const bool last = k == 0 && slot == 0 && forget;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        m.S[e] = f[T - 1][e] * (last ? v[T - 1][e] + h0[e] : v[T - 1][e]);
+        m.F[e] = f[T - 1][e];
+      }
+#pragma unroll
+      for (int i = T - 2; i >= 0; --i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          m.S[e] = f[i][e] * (v[i][e] + m.S[e]);
+          m.F[e] *= f[i][e];
+        }
+    } else {
+      const bool first = k == 0 && slot == 0 && forget;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        m.S[e] = first ? __builtin_fmaf(f[0][e], h0[e], v[0][e]) : v[0][e];
+        m.F[e] = f[0][e];
+      }
+#pragma unroll
+      for (int i = 1; i < T; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          m.S[e] = __builtin_fmaf(f[i][e], m.S[e], v[i][e]);
+          m.F[e] *= f[i][e];
+        }
+    }
+    float unused[V];
+    scan_join<LPC, V, true>(m, carry, unused, buffer, s);
+  }
+  // (where it begins here F is multiplied by the 0 that it is entered with)
+  if (slot == 0 && col.shift < V) {
+    store_vec<float, V>(a.part_F + (int64_t)part * a.r.D + col.at, carry.F);
+    store_vec<float, V>(a.part_S + (int64_t)part * a.r.D + col.at, carry.S);
+  }
+}
+template <typename X, int LPC, int V, bool GRAD>
+__global__ void __launch_bounds__(kScanBlock, kScanSimd)
+scan_part_kernel(ScanArgs a, int32_t* err) {
+  __shared__ ScanShared<LPC, V> s;
+  const unsigned blocks = (unsigned)a.parts * (unsigned)a.groups, groups = (unsigned)a.groups;
+  if (blockIdx.x < blocks) {
+    const unsigned block = block_place(blocks);
+    map_part<X, LPC, V, GRAD>(a, (int)(block / groups), (int)(block % groups), s);
+  } else {   // packed: beside the maps
+    const unsigned block = blockIdx.x - blocks;
+    if (block < blocks) write_sequences(a, (int)(block / groups), (int)(block % groups));
+    check_sequences<GRAD>(a, block, gridDim.x - blocks, err);
+  }
+}
+
+template <typename X, int LPC, int V, int T>
 __global__ void __launch_bounds__(kScanBlock, kScanSimd)
 scan_kernel(ScanArgs a) {
   typedef ScanShape<LPC, V, T> Sh;
   typedef typename VecOf<X, V>::type vec;
   __shared__ ScanShared<LPC, V> s;
-  const unsigned block = block_place();
+  const unsigned block = block_place(gridDim.x);
   const int group = (int)(block % (unsigned)a.groups), part = (int)(block / (unsigned)a.groups);
   const int slot = threadIdx.x / LPC;
   const ScanColumns<V> col(group * Sh::COLUMNS + (int)(threadIdx.x % LPC) * V, a.r.D);
-  const float* first_state = a.state && !MAP ? a.state : a.r.h0;
-  int64_t p0, p1;
-  part_range(a, part, p0, p1);
+  const int64_t p0 = (int64_t)part * a.part_len;
+  int64_t p1 = p0 + a.part_len < a.r.n ? p0 + a.part_len : a.r.n;
+  int from = -1, on = -1;
+  if (a.part) {   // (the same in every lane, also to the compiler)
+    p1 = __builtin_amdgcn_readfirstlane(a.part[part].end);
+    from = __builtin_amdgcn_readfirstlane(a.part[part].from);
+    on = __builtin_amdgcn_readfirstlane(a.part[part].on);
+  }
   int buffer = 0;
   Affine<V> carry;
   carry.clear();
@@ -423,9 +591,9 @@ scan_kernel(ScanArgs a) {
     }
     at.load(a, q);
   };
-  if (p0 < p1) load(p0);
-  if constexpr (!MAP)
-    if (a.split && part > 0) enter_part<LPC, V, false>(a, part, group, col.at, carry, buffer, s);
+  if (p0 >= p1) return;
+  load(p0);
+  if (from >= 0) enter_part<LPC, V, false>(a, from, part - from, col.at, carry, buffer, s);
   for (int64_t p = p0; p < p1; p += Sh::TILE) {
     const int64_t q = p + slot * T;
     const int here = p1 - q < T ? (int)(p1 - q) : T;   // positions of this slot (none: <= 0)
@@ -440,14 +608,14 @@ scan_kernel(ScanArgs a) {
     // (what slots past the end compute goes nowhere: the tile is the last, and nobody enters with the last part's map)
     at.find(a, q, 0, here);
     const uint32_t starts = at.starts, ends = at.ends;
-    if (starts && first_state) {
+    if (starts && a.r.h0) {
 #pragma unroll
       for (int i = 0; i < T; ++i) {
         if (!(starts >> i & 1)) continue;
-        const int64_t to = Bounds<T>::sequence(a, q + i) * a.r.D;
+        const int64_t b = Bounds<T>::sequence(a, q + i);
+        const float* row = a.state && b == on ? a.state + (int64_t)part * a.r.D : a.r.h0 + b * a.r.D;
         float h0[V];
-        load_vec<float, V>(first_state + to + col.at, h0);
-        if (MAP && a.state) col.store(a.state + to + col.at, h0);
+        load_vec<float, V>(row + col.at, h0);
 #pragma unroll
         for (int e = 0; e < V; ++e) v[i][e] = __builtin_fmaf(f[i][e], h0[e], v[i][e]);   // the state after the step
       }
@@ -470,44 +638,40 @@ scan_kernel(ScanArgs a) {
     }
     m.forget = starts != 0;
     float h[V];
-    scan_join<LPC, V, MAP>(m, carry, h, buffer, s);
-    if constexpr (!MAP) {
-      keep_place(place_h);
-      const RowsFrom<X> out(a.r.h, a.r.h_stride, p);
+    scan_join<LPC, V, false>(m, carry, h, buffer, s);
+    keep_place(place_h);
+    const RowsFrom<X> out(a.r.h, a.r.h_stride, p);
 #pragma unroll
-      for (int i = 0; i < T; ++i) {
-        const bool first = starts >> i & 1;
+    for (int i = 0; i < T; ++i) {
+      const bool first = starts >> i & 1;
 #pragma unroll
-        for (int e = 0; e < V; ++e) h[e] = first ? v[i][e] : __builtin_fmaf(f[i][e], h[e], v[i][e]);
-        if (i < here) col.store(out.at(i, place_h), h);
-        if (a.r.h_last && (ends >> i & 1)) col.store(a.r.h_last + Bounds<T>::sequence(a, q + i) * a.r.D + col.at, h);
-      }
+      for (int e = 0; e < V; ++e) h[e] = first ? v[i][e] : __builtin_fmaf(f[i][e], h[e], v[i][e]);
+      if (i < here) col.store(out.at(i, place_h), h);
+      if (a.r.h_last && (ends >> i & 1)) col.store(a.r.h_last + Bounds<T>::sequence(a, q + i) * a.r.D + col.at, h);
     }
-  }
-  if constexpr (MAP) {
-    if ((int)threadIdx.x < LPC) {
-      store_vec<float, V>(a.part_F + (int64_t)part * a.r.D + col.at, carry.F);
-      store_vec<float, V>(a.part_S + (int64_t)part * a.r.D + col.at, carry.S);
-    }
-    if (threadIdx.x == 0) a.part_forget[(int64_t)part * a.groups + group] = carry.forget;
   }
 }
 
 // The gradient: positions from the end; slot 0 takes a tile's last ones.  The
 // state that runs through is f_t g_t, what a position hands to the one before it.
-template <typename X, int LPC, int V, int T, bool MAP>
+template <typename X, int LPC, int V, int T>
 __global__ void __launch_bounds__(kScanBlock, kScanSimd)
 scan_grad_kernel(ScanArgs a) {
   typedef ScanShape<LPC, V, T> Sh;
   typedef typename VecOf<X, V>::type vec;
   __shared__ ScanShared<LPC, V> s;
-  const unsigned block = block_place();
+  const unsigned block = block_place(gridDim.x);
   const int group = (int)(block % (unsigned)a.groups), part = (int)(block / (unsigned)a.groups);
   const int slot = threadIdx.x / LPC;
   const ScanColumns<V> col(group * Sh::COLUMNS + (int)(threadIdx.x % LPC) * V, a.r.D);
-  const float* last_grad = a.state && !MAP ? a.state : a.r.dh_last;
-  int64_t p0, p1;
-  part_range(a, part, p0, p1);
+  const int64_t p0 = (int64_t)part * a.part_len;
+  int64_t p1 = p0 + a.part_len < a.r.n ? p0 + a.part_len : a.r.n;
+  int from = -1, on = -1;
+  if (a.part) {   // (the same in every lane, also to the compiler)
+    p1 = __builtin_amdgcn_readfirstlane(a.part[part].end);
+    from = __builtin_amdgcn_readfirstlane(a.part[part].from);
+    on = __builtin_amdgcn_readfirstlane(a.part[part].on);
+  }
   int buffer = 0;
   Affine<V> carry;
   carry.clear();
@@ -531,10 +695,8 @@ scan_grad_kernel(ScanArgs a) {
       for (int i = 0; i < T; ++i) {
         gate[i] = rows_a.template load<V>(i, place_a);
         dh[i] = rows_d.template load<V>(i, place_d);
-        if constexpr (!MAP) {
-          x[i] = rows_x.template load<V>(i, place_x);
-          before[i] = rows_h.template load<V>(i, place_h);
-        }
+        x[i] = rows_x.template load<V>(i, place_x);
+        before[i] = rows_h.template load<V>(i, place_h);
       }
     } else {
 #pragma unroll
@@ -542,17 +704,15 @@ scan_grad_kernel(ScanArgs a) {
         if (q + i < p0) continue;
         gate[i] = rows_a.template load<V>(i, place_a);
         dh[i] = rows_d.template load<V>(i, place_d);
-        if constexpr (!MAP) {
-          x[i] = rows_x.template load<V>(i, place_x);
-          if (q + i > 0) before[i] = rows_h.template load<V>(i, place_h);
-        }
+        x[i] = rows_x.template load<V>(i, place_x);
+        if (q + i > 0) before[i] = rows_h.template load<V>(i, place_h);
       }
     }
     at.load(a, q);
   };
-  if (p0 < p1) load(p1);
-  if constexpr (!MAP)
-    if (a.split && part + 1 < a.parts) enter_part<LPC, V, true>(a, part, group, col.at, carry, buffer, s);
+  if (p0 >= p1) return;
+  load(p1);
+  if (from >= 0) enter_part<LPC, V, true>(a, from, from - part, col.at, carry, buffer, s);
   for (int64_t p = p1; p > p0; p -= Sh::TILE) {
     const int64_t q = p - Sh::TILE + back;
     const int skip = q < p0 ? (p0 - q < T ? (int)(p0 - q) : T) : 0;
@@ -563,20 +723,12 @@ scan_grad_kernel(ScanArgs a) {
       for (int e = 0; e < V; ++e) {
         gate_of<sizeof(X) == 4>((float)gate[i][e], f[i][e], in[i][e]);
         d[i][e] = (float)dh[i][e];
-        if constexpr (!MAP) diff[i][e] = (float)before[i][e] - (float)x[i][e];
+        diff[i][e] = (float)before[i][e] - (float)x[i][e];
       }
-    if (MAP && p - Sh::TILE < p0) {   // in front of the part (of a map, which is handed on): steps that do nothing
-#pragma unroll
-      for (int i = 0; i < T; ++i)
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          f[i][e] = i < skip ? 1.0f : f[i][e];
-          d[i][e] = i < skip ? 0.0f : d[i][e];
-        }
-    }
+    // (what slots in front of the part compute goes nowhere)
     at.find(a, q, skip, T);
     const uint32_t starts = at.starts, ends = at.ends;
-    if (starts && !MAP) {
+    if (starts) {
 #pragma unroll
       for (int i = 0; i < T; ++i) {
         if (!(starts >> i & 1)) continue;
@@ -586,14 +738,14 @@ scan_grad_kernel(ScanArgs a) {
         for (int e = 0; e < V; ++e) diff[i][e] = h0[e] - (float)x[i][e];
       }
     }
-    if (ends && last_grad) {
+    if (ends && a.r.dh_last) {
 #pragma unroll
       for (int i = 0; i < T; ++i) {
         if (!(ends >> i & 1)) continue;
-        const int64_t to = Bounds<T>::sequence(a, q + i) * a.r.D;
+        const int64_t b = Bounds<T>::sequence(a, q + i);
+        const float* row = a.state && b == on ? a.state + (int64_t)part * a.r.D : a.r.dh_last + b * a.r.D;
         float g[V];
-        load_vec<float, V>(last_grad + to + col.at, g);
-        if (MAP && a.state) col.store(a.state + to + col.at, g);
+        load_vec<float, V>(row + col.at, g);
 #pragma unroll
         for (int e = 0; e < V; ++e) d[i][e] += g[e];
       }
@@ -616,36 +768,28 @@ scan_grad_kernel(ScanArgs a) {
     }
     m.forget = ends != 0;
     float c[V];
-    scan_join<LPC, V, MAP>(m, carry, c, buffer, s);
-    if constexpr (!MAP) {
-      keep_place(place_dx);
-      keep_place(place_da);
-      const RowsFrom<X> out_x(a.r.dx, a.r.dx_stride, p - Sh::TILE), out_a(a.r.da, a.r.da_stride, p - Sh::TILE);
+    // (32 bits: four waves' maps at a time would not fit the registers, 32 x 1024 positions of 1024 157 us to 140)
+    scan_join<LPC, V, false, sizeof(X) == 4 ? 2 : kScanWaves>(m, carry, c, buffer, s);
+    keep_place(place_dx);
+    keep_place(place_da);
+    const RowsFrom<X> out_x(a.r.dx, a.r.dx_stride, p - Sh::TILE), out_a(a.r.da, a.r.da_stride, p - Sh::TILE);
 #pragma unroll
-      for (int i = T - 1; i >= 0; --i) {
-        const bool last = ends >> i & 1;
-        float dx[V], da[V];
+    for (int i = T - 1; i >= 0; --i) {
+      const bool last = ends >> i & 1;
+      float dx[V], da[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float g = last ? d[i][e] : d[i][e] + c[e];
-          dx[e] = in[i][e] * g;
-          da[e] = dx[e] * (diff[i][e] * f[i][e]);
-          c[e] = f[i][e] * g;
-        }
-        if (i >= skip) {
-          col.store(out_x.at(i, place_dx), dx);
-          col.store(out_a.at(i, place_da), da);
-        }
-        if (a.r.dh0 && (starts >> i & 1)) col.store(a.r.dh0 + Bounds<T>::sequence(a, q + i) * a.r.D + col.at, c);
+      for (int e = 0; e < V; ++e) {
+        const float g = last ? d[i][e] : d[i][e] + c[e];
+        dx[e] = in[i][e] * g;
+        da[e] = dx[e] * (diff[i][e] * f[i][e]);
+        c[e] = f[i][e] * g;
       }
+      if (i >= skip) {
+        col.store(out_x.at(i, place_dx), dx);
+        col.store(out_a.at(i, place_da), da);
+      }
+      if (a.r.dh0 && (starts >> i & 1)) col.store(a.r.dh0 + Bounds<T>::sequence(a, q + i) * a.r.D + col.at, c);
     }
-  }
-  if constexpr (MAP) {
-    if ((int)threadIdx.x < LPC) {
-      store_vec<float, V>(a.part_F + (int64_t)part * a.r.D + col.at, carry.F);
-      store_vec<float, V>(a.part_S + (int64_t)part * a.r.D + col.at, carry.S);
-    }
-    if (threadIdx.x == 0) a.part_forget[(int64_t)part * a.groups + group] = carry.forget;
   }
 }
 
@@ -675,15 +819,14 @@ scan_step_kernel(RecurrenceArgs r, int lanes, int column_blocks) {
 }
 
 // ------------------------------------------------------------- launching
-// The most parts that sequences are cut into: of blocks of the widest groups of columns.
+// The most parts that are made: of blocks of the widest groups of columns.
 static int64_t scan_most_parts(int32_t D) { return std::max<int64_t>(1, kScanBlocks / ceil_div(D, kScanWidest)); }
 
-// The sequence of each position, the parts' maps, and the states of as many
-// sequences as are ever cut into parts.
+// The sequence of each position, and the parts' maps and states.
 struct ScanRoom {
-  size_t seq, F, S, forget, state, bytes;
+  size_t seq, part, F, S, state, bytes;
 };
-static ScanRoom scan_room(int64_t n, int64_t B, int32_t D) {
+static ScanRoom scan_room(int64_t n, int32_t D) {
   ScanRoom r;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -691,48 +834,49 @@ static ScanRoom scan_room(int64_t n, int64_t B, int32_t D) {
     at += align_up(bytes);
     return here;
   };
-  const int64_t parts = scan_most_parts(D);
+  const size_t rows = (size_t)scan_most_parts(D) * D * sizeof(float);
   r.seq = take((size_t)n * sizeof(int32_t));
-  r.F = take((size_t)parts * D * sizeof(float));
-  r.S = take((size_t)parts * D * sizeof(float));
-  r.forget = take((size_t)std::max<int64_t>(kScanBlocks, D) * sizeof(int32_t));   // (parts x groups)
-  r.state = take((size_t)std::min(B, kScanSplitBelow) * D * sizeof(float));
+  r.part = take((size_t)scan_most_parts(D) * sizeof(ScanPart));
+  r.F = take(rows);
+  r.S = take(rows);
+  r.state = take(rows);
   r.bytes = at + 256;
   return r;
 }
-size_t recurrence_workspace_bytes(int64_t n, int64_t B, int32_t D) { return scan_room(n, B, D).bytes; }
+size_t recurrence_workspace_bytes(int64_t n, int64_t, int32_t D) { return scan_room(n, D).bytes; }
 
 template <typename X, int LPC, int V, bool GRAD>
-static hipError_t scan_in(ScanArgs a, void* ws, hipStream_t stream) {
+static hipError_t scan_in(ScanArgs a, void* ws, int32_t* err, hipStream_t stream) {
   constexpr int T = kScanT<GRAD>;
   typedef ScanShape<LPC, V, T> Sh;
   const RecurrenceArgs& r = a.r;
   const int64_t tiles = ceil_div(r.n, Sh::TILE);
   a.groups = (int32_t)ceil_div(r.D, Sh::COLUMNS);
-  const ScanRoom room = scan_room(r.n, r.B, r.D);
-  char* base = static_cast<char*>(ws);
-  const int64_t most = std::max<int64_t>(1, kScanBlocks / a.groups);
-  a.split = r.B * a.groups < kScanSplitBelow && most > r.B && tiles > 2 * r.B;
-  const int64_t parts = std::min(most, tiles);
-  if (a.split) {
-    a.part_len = (int32_t)(ceil_div(ceil_div(r.n, parts), Sh::TILE) * Sh::TILE);
+  const int64_t parts = std::max<int64_t>(1, std::min(std::max<int64_t>(1, kScanBlocks / a.groups), tiles));
+  a.part_len = (int32_t)std::max<int64_t>(1, ceil_div(r.n, parts));
+  const bool split = a.seq || (r.B * a.groups < kScanSplitBelow && tiles > 2 * r.B);
+  if (split) {
+    const ScanRoom room = scan_room(r.n, r.D);
+    char* base = static_cast<char*>(ws);
+    a.part_len = (int32_t)std::min<int64_t>(ceil_div(a.part_len, Sh::TILE) * Sh::TILE, INT32_MAX);
+    a.part = reinterpret_cast<ScanPart*>(base + room.part);
     a.part_F = reinterpret_cast<float*>(base + room.F);
     a.part_S = reinterpret_cast<float*>(base + room.S);
-    a.part_forget = reinterpret_cast<int32_t*>(base + room.forget);
     if (GRAD ? r.dh_last && r.dh0 : r.h0 && r.h_last) a.state = reinterpret_cast<float*>(base + room.state);
   } else {
-    a.part_len = (int32_t)ceil_div(r.n, parts);
-    if (!a.seq) a.part_len = (int32_t)(ceil_div(a.part_len, a.length) * a.length);   // (no more than n)
+    a.part_len = (int32_t)(ceil_div(a.part_len, a.length) * a.length);   // (no more than n)
   }
   a.parts = (int32_t)ceil_div(r.n, a.part_len);
-  const dim3 grid((unsigned)((int64_t)a.parts * a.groups));
-  if constexpr (GRAD) {
-    if (a.split) hipLaunchKernelGGL((scan_grad_kernel<X, LPC, V, T, true>), grid, dim3(kScanBlock), 0, stream, a);
-    hipLaunchKernelGGL((scan_grad_kernel<X, LPC, V, T, false>), grid, dim3(kScanBlock), 0, stream, a);
-  } else {
-    if (a.split) hipLaunchKernelGGL((scan_kernel<X, LPC, V, T, true>), grid, dim3(kScanBlock), 0, stream, a);
-    hipLaunchKernelGGL((scan_kernel<X, LPC, V, T, false>), grid, dim3(kScanBlock), 0, stream, a);
+  const int64_t blocks = (int64_t)a.parts * a.groups;
+  if (split) {
+    const int64_t beside = a.seq ? std::max(blocks, std::min<int64_t>(ceil_div(r.B, kScanWaves), 1024)) : 0;
+    hipLaunchKernelGGL((scan_part_kernel<X, LPC, V, GRAD>), dim3((unsigned)(blocks + beside)), dim3(kScanBlock), 0, stream,
+                       a, err);
   }
+  if (r.n == 0) return hipGetLastError();
+  const dim3 grid((unsigned)blocks);
+  if constexpr (GRAD) hipLaunchKernelGGL((scan_grad_kernel<X, LPC, V, T>), grid, dim3(kScanBlock), 0, stream, a);
+  else hipLaunchKernelGGL((scan_kernel<X, LPC, V, T>), grid, dim3(kScanBlock), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -749,47 +893,30 @@ static hipError_t scan_step(const RecurrenceArgs& r, hipStream_t stream) {
 }
 
 template <typename X, bool GRAD>
-static hipError_t scan_as(const ScanArgs& a, void* ws, hipStream_t stream) {
+static hipError_t scan_as(const ScanArgs& a, void* ws, int32_t* err, hipStream_t stream) {
   constexpr int V = kScanV;
   const int32_t D = a.r.D;
   if (!GRAD && !a.seq && a.length == 1) return D < V ? scan_step<X, 1>(a.r, stream) : scan_step<X, V>(a.r, stream);
-  if (D < V) return scan_in<X, 4, 1, GRAD>(a, ws, stream);
-  if (D <= 4 * V) return scan_in<X, 4, V, GRAD>(a, ws, stream);
-  if (D <= 8 * V) return scan_in<X, 8, V, GRAD>(a, ws, stream);
+  if (D < V) return scan_in<X, 4, 1, GRAD>(a, ws, err, stream);
+  if (D <= 4 * V) return scan_in<X, 4, V, GRAD>(a, ws, err, stream);
+  if (D <= 8 * V) return scan_in<X, 8, V, GRAD>(a, ws, err, stream);
   // fewer columns to a block where the sequences are then enough blocks, and are too few for what memory takes at once
   const int64_t blocks = a.r.B * ceil_div(D, kScanWidest);
-  const bool few = blocks * (int64_t)sizeof(X) < kScanBlocks * 2 && 2 * blocks >= kScanSplitBelow;
-  if (D <= 16 * V || few) return scan_in<X, 16, V, GRAD>(a, ws, stream);
-  return scan_in<X, kScanLanes, V, GRAD>(a, ws, stream);
+  const bool few = !a.seq && blocks * (int64_t)sizeof(X) < kScanBlocks * 2 && 2 * blocks >= kScanSplitBelow;
+  if (D <= 16 * V || few) return scan_in<X, 16, V, GRAD>(a, ws, err, stream);
+  return scan_in<X, kScanLanes, V, GRAD>(a, ws, err, stream);
 }
 
 template <bool GRAD>
 static hipError_t launch_scan(const RecurrenceArgs& r, void* ws, int32_t* err, hipStream_t stream) {
+  if (r.n == 0 && !r.offsets) return hipSuccess;
   ScanArgs a{};
   a.r = r;
-  if (r.offsets) {
-    ScanMapArgs m;
-    m.offsets = r.offsets;
-    m.seq = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + scan_room(r.n, r.B, r.D).seq);
-    m.from = GRAD ? r.dh_last : r.h0;
-    m.to = GRAD ? r.dh0 : r.h_last;
-    m.n = r.n;
-    m.B = r.B;
-    m.D = r.D;
-    m.err = err;
-    a.seq = m.seq;
-    const int64_t work = std::max<int64_t>(r.n, m.to ? r.B * kWave : r.B);
-    const int64_t blocks = std::min<int64_t>(ceil_div(work, kScanBlock), 1024);
-    hipLaunchKernelGGL(scan_map_kernel, dim3((unsigned)blocks), dim3(kScanBlock), 0, stream, m);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  } else if (r.n > 0) {
-    a.length = (int32_t)(r.n / r.B);
-  }
-  if (r.n == 0) return hipSuccess;
-  if (r.type == GBA_F32) return scan_as<float, GRAD>(a, ws, stream);
-  if (r.type == GBA_BF16) return scan_as<bf16_t, GRAD>(a, ws, stream);
-  return scan_as<f16_t, GRAD>(a, ws, stream);
+  if (r.offsets) a.seq = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + scan_room(r.n, r.D).seq);
+  else a.length = (int32_t)(r.n / r.B);
+  if (r.type == GBA_F32) return scan_as<float, GRAD>(a, ws, err, stream);
+  if (r.type == GBA_BF16) return scan_as<bf16_t, GRAD>(a, ws, err, stream);
+  return scan_as<f16_t, GRAD>(a, ws, err, stream);
 }
 
 hipError_t launch_recurrence(const RecurrenceArgs& r, void* ws, int32_t* err, hipStream_t stream) {
