@@ -82,6 +82,19 @@ struct RowPlace {
     if (tiny) store_part<T, V>(p, D, o);
     else if (k + 1 < NV || last) store_vec<T, V, true>(p + col[k], o);
   }
+  // foreign elements left out
+  template <typename T>
+  __device__ __forceinline__ void store_own(T* __restrict__ p, int k, const float (&o)[V]) const {
+    if (tiny) {
+      store_part<T, V>(p, D, o);
+    } else if (k + 1 < NV || shift == 0) {
+      store_vec<T, V, true>(p + col[k], o);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (e >= shift) p[col[k] + e] = (T)o[e];
+    }
+  }
 };
 
 // Adds each of x[0..N) over the LPR threads of a row.  Rows of several waves
