@@ -109,7 +109,7 @@ __device__ __forceinline__ void row_stats(const At& at, int kind, float D, float
     for (int k = 0; k < NV; ++k)
 #pragma unroll
       for (int e = 0; e < V; ++e) t[0] += at.own(k, e) ? v[k][e] : 0.0f;
-    row_sum<LPR, WAVES>(t, s, buffer);
+    row_total<LPR, WAVES>(t, s, buffer);
     mean = t[0] / D;
     t[0] = 0.0f;
   }
@@ -120,7 +120,7 @@ __device__ __forceinline__ void row_stats(const At& at, int kind, float D, float
       const float d = at.own(k, e) ? v[k][e] - mean : 0.0f;
       t[0] = __builtin_fmaf(d, d, t[0]);
     }
-  row_sum<LPR, WAVES>(t, s, buffer);
+  row_total<LPR, WAVES>(t, s, buffer);
   rstd = 1.0f / sqrtf(t[0] / D + eps);
 }
 
@@ -132,7 +132,7 @@ residual_norm_kernel(Args a, int64_t per, uint32_t span) {
   typedef typename VecOf<TS, V>::type stream_vec;
   typedef typename VecOf<TZ, V>::type vec;
   __shared__ float s_sum[2][1][S::WAVES];
-  const int gl = threadIdx.x % LPR, grp = threadIdx.x / LPR;
+  const int gl = threadIdx.x % LPR, grp = S::G == 1 ? 0 : threadIdx.x / LPR;   // (a row's addresses are then uniform)
   const RowPlace<V, LPR, NV> at(gl, a.D);
   const float D = (float)a.D, eps = (float)a.eps, alpha = (float)a.alpha;
   float wz[NV][V], bz[NV][V], wh[NV][V], bh[NV][V], f[NV][V], fn[NV][V];
@@ -156,7 +156,7 @@ residual_norm_kernel(Args a, int64_t per, uint32_t span) {
       xv[k] = at.load_raw(static_cast<const TS*>(a.x) + r * a.x_stride, k);
       zv[k] = at.load_raw(static_cast<const TZ*>(a.z) + r * a.z_stride, k);
     }
-    if (each) load_gate_row(at, a, r, g);
+    if (each) load_gate_row(at, a.gate, a.gate_type, r * a.gate_stride, g);
   };
   int buffer = 0;
   if (r0 < r1) load_row(r0, x, z, fn);
@@ -168,13 +168,13 @@ residual_norm_kernel(Args a, int64_t per, uint32_t span) {
       for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int e = 0; e < V; ++e) f[k][e] = fn[k][e];
-      gate_factors(a, f);
+      gate_factors(a.gate_kind, f);
     } else if (gated) {
       const int64_t g = (uint32_t)(active ? r : r1 - 1) / span;
       if (g != gate_row) {
         gate_row = g;
-        load_gate_row(at, a, g, f);
-        gate_factors(a, f);
+        load_gate_row(at, a.gate, a.gate_type, g * a.gate_stride, f);
+        gate_factors(a.gate_kind, f);
       }
     }
     if (rb + S::G < r1) load_row(rb + S::G, xn, zn, fn);

@@ -80,6 +80,36 @@ struct NormShape {
   static constexpr int WAVES = BLOCK / kWave;
 };
 
+// Adds x over the wave, with every exchange an operand of the addition: the sum is in the last lane.
+__device__ __forceinline__ float wave_total(float x) {
+  x = lanes_sum<16>(x);
+  // (lane 15 of rows 0 and 2 to rows 1 and 3, then lane 31 to rows 2 and 3)
+  x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x142, 0xa, 0xf, false));
+  x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x143, 0xc, 0xf, false));
+  return x;
+}
+// As row_sum: rows of eight waves or more have their waves' sums added up by the
+// lanes too (in turn they were 32 reads and additions of a thread at 16 waves).
+template <int LPR, int WAVES, int N>
+__device__ __forceinline__ void row_total(float (&x)[N], float (*s)[N][WAVES], int& buffer) {
+  constexpr int PER = LPR / kWave;
+  if constexpr (PER < 8) {
+    row_sum<LPR, WAVES>(x, s, buffer);
+  } else {
+    static_assert(PER <= 16 && WAVES == PER, "one row of a block, its waves' sums in 16 lanes");
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = wave_total(x[i]);
+    if (lane_id() == kWave - 1) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[buffer][i][threadIdx.x / kWave] = x[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = lanes_sum<PER>(s[buffer][i][lane_id() % PER]);
+    buffer ^= 1;
+  }
+}
+
 // A norm's parameters, or what stands for those that are not there.
 template <typename At, int NV, int V>
 __device__ __forceinline__ void load_params(const At& at, const void* p, int type, float none, float (&o)[NV][V]) {
@@ -90,20 +120,19 @@ __device__ __forceinline__ void load_params(const At& at, const void* p, int typ
     if (p) at.load(p, type, k, o[k]);
   }
 }
-// The gate's row g as it is.
+// The gate's row from element `from` on, as it is.
 template <typename At, int NV, int V>
-__device__ __forceinline__ void load_gate_row(const At& at, const Args& a, int64_t g, float (&o)[NV][V]) {
-  const int64_t from = g * a.gate_stride;
+__device__ __forceinline__ void load_gate_row(const At& at, const void* gate, int type, int64_t from, float (&o)[NV][V]) {
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    if (a.gate_type == GBA_F32) at.load(static_cast<const float*>(a.gate) + from, k, o[k]);
-    else if (a.gate_type == GBA_BF16) at.load(static_cast<const bf16_t*>(a.gate) + from, k, o[k]);
-    else at.load(static_cast<const f16_t*>(a.gate) + from, k, o[k]);
+    if (type == GBA_F32) at.load(static_cast<const float*>(gate) + from, k, o[k]);
+    else if (type == GBA_BF16) at.load(static_cast<const bf16_t*>(gate) + from, k, o[k]);
+    else at.load(static_cast<const f16_t*>(gate) + from, k, o[k]);
   }
 }
 template <int NV, int V>
-__device__ __forceinline__ void gate_factors(const Args& a, float (&f)[NV][V]) {
-  if (a.gate_kind != GBA_GATE_SIGMOID) return;
+__device__ __forceinline__ void gate_factors(int kind, float (&f)[NV][V]) {
+  if (kind != GBA_GATE_SIGMOID) return;
 #pragma unroll
   for (int k = 0; k < NV; ++k)
 #pragma unroll

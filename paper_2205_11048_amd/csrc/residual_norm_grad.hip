@@ -10,10 +10,10 @@ constexpr int64_t kUnitBlocks = 512;        // most partial sums of the paramete
 // How the rows are cut into units, the rows of a gate row (or all rows) in
 // `cuts` equal parts: blocks take units in turn.
 struct Units {
-  int64_t span;      // rows of a gate row whose gradients are added up; else all rows
-  int64_t cuts;      // units of it
-  int64_t rows;      // of a unit
-  int64_t units;
+  uint32_t span;     // rows of a gate row whose gradients are added up; else all rows
+  uint32_t cuts;     // units of it
+  uint32_t rows;     // of a unit
+  uint32_t units;
   bool shared;       // rows share the gate
   bool gate;         // ... and its gradient is asked for
 };
@@ -22,12 +22,12 @@ static Units units_of(const Args& a) {
   // (the same units, and so the same bits, with and without the gate's gradient)
   const bool shared = u.shared = a.gate_kind != GBA_GATE_NONE && a.gate_span > 1;
   u.gate = shared && a.dgate;
-  u.span = shared ? std::min(a.gate_span, a.n) : a.n;
-  const int64_t G = ceil_div(a.n, u.span);
-  u.cuts = std::min(u.span, std::max<int64_t>(1, kUnitBlocks / G));
-  u.rows = ceil_div(u.span, u.cuts);
-  u.cuts = ceil_div(u.span, u.rows);
-  u.units = G * u.cuts;
+  const int64_t span = shared ? std::min(a.gate_span, a.n) : a.n, G = ceil_div(a.n, span);
+  const int64_t rows = ceil_div(span, std::min(span, std::max<int64_t>(1, kUnitBlocks / G))), cuts = ceil_div(span, rows);
+  u.span = (uint32_t)span;
+  u.rows = (uint32_t)rows;
+  u.cuts = (uint32_t)cuts;
+  u.units = (uint32_t)(G * cuts);   // (below 2 n)
   return u;
 }
 
@@ -178,10 +178,10 @@ residual_norm_columns_kernel(Args a, const float* __restrict__ means, Units un, 
     if (cc < a.D) to(cc, t);
   };
   static_assert(kRowBlock == kWave * kV, "a thread per column of the slice");
-  for (int64_t u = blockIdx.x; u < un.units; u += gridDim.x) {
-    const int64_t g = u / un.cuts, first = g * un.span + (u % un.cuts) * un.rows;
+  for (int64_t u = blockIdx.x; u < (int64_t)un.units; u += gridDim.x) {
+    const int64_t g = (uint32_t)u / un.cuts, first = g * un.span + ((uint32_t)u - g * un.cuts) * un.rows;
     int64_t end = first + un.rows;
-    end = end < (g + 1) * un.span ? end : (g + 1) * un.span;
+    end = end < (g + 1) * (int64_t)un.span ? end : (g + 1) * (int64_t)un.span;
     end = end < a.n ? end : a.n;
     float dg[kV] = {};
     if (c < a.D) {
@@ -218,15 +218,23 @@ constexpr int kGradV = 4;   // columns of a thread's vector
 
 // Where a block is in its units: at rows rb .. of unit u, whose last is end - 1.
 struct UnitCursor {
-  int64_t u, g, rb, end;
-  __device__ __forceinline__ void enter(const Units& un, int64_t n) {
+  uint32_t u, g, rb, end;
+  __device__ __forceinline__ void enter(const Units& un, uint32_t n) {
     g = u / un.cuts;
-    rb = g * un.span + (u % un.cuts) * un.rows;
-    end = rb + un.rows;
-    end = end < (g + 1) * un.span ? end : (g + 1) * un.span;
-    end = end < n ? end : n;
+    rb = g * un.span + (u - g * un.cuts) * un.rows;
+    end = min(min(rb + un.rows, (g + 1) * un.span), n);
   }
 };
+
+// The kernel's arguments, read again: what is needed where a unit or the kernel
+// ends would otherwise stay in scalar registers over all rows, which have no room
+// for it (a wave kept 70 of them in lanes of vector registers).
+typedef const __attribute__((address_space(4))) Args* LateArgs;
+__device__ __forceinline__ LateArgs late_args() {
+  LateArgs p = (LateArgs)__builtin_amdgcn_kernarg_segment_ptr();   // (the first argument)
+  asm volatile("" : "+s"(p));
+  return p;
+}
 
 // How the gate goes by rows: a row each (or no gate), a unit of rows that share
 // one for each block, or units in turn.
@@ -251,7 +259,7 @@ residual_norm_grad_kernel(Args a, Units un, float* __restrict__ partial, float* 
   typedef typename VecOf<TZ, V>::type vec;
   __shared__ float s_sum[2][2][S::WAVES];
   __shared__ float s_part[TEAMS > 1 ? TEAMS * COLS : 1];
-  const int gl = threadIdx.x % LPR, grp = threadIdx.x / LPR;
+  const uint32_t gl = threadIdx.x % LPR, grp = S::G == 1 ? 0 : threadIdx.x / LPR;   // (a row's addresses are then uniform)
   const RowPlace<V, LPR, NV> at(gl, a.D);
   const float inv_D = 1.0f / (float)a.D, alpha = (float)a.alpha;
   const bool pre = a.pre != GBA_ROW_NORM_NONE, post = a.post != GBA_ROW_NORM_NONE;
@@ -274,7 +282,7 @@ residual_norm_grad_kernel(Args a, Units un, float* __restrict__ partial, float* 
   stream_vec h[NV] = {}, dh[NV] = {};
   vec z[NV] = {}, dy[NV] = {};
   RowStat st, stn;
-  auto row_of = [&](const UnitCursor& c) { return c.rb + grp < c.end ? c.rb + grp : c.end - 1; };
+  auto row_of = [&](const UnitCursor& c) { return (int64_t)min(c.rb + grp, c.end - 1); };
   auto load_pre = [&](int64_t r) {
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -322,8 +330,9 @@ residual_norm_grad_kernel(Args a, Units un, float* __restrict__ partial, float* 
           if (at.own(k, e)) to(at.col[k] + e, v[k][e]);
     }
   };
-  UnitCursor now{(int64_t)blockIdx.x, 0, 0, 0};
-  now.enter(un, a.n);
+  const uint32_t n = (uint32_t)a.n;
+  UnitCursor now{blockIdx.x, 0, 0, 0};
+  now.enter(un, n);
   {
     const int64_t r = row_of(now);
     st = row_stat(a, r);
@@ -338,14 +347,15 @@ residual_norm_grad_kernel(Args a, Units un, float* __restrict__ partial, float* 
     const bool leaves = next.rb >= now.end;
     if (leaves) {
       next.u += gridDim.x;
-      if (next.u < un.units) next.enter(un, a.n);
+      if (next.u < un.units) next.enter(un, n);
     }
     const bool more = next.u < un.units;
     const int64_t r = now.rb + grp, next_row = more ? row_of(next) : 0;
-    const bool active = r < now.end;   // (the last gate row's units may have no rows)
+    const bool active = now.rb + grp < now.end;   // (the last gate row's units may have no rows)
     if (each ? active : ROWS != kGateEach && entered) {
-      load_gate_row(at, a, each ? r : now.g, f);
-      gate_factors(a, f);
+      const LateArgs l = late_args();
+      load_gate_row(at, l->gate, l->gate_type, (each ? r : (int64_t)now.g) * l->gate_stride, f);
+      gate_factors(l->gate_kind, f);
     }
     if (!active) {
 #pragma unroll
@@ -371,7 +381,7 @@ residual_norm_grad_kernel(Args a, Units un, float* __restrict__ partial, float* 
           sum[3][k][e] += g;
         }
       if (more) load_pre(next_row);
-      row_sum<LPR, S::WAVES>(t, s_sum, buffer);
+      row_total<LPR, S::WAVES>(t, s_sum, buffer);
       const float m1 = a.pre == GBA_ROW_NORM_LAYER ? t[0] * inv_D : 0.0f, m2 = t[1] * inv_D;
 #pragma unroll
       for (int k = 0; k < NV; ++k)
@@ -401,20 +411,21 @@ residual_norm_grad_kernel(Args a, Units un, float* __restrict__ partial, float* 
         if (!post) kk[k][e] = g;
       }
     if (each && a.dgate && active) {
+      const LateArgs l = late_args();
       float bz[NV][V];
-      load_params(at, a.post_bias, a.weight_type, 0.0f, bz);
+      load_params(at, l->post_bias, l->weight_type, 0.0f, bz);
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         float o[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           const float u = __builtin_fmaf(zh[k][e], wz[k][e], bz[k][e]);
-          o[e] = e_[k][e] * u * (a.gate_kind == GBA_GATE_SIGMOID ? f[k][e] * (1.0f - f[k][e]) : 1.0f);
+          o[e] = e_[k][e] * u * (l->gate_kind == GBA_GATE_SIGMOID ? f[k][e] * (1.0f - f[k][e]) : 1.0f);
         }
-        const int64_t to = r * a.dgate_stride;
-        if (a.gate_type == GBA_F32) at.store_own(static_cast<float*>(a.dgate) + to, k, o);
-        else if (a.gate_type == GBA_BF16) at.store_own(static_cast<bf16_t*>(a.dgate) + to, k, o);
-        else at.store_own(static_cast<f16_t*>(a.dgate) + to, k, o);
+        const int64_t to = r * l->dgate_stride;
+        if (l->gate_type == GBA_F32) at.store_own(static_cast<float*>(l->dgate) + to, k, o);
+        else if (l->gate_type == GBA_BF16) at.store_own(static_cast<bf16_t*>(l->dgate) + to, k, o);
+        else at.store_own(static_cast<f16_t*>(l->dgate) + to, k, o);
       }
     }
     if (more) {
@@ -422,7 +433,7 @@ residual_norm_grad_kernel(Args a, Units un, float* __restrict__ partial, float* 
       load_post(next_row);
     }
     if (post) {
-      row_sum<LPR, S::WAVES>(t, s_sum, buffer);
+      row_total<LPR, S::WAVES>(t, s_sum, buffer);
       const float m1 = a.post == GBA_ROW_NORM_LAYER ? t[0] * inv_D : 0.0f, m2 = t[1] * inv_D;
 #pragma unroll
       for (int k = 0; k < NV; ++k)
@@ -443,18 +454,19 @@ residual_norm_grad_kernel(Args a, Units un, float* __restrict__ partial, float* 
     }
     if (ROWS != kGateEach && leaves) {
       if (un.gate) {
+        const LateArgs l = late_args();
         float bz[NV][V], dg[NV][V];
-        load_params(at, a.post_bias, a.weight_type, 0.0f, bz);
+        load_params(at, l->post_bias, l->weight_type, 0.0f, bz);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
           for (int e = 0; e < V; ++e)
             dg[k][e] = __builtin_fmaf(wz[k][e], sum[W][k][e], bz[k][e] * sum[W + 1][k][e]) *
-                       (a.gate_kind == GBA_GATE_SIGMOID ? f[k][e] * (1.0f - f[k][e]) : 1.0f);
+                       (l->gate_kind == GBA_GATE_SIGMOID ? f[k][e] * (1.0f - f[k][e]) : 1.0f);
         join(dg, [&](int c, float v) {
           const float o[1] = {v};
-          if (un.cuts == 1) store_part<1>(a.dgate, a.gate_type, now.g * a.dgate_stride + c, 1, o);
-          else gate_partial[now.u * a.D + c] = v;
+          if (un.cuts == 1) store_part<1>(l->dgate, l->gate_type, now.g * l->dgate_stride + c, 1, o);
+          else gate_partial[(int64_t)now.u * a.D + c] = v;
         });
       }
 #pragma unroll
@@ -476,13 +488,14 @@ residual_norm_grad_kernel(Args a, Units un, float* __restrict__ partial, float* 
     entered = leaves;
     st = stn;
   }
-  void* const outs[4] = {a.dpost_weight, a.dpost_bias, a.dpre_weight, a.dpre_bias};
+  const LateArgs l = late_args();
+  void* const outs[4] = {l->dpost_weight, l->dpost_bias, l->dpre_weight, l->dpre_bias};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if (!outs[i]) continue;
     join(sum[i], [&](int c, float v) {
       const float o[1] = {v};
-      if (gridDim.x == 1) store_part<1>(outs[i], a.grad_type, c, 1, o);   // the only block writes the sums themselves
+      if (gridDim.x == 1) store_part<1>(outs[i], l->grad_type, c, 1, o);   // the only block writes the sums themselves
       else partial[((int64_t)blockIdx.x * 4 + i) * a.D + c] = v;
     });
   }
@@ -561,9 +574,9 @@ struct RowsBackward {
   }
   template <int LPR, int NV>
   hipError_t run() const {
-    const unsigned grid = (unsigned)std::min(un.units, kUnitBlocks);
+    const unsigned grid = (unsigned)std::min<int64_t>(un.units, kUnitBlocks);
     if (!un.shared) launch<LPR, NV, kGateEach>(grid);
-    else if (un.units <= kUnitBlocks) launch<LPR, NV, kGateUnit>(grid);
+    else if ((int64_t)un.units <= kUnitBlocks) launch<LPR, NV, kGateUnit>(grid);
     else launch<LPR, NV, kGateUnits>(grid);
     return hipGetLastError();
   }
@@ -577,7 +590,7 @@ static hipError_t backward_as(const Args& a, void* ws, hipStream_t stream) {
   float* means = reinterpret_cast<float*>(static_cast<char*>(ws) + room.means);
   const Units un = units_of(a);
   const bool params = a.dpost_weight || a.dpost_bias || a.dpre_weight || a.dpre_bias;
-  const int64_t parts = std::min(un.units, kUnitBlocks);
+  const int64_t parts = std::min<int64_t>(un.units, kUnitBlocks);
   if (a.D <= kRegColumns) {
     const hipError_t e = with_grad_shape<1>(a.D, RowsBackward<TS, TZ>{a, un, partial, gate, stream});
     if (e != hipSuccess) return e;

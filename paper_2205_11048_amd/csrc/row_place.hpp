@@ -32,38 +32,43 @@ __device__ __forceinline__ float lanes_sum(float x) {
 // thread past the end); what is stored of them is what their owner stores.
 template <int V, int LPR, int NV>
 struct RowPlace {
-  int col[NV];     // first column of each vector
+  uint32_t col[NV];   // first column of each vector (unsigned: an offset from a uniform address)
   int shift;       // foreign elements of the last one
   bool last;       // the last one holds elements of this thread
-  bool tiny;       // rows narrower than a vector (LPR = NV = 1): element by element
+  bool narrow;     // rows narrower than a vector (LPR = NV = 1): element by element
   int D;
   __device__ __forceinline__ RowPlace(int gl, int width) : D(width) {
-    tiny = width < V;
+    narrow = width < V;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) col[k] = (k * LPR + gl) * V;
-    const int c = col[NV - 1];
+    for (int k = 0; k < NV; ++k) col[k] = (uint32_t)((k * LPR + gl) * V);
+    const int c = (int)col[NV - 1];
     last = c < width;
-    const int moved = tiny ? 0 : (c + V > width ? width - V : c);
+    const int moved = tiny() ? 0 : (c + V > width ? width - V : c);
     shift = c - moved < V ? c - moved : V;
-    col[NV - 1] = moved;
+    col[NV - 1] = (uint32_t)moved;
   }
+  __device__ __forceinline__ bool tiny() const { return LPR == 1 && NV == 1 && narrow; }
   __device__ __forceinline__ bool own(int k, int e) const {
-    return k + 1 < NV || (tiny ? e < D : e >= shift);
+    return k + 1 < NV || (tiny() ? e < D : e >= shift);
+  }
+  template <typename P>
+  __device__ __forceinline__ P* place(P* p, int k) const {
+    return reinterpret_cast<P*>(const_cast<char*>(reinterpret_cast<const char*>(p)) + (uint32_t)(col[k] * (uint32_t)sizeof(P)));
   }
   template <typename P>
   __device__ __forceinline__ void load(const P* __restrict__ p, int k, float (&o)[V]) const {
-    if (tiny) load_part<P, V>(p, D, o);
-    else load_vec<P, V>(p + col[k], o);
+    if (tiny()) load_part<P, V>(p, D, o);
+    else load_vec<P, V>(place(p, k), o);
   }
   // as it is in memory
   template <typename T>
   __device__ __forceinline__ typename VecOf<T, V>::type load_raw(const T* __restrict__ p, int k) const {
     typename VecOf<T, V>::type v;
-    if (tiny) {
+    if (tiny()) {
 #pragma unroll
       for (int e = 0; e < V; ++e) v[e] = e < D ? p[e] : (T)0.0f;
     } else {
-      v = *reinterpret_cast<const typename VecOf<T, V>::type*>(p + col[k]);
+      v = *reinterpret_cast<const typename VecOf<T, V>::type*>(place(p, k));
     }
     return v;
   }
@@ -79,16 +84,16 @@ struct RowPlace {
   // 50.6, 16,384 x 4096 104 and 116)
   template <typename T>
   __device__ __forceinline__ void store(T* __restrict__ p, int k, const float (&o)[V]) const {
-    if (tiny) store_part<T, V>(p, D, o);
-    else if (k + 1 < NV || last) store_vec<T, V, true>(p + col[k], o);
+    if (tiny()) store_part<T, V>(p, D, o);
+    else if (k + 1 < NV || last) store_vec<T, V, true>(place(p, k), o);
   }
   // foreign elements left out
   template <typename T>
   __device__ __forceinline__ void store_own(T* __restrict__ p, int k, const float (&o)[V]) const {
-    if (tiny) {
+    if (tiny()) {
       store_part<T, V>(p, D, o);
     } else if (k + 1 < NV || shift == 0) {
-      store_vec<T, V, true>(p + col[k], o);
+      store_vec<T, V, true>(place(p, k), o);
     } else {
 #pragma unroll
       for (int e = 0; e < V; ++e)
