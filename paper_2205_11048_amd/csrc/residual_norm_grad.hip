@@ -266,15 +266,23 @@ residual_norm_grad_kernel(Args a, Units un, float* __restrict__ partial, float* 
   const bool each = ROWS == kGateEach && a.gate_kind != GBA_GATE_NONE;
   // post's weight and bias, pre's; units in turn: of the rows' sums of e zh and e, whose place is else the first two's
   constexpr int SUMS = ROWS == kGateUnits ? 6 : 4, W = SUMS == 6 ? 4 : 0;
+  constexpr bool KEEP = NV == 1;   // the weights (two vectors of a thread leave no registers for them)
   float wz[NV][V], wh[NV][V], f[NV][V], sum[SUMS][NV][V];
-  load_params(at, a.post_weight, a.weight_type, 1.0f, wz);
-  load_params(at, a.pre_weight, a.weight_type, 1.0f, wh);
+  auto weights = [&](const void* p, int type, float (&w)[NV][V]) {
+    load_params(at, p, type, 1.0f, w);
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int e = 0; e < V; ++e) w[k][e] = at.own(k, e) ? w[k][e] : 0.0f;
+  };
+  if constexpr (KEEP) {
+    weights(a.post_weight, a.weight_type, wz);
+    weights(a.pre_weight, a.weight_type, wh);
+  }
 #pragma unroll
   for (int k = 0; k < NV; ++k)
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      wz[k][e] = at.own(k, e) ? wz[k][e] : 0.0f;
-      wh[k][e] = at.own(k, e) ? wh[k][e] : 0.0f;
       f[k][e] = 1.0f;
 #pragma unroll
       for (int i = 0; i < SUMS; ++i) sum[i][k][e] = 0.0f;
@@ -367,6 +375,10 @@ residual_norm_grad_kernel(Args a, Units un, float* __restrict__ partial, float* 
     // the stream's gradient
     float e_[NV][V], t[2] = {0.0f, 0.0f};
     if (pre) {
+      if constexpr (!KEEP) {
+        const LateArgs l = late_args();
+        weights(l->pre_weight, l->weight_type, wh);
+      }
       float xh[NV][V];
 #pragma unroll
       for (int k = 0; k < NV; ++k)
@@ -395,6 +407,10 @@ residual_norm_grad_kernel(Args a, Units un, float* __restrict__ partial, float* 
         for (int e = 0; e < V; ++e) e_[k][e] = (float)dh[k][e];
     }
     // the block's
+    if constexpr (!KEEP) {
+      const LateArgs l = late_args();
+      weights(l->post_weight, l->weight_type, wz);
+    }
     float zh[NV][V], kk[NV][V];
     t[0] = t[1] = 0.0f;
 #pragma unroll
