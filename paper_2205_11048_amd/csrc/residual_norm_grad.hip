@@ -6,6 +6,7 @@
 namespace gba {
 
 constexpr int64_t kUnitBlocks = 512;        // most partial sums of the parameters' gradients
+constexpr int kGradV = 4;                   // columns of a thread's vector
 
 // How the rows are cut into units, the rows of a gate row (or all rows) in
 // `cuts` equal parts: blocks take units in turn.
@@ -23,7 +24,10 @@ static Units units_of(const Args& a) {
   const bool shared = u.shared = a.gate_kind != GBA_GATE_NONE && a.gate_span > 1;
   u.gate = shared && a.dgate;
   const int64_t span = shared ? std::min(a.gate_span, a.n) : a.n, G = ceil_div(a.n, span);
-  const int64_t rows = ceil_div(span, std::min(span, std::max<int64_t>(1, kUnitBlocks / G))), cuts = ceil_div(span, rows);
+  int64_t lanes = 1;   // no fewer rows to a unit than a block takes at a time
+  while (lanes < kRegBlock && lanes * kGradV < a.D) lanes *= 2;
+  const int64_t rows = std::max(ceil_div(span, std::max<int64_t>(1, kUnitBlocks / G)), std::min(span, kRegBlock / lanes));
+  const int64_t cuts = ceil_div(span, rows);
   u.span = (uint32_t)span;
   u.rows = (uint32_t)rows;
   u.cuts = (uint32_t)cuts;
@@ -214,8 +218,6 @@ residual_norm_columns_kernel(Args a, const float* __restrict__ means, Units un, 
 }
 
 // ------------------------------------------------------ rows in registers
-constexpr int kGradV = 4;   // columns of a thread's vector
-
 // Where a block is in its units: at rows rb .. of unit u, whose last is end - 1.
 struct UnitCursor {
   uint32_t u, g, rb, end;
