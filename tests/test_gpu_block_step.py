@@ -1,0 +1,182 @@
+"""A training step of a sequence block through all of its operators: lookups of
+values and gates, the recurrence over packed histories, the norms with gate and
+residual, their gradients, the clipping's coefficient, and AdamW."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2205_11048_amd as gba
+from block_reference import F32, U32, close, rounded
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+HP = dict(lr=1e-2, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.1)
+MAX_NORM = 0.5
+
+
+def _bytes(n):
+    return torch.empty(n, dtype=torch.uint8, device=DEV)
+
+
+class Block:
+    """Parameters, kept buffers, and a step."""
+
+    def __init__(self, lengths, R, D, eight, seed=0):
+        rng = np.random.default_rng(seed)
+        self.lengths, self.R, self.D, self.B, n = lengths, R, D, len(lengths), sum(lengths)
+        self.n = n
+        starts = np.concatenate([[0], np.cumsum(lengths)])
+        self.offsets = torch.from_numpy(starts).to(DEV)
+        self.ids = torch.from_numpy(rng.integers(0, R, n)).to(DEV)
+        start = {"values": rng.normal(size=(R, D)), "gates": 2.0 + rng.normal(size=(R, D)), "gate": 1.0 + 0.3 * rng.normal(size=(1, D)),
+                 "post": 1.0 + 0.1 * rng.normal(size=D), "pre": 1.0 + 0.1 * rng.normal(size=D), "bias": 0.1 * rng.normal(size=D)}
+        self.names = list(start)
+        self.param = {k: torch.from_numpy(v).float().to(DEV) for k, v in start.items()}
+        self.grad = {k: torch.full_like(v, float("nan")) for k, v in self.param.items()}
+        self.wy, self.wh = (torch.from_numpy(rng.normal(size=(n, D))).float().to(DEV) for _ in range(2))
+
+        def new():
+            return torch.full((n, D), float("nan"), device=DEV)
+
+        self.x, self.a, self.u, self.h, self.y, self.dx, self.dz, self.da, self.dv = (new() for _ in range(9))
+        self.stats = {k: torch.empty(n, device=DEV) for k in ("post_rstd", "pre_mean", "pre_rstd")}
+        self.ws = _bytes(max(gba.gba_recurrence_workspace_size(n, self.B, D), gba.gba_residual_norm_grad_workspace_size(n, D),
+                             gba.gba_embedding_grad_workspace_size(n, D, R)))
+        params, grads = [self.param[k] for k in self.names], [self.grad[k] for k in self.names]
+        self.norms = gba.gba_tensor_list(grads, outs=[None] * len(grads))
+        self.norm, self.coef = torch.zeros(1, device=DEV), torch.zeros(1, device=DEV)
+        self.norm_ws = _bytes(gba.gba_grad_norm_workspace_size(self.norms))
+        kind = torch.uint8 if eight else F32
+        self.m, self.v = ([torch.zeros(p.numel(), dtype=kind, device=DEV) for p in params] for _ in range(2))
+        kw = {}
+        if eight:
+            exps = [[torch.zeros(-(-p.numel() // gba.MOMENT_BLOCK), dtype=torch.uint8, device=DEV) for p in params] for _ in range(2)]
+            kw = dict(m_exps=exps[0], v_exps=exps[1])
+            self.exps = exps
+        self.tensors = gba.gba_adamw_list(params, grads, self.m, self.v, decays=[0.0 if p.dim() == 1 else 1.0 for p in params], **kw)
+        self.t = torch.zeros(1, dtype=torch.int64, device=DEV)
+        self.err = torch.zeros(1, dtype=torch.int32, device=DEV)
+
+    def norm_args(self):
+        p = self.param
+        return dict(gate=p["gate"], gate_span=self.n, post=gba.ROW_NORM_RMS, pre=gba.ROW_NORM_LAYER, post_weight=p["post"],
+                    pre_weight=p["pre"], **self.stats)
+
+    def forward(self):
+        p = self.param
+        gba.gba_embedding_lookup(self.ids, p["values"], self.x, err=self.err)
+        gba.gba_embedding_lookup(self.ids, p["gates"], self.a, err=self.err)
+        gba.gba_recurrence(self.x, self.a, self.u, offsets=self.offsets, workspace=self.ws, err=self.err)
+        gba.gba_residual_norm(self.x, self.u, self.h, self.y, pre_bias=p["bias"], **self.norm_args())
+
+    def backward(self):
+        """Of sum(wy * y) + sum(wh * h)."""
+        g = self.grad
+        gba.gba_residual_norm_grad(self.wy, self.wh, self.u, self.h, self.dx, self.dz, self.ws, dgate=g["gate"],
+                                   dpost_weight=g["post"], dpre_weight=g["pre"], dpre_bias=g["bias"], **self.norm_args())
+        gba.gba_recurrence_grad(self.dz, self.x, self.a, self.u, self.dv, self.da, offsets=self.offsets, workspace=self.ws,
+                                err=self.err)
+        self.dv.add_(self.dx)
+        gba.gba_embedding_grad_dense(self.ids, self.dv, g["values"], self.ws, err=self.err)
+        gba.gba_embedding_grad_dense(self.ids, self.da, g["gates"], self.ws, err=self.err)
+
+    def update(self):
+        gba.gba_clip_grads(self.norms, MAX_NORM, self.norm, self.norm_ws, coef=self.coef, err=self.err)
+        self.t.add_(1)
+        gba.gba_adamw(self.tensors, **HP, t=1, t_device=self.t, seed=99, coef=self.coef, err=self.err)
+
+    def step(self):
+        self.forward()
+        self.backward()
+        self.update()
+
+    def state(self):
+        extra = self.exps[0] + self.exps[1] if hasattr(self, "exps") else []
+        return [*self.param.values(), *self.m, *self.v, *extra, self.t, self.norm]
+
+
+def plain_loss(b, p):
+    """The same in float64, by torch's own operations."""
+    x, a = p["values"][b.ids.cpu()], p["gates"][b.ids.cpu()]
+    f, rows, at = torch.sigmoid(a), [], 0
+    for length in b.lengths:
+        s = torch.zeros(b.D, dtype=torch.float64)
+        for _ in range(length):
+            s = f[at] * s + (1 - f[at]) * x[at]
+            rows.append(s)
+            at += 1
+    u = torch.stack(rows)
+    u = u / (u.square().mean(1, keepdim=True) + 1e-5).sqrt() * p["post"]
+    h = x + p["gate"] * u
+    d = h - h.mean(1, keepdim=True)
+    y = d / (d.square().mean(1, keepdim=True) + 1e-5).sqrt() * p["pre"] + p["bias"]
+    return (y * b.wy.double().cpu()).sum() + (h * b.wh.double().cpu()).sum()
+
+
+@pytest.mark.parametrize("lengths,R,D", [([7, 0, 1, 12, 30], 40, 24), ([3] * 20, 11, 130)])
+def test_the_gradients_of_a_block(lengths, R, D):
+    """Against torch's gradients of the plain form in float64.  An element passes fewer than 2^11 roundings (36 a step of
+    at most 30 positions, two norms of D / 64 + 60, sums of at most 60 tokens), each of a value within 2^3 times the
+    parameter's largest gradient (what the norms take away from each other)."""
+    b = Block(lengths, R, D, False)
+    b.forward()
+    b.backward()
+    p = {k: v.double().cpu().requires_grad_() for k, v in b.param.items()}
+    plain_loss(b, p).backward()
+    for k in b.names:
+        ref = p[k].grad.numpy()
+        close(b.grad[k], ref, np.full(ref.shape, 2.0 ** 14 * U32 * np.abs(ref).max()), k)
+    # ... and the plain form's against differences of itself
+    rng = np.random.default_rng(1)
+    with torch.no_grad():
+        v = {k: torch.from_numpy(rng.normal(size=t.shape)) for k, t in p.items()}
+        along = sum((p[k].grad * v[k]).sum() for k in p)
+        q = [sum(s * plain_loss(b, {k: p[k] + s * e * v[k] for k in p}) for s in (1, -1)) / (2 * e) for e in (2e-4, 1e-4)]
+        assert abs((4 * q[1] - q[0]) / 3 - along) < 1e-6 * sum((p[k].grad * v[k]).abs().sum() for k in p)
+    assert int(b.err) == 0
+
+
+def test_the_update_of_a_block():
+    """Clipped by the coefficient that stays on the device, and stepped: the parameters against float64."""
+    b = Block([9, 2, 17], 20, 32, False)
+    b.forward()
+    b.backward()
+    before = {k: v.double().cpu().numpy() for k, v in b.param.items()}
+    g = {k: v.double().cpu().numpy() for k, v in b.grad.items()}
+    b.update()
+    norm = np.sqrt(sum((x ** 2).sum() for x in g.values()))
+    assert norm > 2 * MAX_NORM and abs(float(b.norm) - norm) < 1e-5 * norm
+    coef = float(b.coef)
+    assert abs(coef - MAX_NORM / norm) < 1e-5 * coef
+    for k in b.names:
+        x = coef * g[k]
+        step = HP["lr"] * x / (np.abs(x) + HP["eps"])   # (the first step: m' / bc1 = x, v' / bc2 = x^2)
+        decay = HP["lr"] * HP["weight_decay"] * (before[k].ndim > 1)
+        ref = before[k] * (1 - decay) - step
+        # 32 roundings of the step, 4 of the parameter
+        close(b.param[k], ref, rounded(32 * U32 * np.abs(step) + 4 * U32 * np.abs(before[k]) + 1e-30, ref, F32), k)
+    assert int(b.err) == 0
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_steps_in_a_graph(eight):
+    """Captured once and replayed: the eager steps' bits, moments in 8 bits too."""
+    lengths = [40, 0, 3, 1, 300, 25]
+    eager, graphed = Block(lengths, 50, 64, eight, seed=5), Block(lengths, 50, 64, eight, seed=5)
+    start = [s.clone() for s in graphed.state()]
+    graphed.step()   # (what allocates or loads does so before the capture)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        graphed.step()
+    for s, was in zip(graphed.state(), start):
+        s.copy_(was)
+    for _ in range(4):
+        graphed.ws.random_(0, 256)   # nothing is kept in the workspace from step to step
+        eager.step()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager.state(), graphed.state()))
+        assert all(torch.equal(eager.grad[k], graphed.grad[k]) for k in eager.names)
+    assert int(eager.err) == 0 and int(graphed.err) == 0
+    assert not torch.equal(graphed.param["values"], start[0])

@@ -126,6 +126,12 @@ def test_long_and_ragged(dtype, D, lengths, tail, packed):
     check(Case(lengths, D, dtype, tail=tail, packed=packed))
 
 
+@pytest.mark.parametrize("dtype,D", [(F32, 3), (F32, 72), (BF16, 130), (F16, 16)])
+def test_one_long_sequence_among_short_ones(dtype, D):
+    """A few parts hold many sequences each, the others are passed by one."""
+    check(Case([2, 0, 5] * 150 + [6000] + [1, 9, 0, 0] * 100 + [1500], D, dtype, tail=9))
+
+
 @pytest.mark.parametrize("packed", [False, True])
 def test_parts_without_states(packed):
     check(Case([6000, 6000], 24, F32, state=False, packed=packed))
@@ -301,3 +307,34 @@ def test_refusals():
                 lambda: gba.gba_recurrence_workspace_size(12, 0, 16), lambda: gba.gba_recurrence_workspace_size(-1, 1, 16)]:
         with pytest.raises(gba.GBAError):
             bad()
+
+
+def test_rows_far_apart_and_many():
+    """Strides of 2^22 elements (more than 2^32 bytes from the first row to the last), and more than 2^31 elements."""
+    c = Case([150] * 4, 40, BF16, packed=False)
+    want, last = c.forward()
+    dx, da, d0 = c.backward(want)
+    far = torch.empty(600 << 22, dtype=BF16, device=DEV).as_strided((600, 40), (1 << 22, 1))
+    far.copy_(c.x)
+    near, c.x = c.x, far
+    h, _ = c.forward()
+    assert torch.equal(h, want)
+    assert torch.equal(c.backward(want)[1], da)
+    c.x = near
+    gba.gba_recurrence(c.x, c.a, far, h0=_dev(c.h0), workspace=c.ws, **c.by)
+    assert torch.equal(far, want)
+    del far
+    n, D, L = 3 << 23, 90, 64
+    x, a = (torch.randn((L, D), device=DEV).to(BF16) for _ in range(2))
+    h = torch.empty_like(x)
+    gba.gba_recurrence(x, a, h, length=L, workspace=_ws(L, 1, D))
+    bound = 2 * 36 * 64 * U32   # (tiles lie elsewhere in the sequences: each is within 36 u a step of the exact state)
+    X, A = (t.repeat(n // L, 1) for t in (x, a))
+    ws = _ws(n, n // L, D)
+    for packed in (False, True):
+        by = dict(offsets=torch.arange(0, n + 1, L, device=DEV)) if packed else dict(length=L)
+        H = torch.full_like(X, float("nan"))
+        gba.gba_recurrence(X, A, H, workspace=ws, **by)
+        # (in bf16 the states are an ulp apart where they lie next to a border)
+        for part in H.view(n // L, L, D).split(1 << 16):
+            assert ((part.float() - h.float()).abs() <= 2.0 ** -7 * h.float().abs() + 8 * bound).all()

@@ -176,7 +176,9 @@ def check_backward(c, h, h64):
         B = np.abs(u * c.df64) * Be + np.abs(e * c.df64) * Bu + np.abs(e * u) * df_err + 3 * U32 * np.abs(each)
         G = c.g64.shape[0]
         ref, bound, size, count = (np.zeros((G, D)) for _ in range(4))
-        for to, val in ((ref, each), (bound, B), (size, np.abs(each)), (count, np.ones_like(each))):
+        # (rows that share a gate add up e * zh and e apart: their sum is w * one + b * the other, whose terms are these)
+        terms = np.abs(e * c.df64) * (np.abs(zh * c.wz64) + np.abs(c.bz64)) if c.span > 1 else np.abs(each)
+        for to, val in ((ref, each), (bound, B), (size, terms), (count, np.ones_like(each))):
             np.add.at(to, c.rows, val)
         close(dg, ref, rounded(bound + (count + 4) * U32 * size * (c.span > 1), ref, c.gtype), "dgate")
     if c.post == "none":
@@ -388,3 +390,33 @@ def test_refusals():
                 lambda: gba.gba_residual_norm_grad_workspace_size(-1, 16), lambda: gba.gba_residual_norm_grad_workspace_size(5, 0)]:
         with pytest.raises(gba.GBAError):
             bad()
+
+
+def test_rows_far_apart_and_many():
+    """Strides of 2^22 elements (more than 2^32 bytes from the first row to the last), and more than 2^31 elements."""
+    n, D = 600, 96
+    far = torch.empty(n << 22, dtype=BF16, device=DEV).as_strided((n, D), (1 << 22, 1))
+    x, z = torch.randn((n, D), device=DEV).to(BF16), torch.randn((n, D), device=DEV).to(BF16)
+    want, got = [torch.empty_like(x) for _ in range(2)], [torch.empty_like(x) for _ in range(2)]
+    gba.gba_residual_norm(x, z, *want)
+    far.copy_(z)
+    gba.gba_residual_norm(x, far, *got)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    far.copy_(x)
+    gba.gba_residual_norm(far, z, far, got[1])
+    assert torch.equal(far, want[0]) and torch.equal(got[1], want[1])
+    stats = dict(post_rstd=torch.rand(n, device=DEV), pre_rstd=torch.rand(n, device=DEV))
+    grads = [[torch.empty_like(x) for _ in range(2)] for _ in range(2)]
+    gba.gba_residual_norm_grad(x, x, z, want[0], *grads[0], _ws(n, D), **stats)
+    far.copy_(want[0])
+    gba.gba_residual_norm_grad(x, x, z, far, *grads[1], _ws(n, D), **stats)
+    assert all(torch.equal(p, q) for p, q in zip(*grads))
+    del far
+    n = (1 << 25) + 3
+    x, z = x[:1].expand(n, D).contiguous(), z[:1].expand(n, D).contiguous()
+    h, y = torch.empty_like(x), torch.empty_like(x)
+    gba.gba_residual_norm(x, z, h, y)
+    assert (h == want[0][0]).all() and (y == want[1][0]).all()
+    stats = dict(post_rstd=torch.ones(n, device=DEV), pre_rstd=torch.ones(n, device=DEV))
+    gba.gba_residual_norm_grad(y, z, z, h, x, y, _ws(n, D), **stats)
+    assert (x == x[0]).all() and (y == y[0]).all()
