@@ -23,6 +23,12 @@
 // launch maps what a part hands on to the next: the positions from its last
 // sequence's beginning on (nothing where that ends with the part).  A block of the
 // second launch joins the maps of those parts that the sequence passes before.
+//
+// Bound by bytes: 32 sequences of 1024 positions of 2048 columns bf16 92 us (403 MB,
+// 4.4 TB/s where a large copy has 5.2), their like of 1024 columns f32 75; the
+// gradient over 16 of 2048 of 2048 bf16 166 us (805 MB, 4.8 TB/s).  Cut sequences
+// are read twice in part: the gradient over one of 100,003 positions of 511
+// columns f32 337 us, of which the maps are 74.
 #include <algorithm>
 
 #include "elements.hpp"
@@ -33,12 +39,23 @@ namespace gba {
 
 constexpr int kScanBlock = 256;
 constexpr int kScanWaves = kScanBlock / kWave;
-constexpr int kScanV = 4;                  // columns of a lane
-constexpr int kScanLanes = 32;             // most lanes over the columns of a block
+// Columns of a lane, and most lanes over the columns of a block: rows by 256 or 512
+// bytes (one sequence of 100,003 x 511 f32, the gradient: by 128 bytes 525 us, 256 449,
+// 512 385).  With two columns of a lane twice as many loads: 32 x 1024 x 2048 bf16
+// 110 us -> 126; with eight (16 bytes of bf16) 112.
+constexpr int kScanV = 4;
+constexpr int kScanLanes = 32;
 constexpr int kScanWidest = kScanLanes * kScanV;
-constexpr int kScanSimd = 2;               // waves of a SIMD that the registers are for
-constexpr int64_t kScanBlocks = 256 * kScanSimd;   // ... and so the blocks of a round, a wave of each on every SIMD
-constexpr int64_t kScanSplitBelow = 192;   // blocks
+// Waves of a SIMD that the registers are for: with three or four of them and tiles of
+// half as many positions, or with spilled registers, the same 125 to 140 us.
+constexpr int kScanSimd = 2;
+// Blocks of a round, a wave of each on every SIMD, that parts are made for: histories
+// of 4096 users of 64 columns, cut between sequences, 48 us, with twice as many parts 52,
+// four times 59.
+constexpr int64_t kScanBlocks = 256 * kScanSimd;
+// Sequences of equal length are cut below as many blocks of whole ones: the maps read
+// two arrays again, of three or (the gradient's) six.
+constexpr int64_t kScanSplitBelow = 192;
 
 __host__ __device__ static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 static inline size_t align_up(size_t x) { return (x + 255) & ~size_t(255); }
@@ -105,7 +122,8 @@ __device__ __forceinline__ void wave_find(const int64_t* offsets, int64_t B, int
 }
 
 // Where a block is in the order of parts and groups: blocks go to the eight dies
-// in turn, and neighbours, which read the same rows, come to one die.
+// in turn, and neighbours, which read the same rows, come to one die (the gradient
+// of 100,003 x 511 f32 449 us -> 437, of 16 x 2048 x 2048 bf16 182 -> 173).
 __device__ __forceinline__ unsigned block_place(unsigned n) {
   constexpr unsigned kDies = 8;
   const unsigned each = n / kDies, more = n % kDies, die = blockIdx.x % kDies;
@@ -184,7 +202,8 @@ struct Affine {
   }
 };
 
-// Positions of a lane.
+// Positions of a lane: what the registers hold beside the next tile (4 forward:
+// 32 x 1024 x 2048 bf16 100 us -> 125; 2 backward: 16 x 2048 x 2048 bf16 185 -> 199, 5 203).
 template <bool GRAD>
 constexpr int kScanT = GRAD ? 4 : 8;
 
@@ -369,14 +388,17 @@ struct Bounds {
 // A lane's place in a matrix, in bytes from a tile's first row: `slot` and
 // column.  The rows of a tile are then at a uniform address each, to which this
 // is added (the compiler would otherwise hold a pointer per row and matrix in
-// registers, twice as many as the tile itself takes).
+// registers, twice as many as the tile itself takes: the gradient of f32 spilled
+// 276 bytes of a lane).
 template <typename X>
 __device__ __forceinline__ uint64_t lane_place(int64_t stride, int64_t row, int col) {
   return (uint64_t)(row * stride + col) * sizeof(X);
 }
 __device__ __forceinline__ void keep_place(uint64_t& place) { asm volatile("" : "+v"(place)); }
 
-// A matrix's rows from a uniform one on.
+// A matrix's rows from a uniform one on.  Read and (ScanColumns) written past the
+// caches, each being touched once: 32 x 1024 x 2048 bf16 109 us -> 103, the gradient of
+// 16 x 2048 x 2048 186 -> 177, of 100,003 x 511 f32 382 -> 353.
 template <typename X>
 struct RowsFrom {
   char* first;
@@ -900,7 +922,8 @@ static hipError_t scan_as(const ScanArgs& a, void* ws, int32_t* err, hipStream_t
   if (D < V) return scan_in<X, 4, 1, GRAD>(a, ws, err, stream);
   if (D <= 4 * V) return scan_in<X, 4, V, GRAD>(a, ws, err, stream);
   if (D <= 8 * V) return scan_in<X, 8, V, GRAD>(a, ws, err, stream);
-  // fewer columns to a block where the sequences are then enough blocks, and are too few for what memory takes at once
+  // 64 columns to a block, not 128, where these are too few blocks for what memory takes at once (the gradient of
+  // 16 x 2048 x 2048 bf16 225 us -> 175; but 256 blocks of f32 are enough: 32 x 1024 x 1024 75, with 64 columns 86)
   const int64_t blocks = a.r.B * ceil_div(D, kScanWidest);
   const bool few = !a.seq && blocks * (int64_t)sizeof(X) < kScanBlocks * 2 && 2 * blocks >= kScanSplitBelow;
   if (D <= 16 * V || few) return scan_in<X, 16, V, GRAD>(a, ws, err, stream);
