@@ -26,9 +26,9 @@
 //
 // Bound by bytes: 32 sequences of 1024 positions of 2048 columns bf16 92 us (403 MB,
 // 4.4 TB/s where a large copy has 5.2), their like of 1024 columns f32 75; the
-// gradient over 16 of 2048 of 2048 bf16 166 us (805 MB, 4.8 TB/s).  Cut sequences
+// gradient over 16 of 2048 of 2048 bf16 166 to 171 us (805 MB, 4.8 TB/s).  Cut sequences
 // are read twice in part: the gradient over one of 100,003 positions of 511
-// columns f32 337 us, of which the maps are 74.
+// columns f32 336 us, of which the maps are 74.
 #include <algorithm>
 
 #include "elements.hpp"
@@ -284,6 +284,8 @@ __device__ __forceinline__ void scan_join(Affine<V>& m, Affine<V>& carry, float 
     }
     x.forget = __shfl_up((int)m.forget, LPC, kWave) != 0;
   }
+  Affine<V> tile;
+  if constexpr (MAP) tile.clear();
   __syncthreads();
 #pragma unroll JOIN
   for (int k = 0; k < kScanWaves; ++k) {
@@ -299,12 +301,13 @@ __device__ __forceinline__ void scan_join(Affine<V>& m, Affine<V>& carry, float 
     }
     b.forget = s.forget[buffer][k] != 0;
     if constexpr (MAP) {
-      b.after(carry);
-      carry = b;
+      b.after(tile);
+      tile = b;
     } else {
       b.apply(carry.S);
     }
   }
+  if constexpr (MAP) carry.after(tile);
   buffer ^= 1;
   if constexpr (!MAP)
     if (lane >= LPC) x.apply(in);
@@ -409,10 +412,11 @@ struct RowsFrom {
   __device__ __forceinline__ X* at(int i, uint64_t place) const {
     return reinterpret_cast<X*>(first + i * step + place);
   }
-  template <int V>
+  template <int V, bool PAST = true>
   __device__ __forceinline__ typename VecOf<X, V>::type load(int i, uint64_t place) const {
     typedef typename VecOf<X, V>::type vec;
-    return __builtin_nontemporal_load(reinterpret_cast<const vec*>(at(i, place)));
+    const vec* p = reinterpret_cast<const vec*>(at(i, place));
+    return PAST ? __builtin_nontemporal_load(p) : *p;
   }
 };
 
@@ -473,15 +477,15 @@ __device__ __forceinline__ void map_part(const ScanArgs& a, int part, int group,
     if (t >= q0 && t + Sh::TILE <= q1) {
 #pragma unroll
       for (int i = 0; i < T; ++i) {
-        g[i] = rows_a.template load<V>(i, place_a);
-        x[i] = rows_x.template load<V>(i, place_x);
+        g[i] = rows_a.template load<V, false>(i, place_a);
+        x[i] = rows_x.template load<V, false>(i, place_x);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < T; ++i) {
         if (q + i < q0 || q + i >= q1) continue;
-        g[i] = rows_a.template load<V>(i, place_a);
-        x[i] = rows_x.template load<V>(i, place_x);
+        g[i] = rows_a.template load<V, false>(i, place_a);
+        x[i] = rows_x.template load<V, false>(i, place_x);
       }
     }
   };
@@ -489,7 +493,9 @@ __device__ __forceinline__ void map_part(const ScanArgs& a, int part, int group,
   Affine<V> carry;
   carry.clear();
   const int64_t tiles = (q1 - q0 + Sh::TILE - 1) / Sh::TILE;
-  auto tile = [&](int64_t k) { return GRAD ? q1 - (k + 1) * Sh::TILE : q0 + k * Sh::TILE; };
+  // the tiles the other way round than the second launch, and through the caches, where it finds the last ones (the gradient
+  // over 100,003 x 511 f32 357 us -> 336, over 2 x 50,000 x 512 bf16 178 -> 172, forward 126 -> 120; histories the same)
+  auto tile = [&](int64_t k) { return GRAD ? q1 - (tiles - k) * Sh::TILE : q0 + (tiles - 1 - k) * Sh::TILE; };
   load(tile(0));
   for (int64_t k = 0; k < tiles; ++k) {
     const int64_t t = tile(k), q = t + place;
@@ -515,7 +521,7 @@ __device__ __forceinline__ void map_part(const ScanArgs& a, int part, int group,
     Affine<V> m;
     m.forget = false;
     if constexpr (GRAD) {
-      const bool last = k == 0 && slot == 0 && forget;
+      const bool last = k == tiles - 1 && slot == 0 && forget;
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         m.S[e] = f[T - 1][e] * (last ? v[T - 1][e] + h0[e] : v[T - 1][e]);
@@ -529,7 +535,7 @@ __device__ __forceinline__ void map_part(const ScanArgs& a, int part, int group,
           m.F[e] *= f[i][e];
         }
     } else {
-      const bool first = k == 0 && slot == 0 && forget;
+      const bool first = k == tiles - 1 && slot == 0 && forget;
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         m.S[e] = first ? __builtin_fmaf(f[0][e], h0[e], v[0][e]) : v[0][e];

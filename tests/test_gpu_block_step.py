@@ -180,3 +180,45 @@ def test_steps_in_a_graph(eight):
         assert all(torch.equal(eager.grad[k], graphed.grad[k]) for k in eager.names)
     assert int(eager.err) == 0 and int(graphed.err) == 0
     assert not torch.equal(graphed.param["values"], start[0])
+
+
+def test_two_graphs_share_a_workspace():
+    """Of different sizes, replayed in turn on one stream, with eager steps between."""
+    shapes = [([5, 600, 0, 31], 30, 48), ([70, 2], 9, 136)]
+    graphed, eager = ([Block(*shape, True, seed=k) for k, shape in enumerate(shapes)] for _ in range(2))
+    shared = _bytes(max(b.ws.numel() for b in graphed))
+    graphs = []
+    for b in graphed:
+        b.ws = shared
+        start = [s.clone() for s in b.state()]
+        b.step()
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            b.step()
+        for s, was in zip(b.state(), start):
+            s.copy_(was)
+    for k in (0, 1, 1, 0, 0, 1):
+        graphs[k].replay()
+        eager[k].step()
+    torch.cuda.synchronize()
+    for a, b in zip(graphed, eager):
+        assert all(torch.equal(s, t) for s, t in zip(a.state(), b.state())) and int(a.err) == 0
+
+
+def test_two_streams_at_once():
+    """Each with its own buffers and workspace: the results of one after the other."""
+    lengths = [900, 0, 41, 3000]
+    blocks, alone = [Block(lengths, 64, 64, k == 1, seed=k) for k in range(2)], [Block(lengths, 64, 64, k == 1, seed=k) for k in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for b, s in zip(blocks, streams):
+            with torch.cuda.stream(s):
+                b.step()
+    torch.cuda.synchronize()
+    for b in alone:
+        for _ in range(3):
+            b.step()
+    for a, b in zip(blocks, alone):
+        assert all(torch.equal(s, t) for s, t in zip(a.state(), b.state())) and int(a.err) == 0
