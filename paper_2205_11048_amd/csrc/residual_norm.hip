@@ -199,7 +199,7 @@ residual_norm_kernel(Args a, int64_t per, uint32_t span) {
         v[k][e] = (float)(TS)v[k][e];   // what pre normalises is the stream as it is stored
       }
     if (a.pre != GBA_ROW_NORM_NONE) row_stats<LPR, S::WAVES>(at, a.pre, D, eps, v, s_sum, buffer, pre_mean, pre_rstd);
-    else if (LPR > kWave && a.post == GBA_ROW_NORM_NONE) __syncthreads();   // h may be x, and rows' last vectors overlap
+    else if (LPR > kWave) __syncthreads();   // h may be x, and the last vectors overlap: all of the row has been read
     if (active) {
       if (gl == 0) {
         if (a.post_mean) a.post_mean[r] = mean;
