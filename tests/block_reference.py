@@ -39,13 +39,19 @@ def sigmoids(a):
 # A step's gate is off by at most 8 u of the smaller of f and 1 - f (the power of two 3 u, the sum, the reciprocal 2 u
 # and the product); a step adds the difference's rounding and its own.  Where maps of steps are joined F is a product of
 # f's, off by 9 u a step, and each join (fewer than 20 a tile) rounds once.  With A the recurrence of magnitudes, 12 u A a
-# step and 24 u A for the joins bound it.
+# step and 24 u A for the joins bound it.  With 16-bit inputs the power of two is taken of a * log2(e) as it is rounded: the
+# smaller of f and 1 - f is off by |a| u more, f (of which it is the whole, or the part 1 - f) by as much of itself at most.
 STEP = 36 * U32
 
 
-def recurrence(x, a, starts, h0):
+def gate_error(a, dtype):
+    return np.zeros_like(a) if dtype == F32 else np.abs(a) * U32
+
+
+def recurrence(x, a, starts, h0, dtype=F32):
     """h, the last states and their bounds; sequence b holds positions starts[b] .. starts[b + 1] - 1."""
     f, i = sigmoids(a)
+    more = gate_error(a, dtype)
     h, E = np.zeros_like(x), np.zeros_like(x)
     last, E_last = h0.copy(), np.zeros_like(h0)
     for b in range(len(starts) - 1):
@@ -53,16 +59,17 @@ def recurrence(x, a, starts, h0):
         for t in range(starts[b], starts[b + 1]):
             s = f[t] * s + i[t] * x[t]
             A = f[t] * A + i[t] * np.abs(x[t])
-            e = f[t] * e + STEP * A
+            e = f[t] * e + (STEP + more[t]) * A
             h[t], E[t] = s, e
         if starts[b + 1] > starts[b]:
             last[b], E_last[b] = s, e
     return h, last, E, E_last
 
 
-def recurrence_grad(dh, x, a, h, starts, h0, dlast):
+def recurrence_grad(dh, x, a, h, starts, h0, dlast, dtype=F32):
     """dx, da, dh0 and their bounds."""
     f, i = sigmoids(a)
+    more = gate_error(a, dtype)
     dx, da, Ex, Ea = (np.zeros_like(x) for _ in range(4))
     d0, E0 = dlast.copy(), np.zeros_like(dlast)
     for b in range(len(starts) - 1):
@@ -71,12 +78,12 @@ def recurrence_grad(dh, x, a, h, starts, h0, dlast):
             g, G = dh[t] + c, np.abs(dh[t]) + C
             eg = e + 2 * U32 * G
             before = h[t - 1] if t > starts[b] else h0[b]
-            dx[t], Ex[t] = i[t] * g, i[t] * eg + 10 * U32 * i[t] * G
+            dx[t], Ex[t] = i[t] * g, i[t] * eg + (10 * U32 + more[t]) * i[t] * G
             diff, D = before - x[t], np.abs(before) + np.abs(x[t])
             da[t] = g * diff * f[t] * i[t]
-            Ea[t] = (np.abs(diff) * eg + 22 * U32 * G * D) * f[t] * i[t]
+            Ea[t] = (np.abs(diff) * eg + (22 * U32 + 2 * more[t]) * G * D) * f[t] * i[t]
             c, C = f[t] * g, f[t] * G
-            e = f[t] * eg + STEP * C
+            e = f[t] * eg + (STEP + more[t]) * C
         if starts[b + 1] > starts[b]:
             d0[b], E0[b] = c, e
     return dx, da, d0, Ex, Ea, E0

@@ -67,14 +67,14 @@ class Case:
 def check(c):
     h, last = c.forward()
     h0 = c.h0.astype(np.float64) if c.h0 is not None else c.zeros()
-    ref, rlast, E, El = recurrence(c.x64, c.a64, c.starts, h0)
+    ref, rlast, E, El = recurrence(c.x64, c.a64, c.starts, h0, c.dtype)
     close(h[:c.used], ref[:c.used], rounded(E, ref, c.dtype)[:c.used], "h")
     close(last, rlast, rounded(El, rlast, F32), "h_last")
     assert (h[c.used:] == 7.0).all()
     dx, da, d0 = c.backward(h)
     h64 = h.double().cpu().numpy()
     dl = c.dlast.astype(np.float64) if c.dlast is not None else c.zeros()
-    rx, ra, r0, Ex, Ea, E0 = recurrence_grad(c.dh64, c.x64, c.a64, h64, c.starts, h0, dl)
+    rx, ra, r0, Ex, Ea, E0 = recurrence_grad(c.dh64, c.x64, c.a64, h64, c.starts, h0, dl, c.dtype)
     close(dx[:c.used], rx[:c.used], rounded(Ex, rx, c.dtype)[:c.used], "dx")
     close(da[:c.used], ra[:c.used], rounded(Ea, ra, c.dtype)[:c.used], "da")
     close(d0, r0, rounded(E0, r0, F32), "dh0")
