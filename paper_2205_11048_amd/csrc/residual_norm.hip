@@ -139,7 +139,7 @@ residual_norm_kernel(Args a, int64_t per, uint32_t span) {
   typedef typename VecOf<TZ, V>::type vec;
   __shared__ float s_sum[2][1][S::WAVES];
   const int gl = threadIdx.x % LPR, grp = S::G == 1 ? 0 : threadIdx.x / LPR;   // (a row's addresses are then uniform)
-  const RowPlace<V, LPR, NV> at(gl, a.D);
+  const RowPlace<V, LPR, NV, false> at(gl, a.D);
   const float D = (float)a.D, eps = (float)a.eps, alpha = (float)a.alpha;
   float wz[NV][V], bz[NV][V], wh[NV][V], bh[NV][V], f[NV][V], fn[NV][V];
   load_params(at, a.post_weight, a.weight_type, 1.0f, wz);

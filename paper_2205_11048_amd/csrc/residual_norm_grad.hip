@@ -269,7 +269,7 @@ residual_norm_grad_kernel(Args a, Units un, float* __restrict__ partial, float* 
   __shared__ float s_sum[2][2][S::WAVES];
   __shared__ float s_part[TEAMS > 1 ? TEAMS * COLS : 1];
   const uint32_t gl = threadIdx.x % LPR, grp = S::G == 1 ? 0 : threadIdx.x / LPR;   // (a row's addresses are then uniform)
-  const RowPlace<V, LPR, NV> at(gl, a.D);
+  const RowPlace<V, LPR, NV, false> at(gl, a.D);
   const float inv_D = 1.0f / (float)a.D, alpha = (float)a.alpha;
   const bool pre = a.pre != GBA_ROW_NORM_NONE, post = a.post != GBA_ROW_NORM_NONE;
   const bool each = ROWS == kGateEach && a.gate_kind != GBA_GATE_NONE;

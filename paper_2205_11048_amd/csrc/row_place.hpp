@@ -30,7 +30,10 @@ __device__ __forceinline__ float lanes_sum(float x) {
 // pass the row's end: it is moved back to end there, its first `shift`
 // elements belong to other threads and count for nothing (all V of them in a
 // thread past the end); what is stored of them is what their owner stores.
-template <int V, int LPR, int NV>
+// CHECK: every shape looks for narrow rows, not only the one that can have them
+// (layer norm in half: how far the compiler joins products and conversions, and so
+// the last bit, goes by it).
+template <int V, int LPR, int NV, bool CHECK = true>
 struct RowPlace {
   uint32_t col[NV];   // first column of each vector (unsigned: an offset from a uniform address)
   int shift;       // foreign elements of the last one
@@ -47,7 +50,7 @@ struct RowPlace {
     shift = c - moved < V ? c - moved : V;
     col[NV - 1] = (uint32_t)moved;
   }
-  __device__ __forceinline__ bool tiny() const { return LPR == 1 && NV == 1 && narrow; }
+  __device__ __forceinline__ bool tiny() const { return (CHECK || (LPR == 1 && NV == 1)) && narrow; }
   __device__ __forceinline__ bool own(int k, int e) const {
     return k + 1 < NV || (tiny() ? e < D : e >= shift);
   }
