@@ -22,8 +22,10 @@ struct Units {
   uint32_t cuts;     // units of it
   uint32_t rows;     // of a unit
   uint32_t units;
+  uint32_t gates;    // rows of the gate
   bool shared;       // rows share the gate
   bool gate;         // ... and its gradient is asked for
+  bool groups;       // a gate row for each group of lanes: units are as many gate rows as a block has groups
 };
 static Units units_of(const Args& a) {
   Units u;
@@ -36,6 +38,17 @@ static Units units_of(const Args& a) {
   const int64_t rows = std::max(ceil_div(span, std::max<int64_t>(1, kUnitBlocks / G)), std::min(span, kRegBlock / lanes));
   const int64_t cuts = ceil_div(span, rows);
   u.span = (uint32_t)span;
+  u.gates = (uint32_t)G;
+  // Few rows to a gate row, and many of these: side by side, not in turn by a block that has lanes for more rows
+  // (239,128 x 32, bf16 beside a stream of f32, a gate for each ten rows 130 us -> 41; 200,000 x 128 bf16, one for each
+  // four, 263 -> 70).  A block in turn takes gates / kUnitBlocks of them, a step each; side by side a step for each row.
+  u.groups = shared && span < kRegBlock / lanes && G > kUnitBlocks * span;
+  if (u.groups) {
+    u.rows = u.span;
+    u.cuts = 1;
+    u.units = (uint32_t)ceil_div(G, kRegBlock / lanes);
+    return u;
+  }
   u.rows = (uint32_t)rows;
   u.cuts = (uint32_t)cuts;
   u.units = (uint32_t)(G * cuts);   // (below 2 n)
@@ -246,8 +259,9 @@ __device__ __forceinline__ LateArgs late_args() {
 }
 
 // How the gate goes by rows: a row each (or no gate), a unit of rows that share
-// one for each block, or units in turn.
-enum GateRows { kGateEach, kGateUnit, kGateUnits };
+// one for each block, units in turn, or a gate row for each group of lanes, which
+// takes its rows one after another.
+enum GateRows { kGateEach, kGateUnit, kGateUnits, kGateGroups };
 
 // A thread keeps its columns of the parameters' sums and of the weights in
 // registers from row to row.  Foreign columns (RowPlace) have weights of 0, so
@@ -274,7 +288,8 @@ residual_norm_grad_kernel(Args a, Units un, float* __restrict__ partial, float* 
   const bool pre = a.pre != GBA_ROW_NORM_NONE, post = a.post != GBA_ROW_NORM_NONE;
   const bool each = ROWS == kGateEach && a.gate_kind != GBA_GATE_NONE;
   // post's weight and bias, pre's; units in turn: of the rows' sums of e zh and e, whose place is else the first two's
-  constexpr int SUMS = ROWS == kGateUnits ? 6 : 4, W = SUMS == 6 ? 4 : 0;
+  constexpr bool GROUPS = ROWS == kGateGroups;
+  constexpr int SUMS = ROWS == kGateUnits || GROUPS ? 6 : 4, W = SUMS == 6 ? 4 : 0;
   constexpr bool KEEP = NV == 1;   // the weights (two vectors of a thread leave no registers for them)
   float wz[NV][V], wh[NV][V], f[NV][V], sum[SUMS][NV][V];
   auto weights = [&](const void* p, int type, float (&w)[NV][V]) {
@@ -299,7 +314,9 @@ residual_norm_grad_kernel(Args a, Units un, float* __restrict__ partial, float* 
   stream_vec h[NV] = {}, dh[NV] = {};
   vec z[NV] = {}, dy[NV] = {};
   RowStat st, stn;
-  auto row_of = [&](const UnitCursor& c) { return (int64_t)min(c.rb + grp, c.end - 1); };
+  const uint32_t n = (uint32_t)a.n;
+  auto place_of = [&](const UnitCursor& c) { return GROUPS ? (c.g + grp) * un.span + c.rb : c.rb + grp; };
+  auto row_of = [&](const UnitCursor& c) { return (int64_t)min(place_of(c), (GROUPS ? n : c.end) - 1); };
   auto load_pre = [&](int64_t r) {
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -347,9 +364,18 @@ residual_norm_grad_kernel(Args a, Units un, float* __restrict__ partial, float* 
           if (at.own(k, e)) to(at.col[k] + e, v[k][e]);
     }
   };
-  const uint32_t n = (uint32_t)a.n;
+  // (GROUPS: g is the first group's gate row, and rb .. end - 1 are places in the gate rows)
+  auto enter = [&](UnitCursor& c) {
+    if constexpr (GROUPS) {
+      c.g = c.u * S::G;
+      c.rb = 0;
+      c.end = un.span;
+    } else {
+      c.enter(un, n);
+    }
+  };
   UnitCursor now{blockIdx.x, 0, 0, 0};
-  now.enter(un, n);
+  enter(now);
   {
     const int64_t r = row_of(now);
     st = row_stat(a, r);
@@ -360,18 +386,18 @@ residual_norm_grad_kernel(Args a, Units un, float* __restrict__ partial, float* 
   int buffer = 0;
   for (;;) {
     UnitCursor next = now;
-    next.rb += S::G;
+    next.rb += GROUPS ? 1 : S::G;
     const bool leaves = next.rb >= now.end;
     if (leaves) {
       next.u += gridDim.x;
-      if (next.u < un.units) next.enter(un, n);
+      if (next.u < un.units) enter(next);
     }
     const bool more = next.u < un.units;
-    const int64_t r = now.rb + grp, next_row = more ? row_of(next) : 0;
-    const bool active = now.rb + grp < now.end;   // (the last gate row's units may have no rows)
+    const int64_t r = place_of(now), next_row = more ? row_of(next) : 0;
+    const bool active = place_of(now) < (GROUPS ? n : now.end);   // (the last gate row's units may have no rows)
     if (each ? active : ROWS != kGateEach && entered) {
       const LateArgs l = late_args();
-      load_gate_row(at, l->gate, l->gate_type, (each ? r : (int64_t)now.g) * l->gate_stride, f);
+      load_gate_row(at, l->gate, l->gate_type, (each ? r : (int64_t)(GROUPS ? min(now.g + grp, un.gates - 1) : now.g)) * l->gate_stride, f);
       gate_factors(l->gate_kind, f);
     }
     if (!active) {
@@ -488,17 +514,29 @@ residual_norm_grad_kernel(Args a, Units un, float* __restrict__ partial, float* 
           for (int e = 0; e < V; ++e)
             dg[k][e] = __builtin_fmaf(wz[k][e], sum[W][k][e], bz[k][e] * sum[W + 1][k][e]) *
                        (l->gate_kind == GBA_GATE_SIGMOID ? f[k][e] * (1.0f - f[k][e]) : 1.0f);
-        join(dg, [&](int c, float v) {
-          const float o[1] = {v};
-          if (un.cuts == 1) store_part<1>(l->dgate, l->gate_type, now.g * l->dgate_stride + c, 1, o);
-          else gate_partial[(int64_t)now.u * a.D + c] = v;
-        });
+        if constexpr (GROUPS) {
+          const int64_t to = (int64_t)(now.g + grp) * l->dgate_stride;
+          if (now.g + grp < un.gates) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+              if (l->gate_type == GBA_F32) at.store_own(static_cast<float*>(l->dgate) + to, k, dg[k]);
+              else if (l->gate_type == GBA_BF16) at.store_own(static_cast<bf16_t*>(l->dgate) + to, k, dg[k]);
+              else at.store_own(static_cast<f16_t*>(l->dgate) + to, k, dg[k]);
+            }
+          }
+        } else {
+          join(dg, [&](int c, float v) {
+            const float o[1] = {v};
+            if (un.cuts == 1) store_part<1>(l->dgate, l->gate_type, now.g * l->dgate_stride + c, 1, o);
+            else gate_partial[(int64_t)now.u * a.D + c] = v;
+          });
+        }
       }
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          if constexpr (ROWS == kGateUnits) {
+          if constexpr (SUMS == 6) {
             sum[0][k][e] = __builtin_fmaf(f[k][e], sum[W][k][e], sum[0][k][e]);
             sum[1][k][e] = __builtin_fmaf(f[k][e], sum[W + 1][k][e], sum[1][k][e]);
             sum[W][k][e] = sum[W + 1][k][e] = 0.0f;
@@ -598,9 +636,14 @@ struct RowsBackward {
                        0, stream, a, un, partial, gate);
   }
   template <int LPR, int NV>
+  void launch_groups(unsigned grid) const {
+    if constexpr (NormShape<kGradV, LPR, NV>::G > 1) launch<LPR, NV, kGateGroups>(grid);
+  }
+  template <int LPR, int NV>
   hipError_t run() const {
     const unsigned grid = (unsigned)std::min<int64_t>(un.units, kUnitBlocks);
     if (!un.shared) launch<LPR, NV, kGateEach>(grid);
+    else if (un.groups) launch_groups<LPR, NV>(grid);
     else if ((int64_t)un.units <= kUnitBlocks) launch<LPR, NV, kGateUnit>(grid);
     else launch<LPR, NV, kGateUnits>(grid);
     return hipGetLastError();

@@ -258,6 +258,14 @@ def test_rows_that_share_a_gate(n, D, span):
     check(n, D, BF16, BF16, gate="sigmoid", span=span, gtype=BF16, post="layer")
 
 
+@pytest.mark.parametrize("n,D,span", [(2501, 8, 2), (4801, 24, 3), (2100, 130, 2), (4700, 300, 3), (2200, 2, 2), (40_000, 16, 8)])
+def test_many_gates_of_few_rows(n, D, span):
+    """A gate row for each group of lanes (more than 512 times as many as rows share one)."""
+    check(n, D, F32, F32, gate="linear", span=span, post="layer", pre="rms")
+    check(n, D, F32, BF16, gate="sigmoid", span=span, gtype=BF16, post="rms", pre="layer")
+    check(n, D, BF16, BF16, gate="linear", span=span, gtype=F32, post="none", pre="none")
+
+
 def test_many_rows():
     check(9001, 40, F32, F32, gate="linear", span=9001, post="layer", pre="layer")
     check(5003, 264, BF16, BF16, gate="sigmoid", span=1)
