@@ -105,7 +105,6 @@ __host__ __device__ inline double power_of(double b, int64_t t) {
   return r;
 }
 __host__ __device__ inline void bias_constants(const AdamwParams& p, int64_t t, AdamwStep& s) {
-  if (t < 1) t = 1;
   s.lr_m = (float)(p.lr / (1.0 - power_of(p.beta1, t)));
   s.r_scale = (float)(1.0 / sqrt(1.0 - power_of(p.beta2, t)));
 }
@@ -305,7 +304,7 @@ adamw_kernel(const AdamwChunk* __restrict__ list, int64_t chunks, AdamwParams hp
   const float coef = coef_device ? *coef_device : 1.0f;
   if (coef == 0.0f) return;   // the gradients' norm was not finite: no step
   if (t_device) {
-    t = *t_device;
+    t = *t_device < 1 ? 1 : *t_device;   // also of what the rounding is drawn from
     bias_constants(hp, t, s);
   }
   const uint32_t step_key = mix_bits(seed + (uint32_t)t);
