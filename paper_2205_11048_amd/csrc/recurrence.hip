@@ -936,9 +936,23 @@ static hipError_t scan_as(const ScanArgs& a, void* ws, int32_t* err, hipStream_t
   return scan_in<X, kScanLanes, V, GRAD>(a, ws, err, stream);
 }
 
+// Sequences of no positions at all: each hands on its state, or its state's gradient.
+__global__ void __launch_bounds__(kScanBlock)
+scan_empty_kernel(const float* __restrict__ from, float* __restrict__ to, int64_t count) {
+  const int64_t step = (int64_t)gridDim.x * kScanBlock;
+  for (int64_t i = (int64_t)blockIdx.x * kScanBlock + threadIdx.x; i < count; i += step) to[i] = from ? from[i] : 0.0f;
+}
+static hipError_t scan_empty(const float* from, float* to, int64_t count, hipStream_t stream) {
+  if (!to || to == from) return hipSuccess;
+  const int64_t blocks = std::min(ceil_div(count, kScanBlock), int64_t(1) << 20);
+  hipLaunchKernelGGL(scan_empty_kernel, dim3((unsigned)blocks), dim3(kScanBlock), 0, stream, from, to, count);
+  return hipGetLastError();
+}
+
 template <bool GRAD>
 static hipError_t launch_scan(const RecurrenceArgs& r, void* ws, int32_t* err, hipStream_t stream) {
-  if (r.n == 0 && !r.offsets) return hipSuccess;
+  if (r.n == 0 && !r.offsets)
+    return GRAD ? scan_empty(r.dh_last, r.dh0, r.B * r.D, stream) : scan_empty(r.h0, r.h_last, r.B * r.D, stream);
   ScanArgs a{};
   a.r = r;
   if (r.offsets) a.seq = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + scan_room(r.n, r.D).seq);
