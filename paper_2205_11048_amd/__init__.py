@@ -820,14 +820,14 @@ def _addresses(*tensors):
 
 
 def _gate_matrix(gate, gate_kind, gate_span, n, D):
+    if gate_span < 1:
+        raise GBAError(f"gate_span: expected 1 or more, got {gate_span}")
     if gate is None:
         if gate_kind != GATE_NONE:
             raise GBAError("gate: missing")
         return 0, D
     if gate_kind == GATE_NONE:
         raise GBAError("gate: given with GATE_NONE")
-    if gate_span < 1:
-        raise GBAError(f"gate_span: expected 1 or more, got {gate_span}")
     return _matrix(gate, "gate", -(-n // gate_span), D)
 
 
