@@ -750,6 +750,13 @@ gba_status gba_recurrence_grad(const void* dh, int64_t dh_stride, const void* x,
  *                 between two codes is rounded up with the probability of its
  *                 fraction, by a hash of seed, t, the tensor's place in the list and
  *                 the element's place in the tensor: the same call gives the same bits.
+ *                 What 8 bits hold: the least code of m is 2^-17, of v's root 2^-18 of 2^(E - 127),
+ *                 and less than that becomes it or 0, by chance.  Down to gradients of 2^-12 of
+ *                 a block's largest, steps are those of 32 bits with some noise; an element below
+ *                 2^-14 of it may lose its root and keep an m, and only eps then bounds its step:
+ *                 with eps no less than these least codes (about 2^-17 of the block's largest m
+ *                 and root) it stays near lr, with eps far below it can be thousands of times lr.
+ *                 Tensors whose neighbours differ by more belong in 32 bits.
  *   copy          n elements of copy_type that get the updated parameters as well; may be NULL.
  *   decay         what this tensor takes of the weight decay (0 for none, 1 for all of it).
  * gba_adamw_list_size, gba_adamw_list_fill: as gba_tensor_list_*.

@@ -980,7 +980,9 @@ def gba_adamw_list(params, grads, m, v, m_exps=None, v_exps=None, copies=None, d
     """Describes ``params`` (contiguous float32) with their gradients (contiguous
     float32, bfloat16 or float16) and moments: float32 tensors of the same
     sizes, or uint8 ones with an exponent (uint8) for every MOMENT_BLOCK elements in
-    ``m_exps`` and ``v_exps``; all of them zeros before the first step.
+    ``m_exps`` and ``v_exps``; all of them zeros before the first step.  8 bits are for
+    blocks whose gradients are within 2^12 of each other, or an eps of no less than 2^-17 of a
+    block's largest moment: smaller elements may otherwise take steps of many times lr.
     ``copies``: tensors (or None) that get the updated parameters in their own
     type.  ``decays``: each one's part of the weight decay (default 1).  As with
     gba_tensor_list, the list is of addresses: it is made again when a tensor is replaced."""

@@ -12,8 +12,11 @@
 // moment by far less than the distance of two codes (1 - b2 is 1/1000), which
 // rounding to the nearest would lose every time: a code is rounded up with the
 // probability of the fraction that it leaves, by a hash of the seed, the step
-// and the element's place, so the moments are right on average and the same
-// call gives the same bits.
+// and the element's place, so m and the root are right on average and the same
+// call gives the same bits.  The step, a quotient of the two, is not: a root
+// that became 0 beside an m that did not leaves it to eps (the largest step of
+// gradients at 2^-18 of a block's largest of 1e-2, moments in 32 bits 1.2 lr: 13 lr at
+// eps 1e-8, 4e4 at 1e-12, 0.9 at 2^-23, which is m's least code there).
 //
 // The list is cut into chunks of kAdamwChunk elements on the host, once, as the
 // list of clipping is: a chunk's record holds all that a block needs.
