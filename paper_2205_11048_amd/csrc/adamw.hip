@@ -21,9 +21,9 @@
 // The list is cut into chunks of kAdamwChunk elements on the host, once, as the
 // list of clipping is: a chunk's record holds all that a block needs.
 //
-// Bound by bytes: 16 M parameters with moments in 32 bits 70 us (417 MB, 5.9 TB/s),
-// 200 M with moments in 8 bits, gradients and a copy in 16 550 us (3.2 GB, 5.8 TB/s),
-// the moments read back 185 us each (1 GB).  Four elements of a thread and a block for each chunk:
+// Bound by bytes: 16 M parameters with moments in 32 bits 72 us (417 MB, 5.8 TB/s),
+// 200 M with moments in 8 bits, gradients and a copy in 16 565 us (3.2 GB, 5.7 TB/s),
+// the moments read back 190 us each (1 GB).  Four elements of a thread and a block for each chunk:
 // with sixteen of a thread the loads of a block wait for its arithmetic (830 us of the
 // 200 M), with 4096 blocks that take chunks in turn 650.  Read and written past the
 // caches: 16 M 94 us -> 82 (both with sixteen of a thread).

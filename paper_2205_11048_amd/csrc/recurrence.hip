@@ -24,9 +24,9 @@
 // sequence's beginning on (nothing where that ends with the part).  A block of the
 // second launch joins the maps of those parts that the sequence passes before.
 //
-// Bound by bytes: 32 sequences of 1024 positions of 2048 columns bf16 92 us (403 MB,
-// 4.4 TB/s where a large copy has 5.2), their like of 1024 columns f32 75; the
-// gradient over 16 of 2048 of 2048 bf16 166 to 171 us (805 MB, 4.8 TB/s).  Cut sequences
+// Bound by bytes: 32 sequences of 1024 positions of 2048 columns bf16 94 to 98 us (403 MB,
+// 4.2 TB/s where a large copy has 5.2), their like of 1024 columns f32 75; the
+// gradient over 16 of 2048 of 2048 bf16 172 us (805 MB, 4.7 TB/s).  Cut sequences
 // are read twice in part: the gradient over one of 100,003 positions of 511
 // columns f32 336 us, of which the maps are 74.
 #include <algorithm>
@@ -61,8 +61,9 @@ __host__ __device__ static inline int64_t ceil_div(int64_t a, int64_t b) { retur
 static inline size_t align_up(size_t x) { return (x + 255) & ~size_t(255); }
 
 // ---------------------------------------------------------------- the gate
-// f = sigmoid(a) and i = 1 - f, each within a few u of itself, or (not FINE:
-// 16-bit types, whose values carry 2^-9 or 2^-12 anyway) |a| u more.
+// f = sigmoid(a) and i = 1 - f, each within a few u of itself (0 below the normal
+// numbers), or (not FINE: 16-bit types, whose values carry 2^-9 or 2^-12 anyway)
+// |a| u more, also in the states of 32 bits.
 template <bool FINE>
 __device__ __forceinline__ void gate_of(float a, float& f, float& i) {
   const float y = -1.44269504f * fabsf(a);
@@ -892,7 +893,9 @@ static hipError_t scan_in(ScanArgs a, void* ws, int32_t* err, hipStream_t stream
     a.part_S = reinterpret_cast<float*>(base + room.S);
     if (GRAD ? r.dh_last && r.dh0 : r.h0 && r.h_last) a.state = reinterpret_cast<float*>(base + room.state);
   } else {
-    a.part_len = (int32_t)(ceil_div(a.part_len, a.length) * a.length);   // (no more than n)
+    // (no more than n; one sequence more than blocks of one round take makes two of each block: 32 x 1024 x 2048 bf16 98 us,
+    // 33 164, 64 176)
+    a.part_len = (int32_t)(ceil_div(a.part_len, a.length) * a.length);
   }
   a.parts = (int32_t)ceil_div(r.n, a.part_len);
   const int64_t blocks = (int64_t)a.parts * a.groups;

@@ -2,12 +2,13 @@
 //   e = dh + pre'(dy),  dx = alpha e,  dz = post'(act(gate) e),
 //   dgate = act'(gate) sum e u over the rows that share a gate row.
 //
-// Bound by bytes: 16,384 x 4096 bf16 with a gate for each 1024 rows 166 us (805 MB,
-// 4.8 TB/s), 131,071 x 64 f32 with a gate for each row 61 (270 MB, 4.4); a second launch
-// of 4 to 6 us joins the blocks' sums where there are several.  Four columns of a thread: with
+// Bound by bytes: 16,384 x 4096 bf16 with a gate for each 1024 rows 170 us (805 MB,
+// 4.7 TB/s), 131,071 x 64 f32 with a gate for each row 63 (270 MB, 4.3); a second launch
+// of 4 to 8 us joins the blocks' sums where there are several.  Four columns of a thread: with
 // eight and twice the registers half as many waves wait for each other at two sums a
 // row (264 us).  Rows of 4097 to 8192 columns take eight, spill, and read the weights
-// again (8000 x 8192 bf16 268 us, 2.9 TB/s); wider ones are read three times.
+// again (8000 x 8192 bf16 270 us, 2.9 TB/s); wider ones are read three times (4000 x 16,384
+// bf16 813).  Threads of a row go by powers of two: 32,548 x 1154 bf16 139 us (3.2 TB/s).
 #include "residual_norm.hpp"
 
 namespace gba {
